@@ -1,0 +1,353 @@
+"""Performance cases of the layer operators that stand without a model handle.
+
+Four operators of a diffusion-transformer layer, as a control program calls them
+through ``paper_2609_34608_amd.runtime``:
+
+  rope      rotary positions over (time, height, width) of q and k, with or
+            without the per-head RMS norm in front: ``rope``
+  norm      post-norm of a block's output, gate, scaled residual and the pre-norm
+            with modulation of the next block: ``norm_residual``
+  quantize  8-bit blocks of activations (1 x 128): ``quantize_fp8``
+  product   the product of two e4m3 matrices with a scale per block of 128
+            (activations 1 x 128, weights 128 x 128): ``matmul_fp8``
+
+Where ``own`` is false ``run`` computes the same in elementary torch operations.
+Inputs stand in for what the layers of a trained model hold: unit-normal hidden
+states whose residual stream has grown, weights N(0, 0.02^2), gates and
+modulations of order 0.3, gains near one, positions of a video grid.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEVICE = "cuda:0"
+BLOCK = 128
+E4M3_MAX = 448.0
+TINY = 2.0 ** -126
+EPS = 1e-6
+F8 = torch.float8_e4m3fn
+DTYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "e4m3": F8}
+SIZE = {"fp32": 4, "bf16": 2, "e4m3": 1}
+
+
+def _rope(name, B, T, Hq, Hk, dh, sections, dtype="bf16", layout="halves", norm=False, far=0, head_major=False):
+    return dict(name=name, kind="rope", B=B, T=T, Hq=Hq, Hk=Hk, dh=dh, s0=sections[0], s1=sections[1], s2=sections[2],
+                dtype=dtype, layout=layout, norm=norm, far=far, head_major=head_major)
+
+
+def _norm(name, B, T, D, y="bf16", h="fp32", u="bf16", post="rms", pre="layer", res_scale=1.0, per_row=False):
+    return dict(name=name, kind="norm", B=B, T=T, D=D, y=y, h=h, u=u, post=post, pre=pre, res_scale=res_scale,
+                per_row=per_row)
+
+
+def listed():
+    return [
+        # q and k of one new action row of the single-arm model (launch latency)
+        _rope("rope_one_row", 1, 1, 12, 12, 64, (8, 12, 12), dtype="fp32", layout="pairs", far=100000),
+        # two samples of odd length, an odd head count, QK-norm in front, heads before rows in memory
+        _rope("rope_normed_ragged", 2, 2877, 19, 19, 64, (8, 12, 12), norm=True, head_major=True),
+        # q and k of one layer of the long-horizon model
+        _rope("rope_large", 1, 10176, 24, 24, 64, (8, 12, 12)),
+        # around the attention block of the action-only model, float32
+        _norm("norm_action_fp32", 1, 137, 512, y="fp32", u="fp32"),
+        # around a block of the bimanual model, four samples, modulation per row (a noise level per frame)
+        _norm("norm_mid", 4, 2306, 1024, per_row=True),
+        # the long-horizon model, the result straight into 8-bit blocks
+        _norm("norm_large_e4m3", 1, 10176, 1536, u="e4m3", res_scale=0.7071067811865476),
+        # activations in front of an 8-bit projection: off the blocks of 128
+        dict(name="quantize_ragged", kind="quantize", M=2754, K=1216, dtype="bf16"),
+        # the hidden layer of the long-horizon model's MLP
+        dict(name="quantize_large", kind="quantize", M=10176, K=6144, dtype="bf16"),
+        # one new row through the QKV projection of the long-horizon model
+        dict(name="product_one_row", kind="product", M=1, N=4608, K=1536, out="bf16", gelu=False),
+        # the QKV projection of the single-arm model, float32 result
+        dict(name="product_small_fp32", kind="product", M=864, N=2304, K=768, out="fp32", gelu=False),
+        # an output width and a depth off the tiles and the blocks of 128
+        dict(name="product_ragged", kind="product", M=5754, N=3243, K=1216, out="bf16", gelu=False),
+        # the MLP-up projection of the long-horizon model with its GELU
+        dict(name="product_large", kind="product", M=10176, N=6144, K=1536, out="bf16", gelu=True),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    kind = rng.choice(["rope", "rope", "norm", "norm", "quantize", "product", "product", "product"])
+    if kind == "rope":
+        dh = rng.choice([32, 64, 64, 64, 128])
+        B, T = rng.randint(1, 4), _log_int(rng, 1, 8000)
+        Hq = rng.randint(1, max(1, min(24, 24 * 10176 * 64 // (B * T * dh))))
+        Hk = rng.choice([Hq, Hq, rng.randint(1, Hq)])
+        rotated = rng.choice([dh // 2, dh // 2, dh // 4])
+        s1 = rng.randint(1, rotated // 3)
+        s2 = rng.choice([s1, s1, 0])
+        case = _rope("", B, T, Hq, Hk, dh, (rotated - s1 - s2, s1, s2), rng.choice(["bf16", "bf16", "fp32"]),
+                     rng.choice(["halves", "pairs"]), rng.random() < 0.5, rng.choice([0, 0, 5000, 100000]),
+                     rng.random() < 0.5)
+    elif kind == "norm":
+        D = rng.choice([64 * rng.randint(1, 32), 64 * rng.randint(1, 32), rng.randint(33, 2048)])
+        B = rng.randint(1, 4)
+        T = max(1, min(_log_int(rng, 1, 10000), 10000 * 1536 // (B * D)))
+        h = rng.choice(["fp32", "fp32", "bf16"])
+        case = _norm("", B, T, D, rng.choice(["bf16", "bf16", "fp32"]), h, rng.choice(["bf16", "fp32", "e4m3"]),
+                     rng.choice(["rms", "rms", "layer", "none"]), rng.choice(["layer", "layer", "rms"]),
+                     rng.choice([1.0, 1.0, 0.7071067811865476]), rng.random() < 0.3)
+    elif kind == "quantize":
+        K = rng.choice([64 * rng.randint(2, 96), rng.randint(100, 6144)])
+        case = dict(name="", kind=kind, M=_log_int(rng, 1, 10000), K=K, dtype=rng.choice(["bf16", "bf16", "fp32"]))
+    else:
+        while True:
+            M = _log_int(rng, 1, 10000)
+            N = rng.choice([64 * rng.randint(4, 96), rng.randint(200, 6144)])
+            K = rng.choice([64 * rng.randint(4, 96), rng.randint(200, 6144)])
+            if M * N * K <= 9e10:
+                break
+        case = dict(name="", kind=kind, M=M, N=N, K=K, out=rng.choice(["bf16", "bf16", "fp32"]),
+                    gelu=rng.random() < 0.3)
+    del case["name"]
+    return case
+
+
+# ------------------------------------------------------------------ inputs
+def _randn(seed, stream, *shape):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(1000003 * int(seed) + stream)
+    return torch.randn(*shape, generator=g, device=DEVICE, dtype=torch.float32)
+
+
+def _frequencies(sections, theta=10000.0):
+    """theta^(-j / n) for pair j of an axis of n pairs, axis after axis."""
+    return [theta ** (-j / n) for n in sections for j in range(n)]
+
+
+def _positions(T, far):
+    """(time, height, width) of row-major video rows; frames three quarters of a step apart."""
+    i = torch.arange(T, device=DEVICE)
+    g = max(1, int(math.sqrt(T / 8)))
+    return torch.stack([0.75 * (i // (g * g)) + far, (i // g) % g, i % g], dim=1).to(torch.float32)
+
+
+def _padded(x):
+    """The same e4m3 matrix with rows a multiple of 16 bytes apart."""
+    M, K = x.shape
+    buf = torch.zeros((M, -(-K // 16) * 16), dtype=x.dtype, device=x.device)
+    buf[:, :K] = x
+    return buf[:, :K]
+
+
+def _inputs(case, seed):
+    kind = case["kind"]
+    if kind == "rope":
+        B, T, dh, dt = case["B"], case["T"], case["dh"], DTYPES[case["dtype"]]
+
+        def heads(stream, H):
+            if case["head_major"]:
+                return (1.5 * _randn(seed, stream, B, H, T, dh)).to(dt).transpose(1, 2)
+            return (1.5 * _randn(seed, stream, B, T, H, dh)).to(dt)
+
+        s = (case["s0"], case["s1"], case["s2"])
+        return dict(q=heads(1, case["Hq"]), k=heads(2, case["Hk"]), pos=_positions(T, case["far"]), sections=s,
+                    q_gain=1.0 + 0.1 * _randn(seed, 3, dh) if case["norm"] else None,
+                    k_gain=1.0 + 0.1 * _randn(seed, 4, dh) if case["norm"] else None)
+    if kind == "norm":
+        B, T, D = case["B"], case["T"], case["D"]
+        rows = T if case["per_row"] else 1
+        return dict(h=(3.0 * _randn(seed, 1, B, T, D)).to(DTYPES[case["h"]]),
+                    y=(0.5 * _randn(seed, 2, B, T, D)).to(DTYPES[case["y"]]),
+                    gate=0.3 * _randn(seed, 3, B, rows, D), shift=0.3 * _randn(seed, 4, B, rows, D),
+                    scale=0.3 * _randn(seed, 5, B, rows, D), post_gain=1.0 + 0.1 * _randn(seed, 6, D))
+    if kind == "quantize":
+        return dict(x=_randn(seed, 1, case["M"], case["K"]).to(DTYPES[case["dtype"]]))
+    M, N, K = case["M"], case["N"], case["K"]
+    qa, sa = _quantize(_randn(seed, 1, M, K), 1)
+    qw, sw = _quantize(0.02 * _randn(seed, 2, N, K), BLOCK)
+    return dict(a=_padded(qa), a_scale=sa, w=_padded(qw), w_scale=sw, bias=0.02 * _randn(seed, 3, N))
+
+
+def prepare(case, seed):
+    t = _inputs(case, seed)
+    if case["kind"] == "rope":
+        t["freq"] = torch.tensor(_frequencies(t["sections"]), dtype=torch.float64, device=DEVICE)
+        # what a program keeps for the call: the ladder on the host, the result's buffers
+        t["ladder"] = _frequencies(t["sections"])
+        t["q_out"], t["k_out"] = torch.empty_like(t["q"]), torch.empty_like(t["k"])
+    return dict(case=case, t=t)
+
+
+# ------------------------------------------------------------------ plain forms
+def _rms(x):
+    return x * torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS)
+
+
+def _layer(x):
+    return _rms(x - x.mean(-1, keepdim=True))
+
+
+def _quantize(x, rows):
+    """e4m3 values and float32 scales of blocks of (rows x 128)."""
+    M, K = x.shape
+    mb, kb = -(-M // rows), -(-K // BLOCK)
+    p = torch.nn.functional.pad(x, (0, kb * BLOCK - K, 0, mb * rows - M)).view(mb, rows, kb, BLOCK)
+    amax = p.abs().amax(dim=(1, 3))
+    s = torch.where(amax > 0, (amax / E4M3_MAX).clamp_min(TINY), torch.ones_like(amax))
+    q = (p / s[:, None, :, None]).to(F8)
+    return q.view(mb * rows, kb * BLOCK)[:M, :K], s
+
+
+def _values(q, s, rows):
+    """float32 matrix that e4m3 blocks of (rows x 128) stand for."""
+    M, K = q.shape
+    full = s.repeat_interleave(rows, 0)[:M].repeat_interleave(BLOCK, 1)[:, :K]
+    return q.to(torch.float32) * full
+
+
+def _rotate(x, gain, cos, sin, layout):
+    v = x.to(torch.float32)
+    if gain is not None:
+        v = _rms(v) * gain
+    P = cos.shape[-1]
+    if layout == "halves":
+        a, b = v[..., :P], v[..., P:2 * P]
+    else:
+        a, b = v[..., 0:2 * P:2], v[..., 1:2 * P:2]
+    ra, rb = a * cos - b * sin, a * sin + b * cos
+    r = torch.cat([ra, rb], -1) if layout == "halves" else torch.stack([ra, rb], -1).flatten(-2)
+    return torch.cat([r, v[..., 2 * P:]], -1).to(x.dtype)
+
+
+def _plain(case, t):
+    kind = case["kind"]
+    if kind == "rope":
+        axis = torch.repeat_interleave(torch.arange(3, device=DEVICE),
+                                       torch.tensor(t["sections"], device=DEVICE), output_size=len(t["ladder"]))
+        ang = t["pos"].to(torch.float64)[:, axis] * t["freq"]
+        cos, sin = ang.cos().to(torch.float32)[:, None, :], ang.sin().to(torch.float32)[:, None, :]
+        return [_rotate(t["q"], t["q_gain"], cos, sin, case["layout"]),
+                _rotate(t["k"], t["k_gain"], cos, sin, case["layout"])]
+    if kind == "norm":
+        y, h = t["y"].to(torch.float32), t["h"].to(torch.float32)
+        if case["post"] != "none":
+            y = (_rms(y) if case["post"] == "rms" else _layer(y)) * t["post_gain"]
+        h = case["res_scale"] * h + t["gate"] * y
+        u = (_rms(h) if case["pre"] == "rms" else _layer(h)) * (1.0 + t["scale"]) + t["shift"]
+        out = [h.to(t["h"].dtype)]
+        if case["u"] == "e4m3":
+            q, s = _quantize(u.view(-1, case["D"]), 1)
+            return out + [q.view(u.shape), s.view(*u.shape[:2], -1)]
+        return out + [u.to(DTYPES[case["u"]])]
+    if kind == "quantize":
+        return list(_quantize(t["x"].to(torch.float32), 1))
+    c = _values(t["a"], t["a_scale"], 1) @ _values(t["w"], t["w_scale"], BLOCK).t() + t["bias"]
+    if case["gelu"]:
+        c = 0.5 * c * (1.0 + torch.tanh(math.sqrt(2.0 / math.pi) * (c + 0.044715 * c * c * c)))
+    return c.to(DTYPES[case["out"]])
+
+
+def _calls(case, t):
+    from paper_2609_34608_amd import runtime as R
+
+    kind = case["kind"]
+    if kind == "rope":
+        return list(R.rope(t["q"], t["k"], t["pos"], t["sections"], t["ladder"], layout=case["layout"],
+                           q_gain=t["q_gain"], k_gain=t["k_gain"], eps=EPS, q_out=t["q_out"], k_out=t["k_out"]))
+    if kind == "norm":
+        return list(R.norm_residual(t["h"], t["y"], post=case["post"], post_gain=t["post_gain"], gate=t["gate"],
+                                    res_scale=case["res_scale"], pre=case["pre"], scale=t["scale"], shift=t["shift"],
+                                    eps=EPS, u_dtype=DTYPES[case["u"]]))
+    if kind == "quantize":
+        return list(R.quantize_fp8(t["x"]))
+    return R.matmul_fp8(t["a"], t["a_scale"], t["w"], t["w_scale"], bias=t["bias"], gelu=case["gelu"],
+                        out_dtype=DTYPES[case["out"]])
+
+
+def run(state):
+    return _calls(state["case"], state["t"]) if own else _plain(state["case"], state["t"])
+
+
+# ------------------------------------------------------------------ work
+def work(case):
+    kind = case["kind"]
+    if kind == "rope":
+        rows = case["B"] * case["T"]
+        n = rows * (case["Hq"] + case["Hk"]) * case["dh"]
+        return {"bytes": 2.0 * n * SIZE[case["dtype"]] + 12.0 * case["T"], "flops": (3.0 + 4.0 * case["norm"]) * n}
+    if kind == "norm":
+        n = case["B"] * case["T"] * case["D"]
+        vectors = 3 * 4.0 * (n if case["per_row"] else case["B"] * case["D"])
+        return {"bytes": n * (2.0 * SIZE[case["h"]] + SIZE[case["y"]] + SIZE[case["u"]]) + vectors, "flops": 14.0 * n}
+    if kind == "quantize":
+        n = case["M"] * case["K"]
+        return {"bytes": n * (SIZE[case["dtype"]] + 1.0 + 4.0 / BLOCK), "flops": 2.0 * n}
+    M, N, K = case["M"], case["N"], case["K"]
+    return {"bytes": float(M * K + N * K + M * N * SIZE[case["out"]] + 4 * N), "flops": 2.0 * M * N * K}
+
+
+# ------------------------------------------------------------------ in 64 bits
+def _e4m3(v):
+    """v rounded to four significant bits with exponents from -6 on, ties to even."""
+    e = torch.floor(torch.log2(v.abs().clamp_min(2.0 ** -20))).clamp_min(-6.0)
+    step = torch.exp2(e - 3.0)
+    return (torch.round(v / step) * step).clamp(-E4M3_MAX, E4M3_MAX)
+
+
+def _blocks64(x):
+    """Values and scales of the 1 x 128 blocks of the last axis, in 64 bits."""
+    *lead, K = x.shape
+    v, s = torch.empty_like(x), torch.empty(*lead, -(-K // BLOCK), dtype=torch.float64, device=x.device)
+    for j in range(s.shape[-1]):
+        part = x[..., j * BLOCK:(j + 1) * BLOCK]
+        top = part.abs().max(dim=-1).values
+        s[..., j] = torch.where(top == 0, 1.0, torch.clamp(top / E4M3_MAX, min=TINY))
+        v[..., j * BLOCK:(j + 1) * BLOCK] = _e4m3(part / s[..., j:j + 1])
+    return v, s
+
+
+def _standard64(x, kind):
+    if kind == "none":
+        return x
+    if kind == "layer":
+        x = x - x.sum(-1, keepdim=True) / x.shape[-1]
+    return x / torch.sqrt((x * x).sum(-1, keepdim=True) / x.shape[-1] + EPS)
+
+
+def exact(case, seed):
+    t = {n: v.to(torch.float64) if isinstance(v, torch.Tensor) else v for n, v in _inputs(case, seed).items()}
+    kind = case["kind"]
+    if kind == "rope":
+        out = []
+        for x, g in ((t["q"], t["q_gain"]), (t["k"], t["k_gain"])):
+            x = x if g is None else _standard64(x, "rms") * g
+            r = x.clone()
+            i, P = 0, sum(t["sections"])
+            for ax, n in enumerate(t["sections"]):
+                for j in range(n):
+                    turn = torch.polar(torch.ones_like(t["pos"][:, ax]), t["pos"][:, ax] * 10000.0 ** (-j / n))
+                    at = (i, i + P) if case["layout"] == "halves" else (2 * i, 2 * i + 1)
+                    z = torch.complex(x[..., at[0]], x[..., at[1]]) * turn[None, :, None]
+                    r[..., at[0]], r[..., at[1]] = z.real, z.imag
+                    i += 1
+            out.append(r)
+        return out
+    if kind == "norm":
+        y = t["y"] if case["post"] == "none" else _standard64(t["y"], case["post"]) * t["post_gain"]
+        h = case["res_scale"] * t["h"] + t["gate"] * y
+        u = _standard64(h, case["pre"]) * (1.0 + t["scale"]) + t["shift"]
+        return [h, *_blocks64(u)] if case["u"] == "e4m3" else [h, u]
+    if kind == "quantize":
+        return list(_blocks64(t["x"]))
+    M, N, K = case["M"], case["N"], case["K"]
+    c = torch.zeros((M, N), dtype=torch.float64, device=DEVICE)
+    for j in range(t["a_scale"].shape[1]):
+        cols = slice(j * BLOCK, min(K, (j + 1) * BLOCK))
+        part = t["a"][:, cols] @ t["w"][:, cols].t()
+        c += part * t["a_scale"][:, j:j + 1] * t["w_scale"][torch.arange(N, device=DEVICE) // BLOCK, j]
+    c += t["bias"]
+    if case["gelu"]:
+        c = c / (1.0 + torch.exp(-2.0 * math.sqrt(2.0 / math.pi) * (c + 0.044715 * c ** 3)))
+    return c

@@ -63,6 +63,7 @@ extern "C" {
 #define WAM_BF16 1 /* projection / attention operands bf16, fp32 accumulate;
                       residual stream, trajectory, layer state, norms and all
                       reductions stay float32 (or float64 for gate sums)      */
+#define WAM_FP8 2  /* as an element type: e4m3 (layer operators)               */
 
 /* ---- Residual Rescaling modes ------------------------------------------ */
 #define WAM_RR_OFF 0        /* plain full forward, no layer state kept        */
@@ -378,9 +379,142 @@ int wam_get_replan_state(wam_t h, float *x_bar, float *x_r, int32_t *kappa);
  * allocation and no hipMalloc / hipFree.  Errors: WAM_E_SHAPE for sizes
  * beyond those limits, WAM_E_ARG for invalid arguments, WAM_E_HIP for a
  * runtime error; wam_noalloc_last_error() returns this thread's message of
- * the last failing call. */
+ * the last failing call without a handle. */
 int wam_remap_noalloc(const wam_config *cfg, const wam_remap_args *args, void *hip_stream);
 const char *wam_noalloc_last_error(void);
+
+/* ---- layer operators ---------------------------------------------------------- */
+/* Operators of a transformer layer on caller-owned device buffers, without a
+ * handle: rotary positions over several axes, the norms around a block with
+ * its gate and residual, 8-bit blocks and their product.  Each is enqueued on
+ * hip_stream (NULL: the default stream) of the current device, allocates
+ * nothing, shares no scratch between calls (calls may overlap), does not
+ * synchronise and may be captured into a graph.  Struct and host pointers are
+ * read during the call only.  Strides count elements and may be any size;
+ * the last dimension is contiguous.  An input stride may be 0 (the same values
+ * for every index); the elements of an output must be distinct.  An input and
+ * an output must not overlap, except where a call says that they may be the
+ * same buffer.  A call with an empty dimension does nothing.  Errors: WAM_E_ARG
+ * for an invalid argument, WAM_E_SHAPE for a size beyond the limits stated,
+ * WAM_E_HIP for a runtime error; wam_noalloc_last_error() returns this thread's
+ * message.  Element types: WAM_FP32, WAM_BF16 and, where said, WAM_FP8 (e4m3:
+ * 4 exponent and 3 mantissa bits, largest value 448, no infinity). */
+
+/* Rotary positions.  Row t of sample b has one position per axis, pos[t][a]
+ * (time, height, width; fractions allowed), and pair i of a head, which belongs
+ * to axis 0 for i < sections[0], to axis 1 for the next sections[1], to axis 2
+ * for the rest, turns by the angle pos[t][axis(i)] * freq[i]:
+ *   (x1, x2) -> (x1 cos - x2 sin, x1 sin + x2 cos)
+ * with P = sections[0] + sections[1] + sections[2] pairs, 2 P <= dh, of
+ *   WAM_ROPE_HALVES  elements i and i + P,
+ *   WAM_ROPE_PAIRS   elements 2 i and 2 i + 1;
+ * elements from 2 P on pass unchanged.  Angles are formed in float64.  With
+ * q_gain / k_gain (float32 [dh]) each head vector x is first divided by its
+ * root mean square and multiplied by the gain: x gain / sqrt(mean(x^2) + eps);
+ * NULL leaves it out.  Results are rounded once.  q_out may be q and k_out may be k
+ * (with the same strides).  Hk = 0 leaves k out (Hq = 0: q).  dh <= 256. */
+#define WAM_ROPE_HALVES 0
+#define WAM_ROPE_PAIRS 1
+#define WAM_MAX_HEAD 256
+typedef struct {
+  int32_t B, T, Hq, Hk, dh;
+  int32_t dtype;              /* of q, k and the results: WAM_FP32 | WAM_BF16  */
+  int32_t layout;             /* WAM_ROPE_*                                    */
+  int32_t sections[3];        /* pairs of each axis, >= 0                      */
+  const void *q, *k;          /* device [B][T][H][dh] by the strides below     */
+  void *q_out, *k_out;
+  int64_t q_stride[3], k_stride[3];         /* of sample, row, head            */
+  int64_t q_out_stride[3], k_out_stride[3];
+  const float *pos;           /* device [T][3] per sample, contiguous          */
+  int64_t pos_stride;         /* floats between samples; 0: the same for all   */
+  const double *freq;         /* host [P]: radians per unit of position        */
+  const float *q_gain, *k_gain; /* device [dh] or NULL                         */
+  float eps;                  /* >= 0; used with a gain                        */
+} wam_rope_args;
+int wam_rope(const wam_rope_args *args, void *hip_stream);
+/* Frequencies of the usual ladder into freq (host [P]): pair j of an axis of n
+ * pairs gets theta^(-j / n); with shared != 0 one ladder runs over all P pairs,
+ * pair i gets theta^(-i / P).  theta > 0. */
+int wam_rope_frequencies(const int32_t *sections, double theta, int32_t shared, double *freq);
+
+/* Norms around a block.  h is the residual stream, y the block's output:
+ *   h_out = res_scale * h + gate * post(y)
+ *   u     = pre(h_out before its rounding) * (1 + scale) + shift
+ * post and pre are WAM_NORM_NONE (x), WAM_NORM_RMS (x / sqrt(mean(x^2) + eps))
+ * or WAM_NORM_LAYER ((x - mean) / sqrt(mean((x - mean)^2) + eps)), times
+ * post_gain / pre_gain (NULL: 1).  gate, scale and shift are float32 vectors of
+ * D values per row, by strides of sample and row (0: shared); NULL: gate 1,
+ * scale 0, shift 0.  y NULL: h_out = res_scale * h.  u NULL: no second part;
+ * h_out NULL: not stored (u must be asked for).  Sums are float32.  u of type
+ * WAM_FP8 is stored as blocks of 128 columns of a row, as wam_quantize_fp8
+ * does, with its float32 scales in u_scale [B][T][ceil(D / 128)].  h_out may
+ * be h and u may be y (with the same type and strides).  1 <= D <= 8192. */
+#define WAM_NORM_NONE 0
+#define WAM_NORM_RMS 1
+#define WAM_NORM_LAYER 2
+#define WAM_MAX_NORM_D 8192
+typedef struct {
+  int32_t B, T, D;
+  int32_t h_dtype, y_dtype, u_dtype; /* h and h_out, y: WAM_FP32 | WAM_BF16; u: any */
+  int32_t post, pre;                 /* WAM_NORM_*                                   */
+  const void *h, *y;                 /* device [B][T][D]                             */
+  void *h_out, *u;
+  float *u_scale;
+  int64_t h_stride[2], y_stride[2], h_out_stride[2], u_stride[2], u_scale_stride[2]; /* of sample, row */
+  const float *gate, *scale, *shift;
+  int64_t gate_stride[2], scale_stride[2], shift_stride[2];
+  const float *post_gain, *pre_gain; /* device [D] or NULL                           */
+  float res_scale, eps;
+} wam_norm_args;
+int wam_norm_residual(const wam_norm_args *args, void *hip_stream);
+
+/* 8-bit blocks: x [M][K] is cut into blocks of block_rows (1 or 128) rows and
+ * 128 columns (the last ones smaller); a block's scale is max|x| / 448 in
+ * float32, at least 2^-126 (1 where the block is zero), and q = x / scale rounded
+ * to e4m3, to nearest, ties to even.  A block with a NaN or an infinity has that
+ * as its scale, and stands for NaN.  scale: [ceil(M / block_rows)][ceil(K / 128)].
+ * Bytes of a row of q past K are left as they are. */
+typedef struct {
+  int32_t M, K;
+  int32_t dtype;       /* of x: WAM_FP32 | WAM_BF16 */
+  int32_t block_rows;  /* 1 (activations) or 128 (weights) */
+  const void *x;
+  int64_t x_stride;    /* of a row */
+  void *q;
+  int64_t q_stride;
+  float *scale;
+  int64_t scale_stride;
+} wam_quantize_args;
+int wam_quantize_fp8(const wam_quantize_args *args, void *hip_stream);
+
+/* Product of e4m3 matrices with a float32 scale per block of 128:
+ *   out[m][n] = act(sum_j a_scale[m][j] w_scale[n / 128][j]
+ *                   sum_{k in block j} a[m][k] w[n][k] + bias[n])
+ * a [M][K] with scales per row (blocks of 1 x 128), w [N][K] with scales per
+ * block of 128 x 128, as wam_quantize_fp8 makes them.  Block products and their
+ * scaled sum are float32; with a bf16 result the products of 8 consecutive k are
+ * cut below 2^-13 of the power of two of the largest of them (the 8-bit matrix
+ * instruction), with a float32 result they are not.  a and w must start on 16 bytes and their row strides
+ * be multiples of 16; the bytes of a row past K may hold anything.  act:
+ * WAM_ACT_NONE or WAM_ACT_GELU (tanh form).  out: WAM_FP32 | WAM_BF16. */
+#define WAM_ACT_NONE 0
+#define WAM_ACT_GELU 1
+typedef struct {
+  int32_t M, N, K;
+  int32_t out_dtype, act;
+  const void *a;
+  int64_t a_stride;
+  const float *a_scale;
+  int64_t a_scale_stride;
+  const void *w;
+  int64_t w_stride;
+  const float *w_scale;
+  int64_t w_scale_stride;
+  const float *bias;   /* device [N] or NULL */
+  void *out;
+  int64_t out_stride;
+} wam_matmul_args;
+int wam_matmul_fp8(const wam_matmul_args *args, void *hip_stream);
 
 /* ---- measurement ------------------------------------------------------------ */
 /* Time every launch of kernel class kc (WAM_KC_*), up to max_launches

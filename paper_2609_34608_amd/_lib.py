@@ -13,7 +13,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "lib", "libwam.so")
 
 WAM_OK, WAM_E_ARG, WAM_E_SHAPE, WAM_E_STATE, WAM_E_HIP, WAM_E_WORKSPACE, WAM_E_UNSUPPORTED = 0, -1, -2, -3, -4, -5, -6
-WAM_FP32, WAM_BF16 = 0, 1
+WAM_FP32, WAM_BF16, WAM_FP8 = 0, 1, 2
 WAM_RR_OFF, WAM_RR_AUTO, WAM_RR_FORCE_SKIP, WAM_RR_FORCE_FULL = 0, 1, 2, 3
 WAM_RR_JOINT, WAM_RR_SINGLE = 0, 1
 WAM_ADAPT_REMAP, WAM_ADAPT_RESET_LAYER, WAM_ADAPT_RESET_ALL, WAM_ADAPT_SET_REPLAN, WAM_ADAPT_REBIND = 1, 2, 3, 4, 5
@@ -23,6 +23,10 @@ WAM_OPT_DEVICE_DECISION, WAM_OPT_GRAPHS, WAM_OPT_ATTENTION = 1, 2, 3
 WAM_ATTN_AUTO, WAM_ATTN_RUNNING_MAX, WAM_ATTN_BOUNDED, WAM_ATTN_PINGPONG, WAM_ATTN_PLAIN = 0, 1, 2, 3, 4
 (WAM_KC_GEMM_QKV, WAM_KC_GEMM_PROJ, WAM_KC_GEMM_FC1, WAM_KC_GEMM_FC2, WAM_KC_ATTENTION,
  WAM_KC_RR_GATE, WAM_KC_RR_INJECT, WAM_KC_RR_REFRESH, WAM_KC_COUNT) = range(9)
+
+WAM_ROPE_HALVES, WAM_ROPE_PAIRS, WAM_MAX_HEAD = 0, 1, 256
+WAM_NORM_NONE, WAM_NORM_RMS, WAM_NORM_LAYER, WAM_MAX_NORM_D = 0, 1, 2, 8192
+WAM_ACT_NONE, WAM_ACT_GELU = 0, 1
 
 KERNEL_CLASS_NAMES = ["gemm_qkv", "gemm_proj", "gemm_fc1", "gemm_fc2", "attention",
                       "rr_gate", "rr_inject", "rr_refresh"]
@@ -79,6 +83,39 @@ class WamReplanInfo(C.Structure):
                 ("S", C.c_double), ("decision", C.c_int8 * WAM_MAX_STEPS)]
 
 
+class WamRopeArgs(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hk", C.c_int32), ("dh", C.c_int32),
+                ("dtype", C.c_int32), ("layout", C.c_int32), ("sections", C.c_int32 * 3),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("q_out", C.c_void_p), ("k_out", C.c_void_p),
+                ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("q_out_stride", C.c_int64 * 3),
+                ("k_out_stride", C.c_int64 * 3), ("pos", C.c_void_p), ("pos_stride", C.c_int64),
+                ("freq", C.c_void_p), ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("eps", C.c_float)]
+
+
+class WamNormArgs(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("D", C.c_int32), ("h_dtype", C.c_int32),
+                ("y_dtype", C.c_int32), ("u_dtype", C.c_int32), ("post", C.c_int32), ("pre", C.c_int32),
+                ("h", C.c_void_p), ("y", C.c_void_p), ("h_out", C.c_void_p), ("u", C.c_void_p),
+                ("u_scale", C.c_void_p), ("h_stride", C.c_int64 * 2), ("y_stride", C.c_int64 * 2),
+                ("h_out_stride", C.c_int64 * 2), ("u_stride", C.c_int64 * 2), ("u_scale_stride", C.c_int64 * 2),
+                ("gate", C.c_void_p), ("scale", C.c_void_p), ("shift", C.c_void_p), ("gate_stride", C.c_int64 * 2),
+                ("scale_stride", C.c_int64 * 2), ("shift_stride", C.c_int64 * 2), ("post_gain", C.c_void_p),
+                ("pre_gain", C.c_void_p), ("res_scale", C.c_float), ("eps", C.c_float)]
+
+
+class WamQuantizeArgs(C.Structure):
+    _fields_ = [("M", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("block_rows", C.c_int32),
+                ("x", C.c_void_p), ("x_stride", C.c_int64), ("q", C.c_void_p), ("q_stride", C.c_int64),
+                ("scale", C.c_void_p), ("scale_stride", C.c_int64)]
+
+
+class WamMatmulArgs(C.Structure):
+    _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("out_dtype", C.c_int32), ("act", C.c_int32),
+                ("a", C.c_void_p), ("a_stride", C.c_int64), ("a_scale", C.c_void_p), ("a_scale_stride", C.c_int64),
+                ("w", C.c_void_p), ("w_stride", C.c_int64), ("w_scale", C.c_void_p), ("w_scale_stride", C.c_int64),
+                ("bias", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64)]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "wam_host_weight_count": (C.c_size_t, [C.POINTER(WamConfig)]),
@@ -115,6 +152,11 @@ EXPORTS = {
                                    C.POINTER(C.c_double)]),
     "wam_remap_noalloc": (C.c_int, [C.POINTER(WamConfig), C.POINTER(WamRemapArgs), C.c_void_p]),
     "wam_noalloc_last_error": (C.c_char_p, []),
+    "wam_rope": (C.c_int, [C.POINTER(WamRopeArgs), C.c_void_p]),
+    "wam_rope_frequencies": (C.c_int, [C.POINTER(C.c_int32), C.c_double, C.c_int32, C.POINTER(C.c_double)]),
+    "wam_norm_residual": (C.c_int, [C.POINTER(WamNormArgs), C.c_void_p]),
+    "wam_quantize_fp8": (C.c_int, [C.POINTER(WamQuantizeArgs), C.c_void_p]),
+    "wam_matmul_fp8": (C.c_int, [C.POINTER(WamMatmulArgs), C.c_void_p]),
     "wam_probe_mfma_bf16": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.POINTER(C.c_double),
                                       C.POINTER(C.c_double)]),
     "wam_probe_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.POINTER(C.c_double),

@@ -1,0 +1,60 @@
+// Product of e4m3 matrices with block scales: checks and dispatch of
+// wam_matmul_fp8 for the kernels of gemm_fp8.h.
+#include "gemm_fp8.h"
+
+namespace wam {
+
+namespace {
+
+template <int BM, int BN, int WGM, int WGN, int ST>
+hipError_t launch_fp8(const gemm::Fp8Operands& p, const gemm::Fp8Out& o, hipStream_t s) {
+  const int64_t blocks = (int64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN);
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks);
+  if (o.bf16_out) launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, false>, grid, WGM * WGN * 64, 0, s, p, o);
+  else launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, true>, grid, WGM * WGN * 64, 0, s, p, o);
+  return hipGetLastError();
+}
+
+bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)n == 0; }
+
+}  // namespace
+
+}  // namespace wam
+
+using namespace wam;
+
+extern "C" int wam_matmul_fp8(const wam_matmul_args* a, void* hip_stream) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: null argument");
+  if (a->M < 0 || a->N < 0 || a->K < 0) return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: sizes must be >= 0");
+  if (a->out_dtype != WAM_FP32 && a->out_dtype != WAM_BF16)
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: out must be WAM_FP32 or WAM_BF16");
+  if (a->act != WAM_ACT_NONE && a->act != WAM_ACT_GELU)
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: unknown activation");
+  if (a->M == 0 || a->N == 0) return WAM_OK;
+  if (a->K == 0) return noalloc_fail(WAM_E_SHAPE, "wam_matmul_fp8: K must be >= 1");
+  constexpr int kMaxDim = 0x7fffffff - 1024;  // tile arithmetic stays in 31 bits
+  if (a->M > kMaxDim || a->N > kMaxDim || a->K > kMaxDim)
+    return noalloc_fail(WAM_E_SHAPE, "wam_matmul_fp8: a size is too large");
+  if (!a->a || !a->a_scale || !a->w || !a->w_scale || !a->out)
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: null buffer");
+  if (!aligned_to(a->a, 16) || !aligned_to(a->w, 16) || (a->M > 1 && a->a_stride % 16) ||
+      (a->N > 1 && a->w_stride % 16))
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: a and w must start on 16 bytes, their rows a multiple of 16 apart");
+  if ((a->M > 1 && a->a_stride < a->K) || (a->N > 1 && a->w_stride < a->K))
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: rows of a and w must not overlap");
+  if (a->a_scale_stride < 0 || a->w_scale_stride < 0 || !aligned_to(a->a_scale, 4) || !aligned_to(a->w_scale, 4) ||
+      !aligned_to(a->bias, 4))
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: scales must be aligned, their strides >= 0");
+  const int64_t esize = a->out_dtype == WAM_FP32 ? 4 : 2;
+  if ((a->M > 1 && a->out_stride < a->N) || !aligned_to(a->out, esize))
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: rows of out must be distinct and aligned to their elements");
+  if (a->out == a->a || a->out == a->w) return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: out must not be a or w");
+  gemm::Fp8Operands p{static_cast<const uint8_t*>(a->a), static_cast<const uint8_t*>(a->w), a->a_scale, a->w_scale,
+                      a->a_stride, a->w_stride, a->a_scale_stride, a->w_scale_stride, a->M, a->N, a->K};
+  gemm::Fp8Out o{a->bias, a->out, a->out_stride, a->out_dtype == WAM_BF16, a->act == WAM_ACT_GELU,
+                 aligned_to(a->out, 4 * esize) && a->out_stride % 4 == 0};
+  if (launch_fp8<128, 128, 2, 2, 2>(p, o, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+    return noalloc_fail(WAM_E_HIP, "wam_matmul_fp8: kernel launch failed");
+  return WAM_OK;
+}

@@ -1,0 +1,392 @@
+// Layer operators behind the handle-free entry points of wam.h (gfx950): rotary
+// positions over several axes, the norms around a block with its gate and
+// residual, and the quantisation into e4m3 blocks.  All are bound by memory:
+// each reads its inputs once and writes its results once.
+#include <math.h>
+
+#include "fp8.h"
+#include "wam_internal.h"
+
+namespace wam {
+
+namespace {
+
+// ------------------------------------------------------------- elements
+// Element i of a row of float32 or bf16 values (type uniform over the launch).
+__device__ __forceinline__ float load1(const void* p, int64_t i, int dtype) {
+  return dtype == WAM_BF16 ? to_f32(static_cast<const bf16*>(p)[i]) : static_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ void store1(void* p, int64_t i, int dtype, float v) {
+  if (dtype == WAM_BF16) static_cast<bf16*>(p)[i] = static_cast<bf16>(v);
+  else static_cast<float*>(p)[i] = v;
+}
+
+// ------------------------------------------------------------- rotary positions
+constexpr int kMaxPairs = WAM_MAX_HEAD / 2;
+struct RopeParams {
+  wam_rope_args a;
+  int pairs, end0, end1;     // pairs of axis 0 end at end0, of axis 1 at end1
+  double turns[kMaxPairs];   // revolutions per unit of position
+};
+
+// cos and sin of pos * freq.  The product is taken in revolutions and in
+// float64, so that dropping the whole ones is exact and far positions lose
+// nothing (a float32 angle of position 1e5 is off by 4e-3); what is left lies
+// within half a turn and float32 does for it.
+__device__ __forceinline__ void axis_turn(const RopeParams& p, const float* pos, int i, float& c, float& s) {
+  const int axis = i < p.end0 ? 0 : i < p.end1 ? 1 : 2;
+  double t = (double)pos[axis] * p.turns[i];
+  t -= rint(t);
+  sincospif((float)(2.0 * t), &s, &c);
+}
+
+// One wave per head vector, element e = lane + 64 j: any head size, layout,
+// stride and alignment.
+__global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
+  const wam_rope_args& a = p.a;
+  const int heads = a.Hq + a.Hk;
+  const int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  if (item >= (int64_t)a.B * a.T * heads) return;
+  const int lane = threadIdx.x % kWave;
+  const int hd = (int)(item % heads);
+  const int64_t row = item / heads;
+  const int t = (int)(row % a.T), b = (int)(row / a.T);
+  const bool isq = hd < a.Hq;
+  const int h = isq ? hd : hd - a.Hq;
+  const int64_t* si = isq ? a.q_stride : a.k_stride;
+  const int64_t* so = isq ? a.q_out_stride : a.k_out_stride;
+  const int64_t in = b * si[0] + t * si[1] + h * si[2], out = b * so[0] + t * so[1] + h * so[2];
+  const void* x = isq ? a.q : a.k;
+  void* o = isq ? a.q_out : a.k_out;
+  const float* gain = isq ? a.q_gain : a.k_gain;
+  const float* pos = a.pos + b * a.pos_stride + (int64_t)t * 3;
+
+  constexpr int J = WAM_MAX_HEAD / kWave;
+  float own[J], other[J];
+  float ss = 0.f;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int e = lane + kWave * j;
+    own[j] = other[j] = 0.f;
+    if (e >= a.dh) continue;
+    own[j] = load1(x, in + e, a.dtype);
+    ss += own[j] * own[j];
+    if (e < 2 * p.pairs) {
+      const int partner = a.layout == WAM_ROPE_PAIRS ? e ^ 1 : e < p.pairs ? e + p.pairs : e - p.pairs;
+      other[j] = load1(x, in + partner, a.dtype);
+      if (gain) other[j] *= gain[partner];
+    }
+    if (gain) own[j] *= gain[e];
+  }
+  const float rs = gain ? rsqrt_newton(wave_sum(ss) / (float)a.dh + a.eps) : 1.0f;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int e = lane + kWave * j;
+    if (e >= a.dh) continue;
+    float v = own[j] * rs;
+    if (e < 2 * p.pairs) {
+      const bool first = a.layout == WAM_ROPE_PAIRS ? e % 2 == 0 : e < p.pairs;
+      const int i = a.layout == WAM_ROPE_PAIRS ? e / 2 : first ? e : e - p.pairs;
+      float c, s;
+      axis_turn(p, pos, i, c, s);
+      v = v * c + other[j] * rs * (first ? -s : s);
+    }
+    store1(o, out + e, a.dtype, v);
+  }
+}
+
+// ------------------------------------------------------------- norms around a block
+// Sum over the block (256 threads), the same in every thread.
+__device__ __forceinline__ float block_sum(float v, float* sh) {
+  v = wave_sum(v);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = v;
+  __syncthreads();
+  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
+}
+
+// Mean to subtract and scale to multiply with of the row x[0 .. D) in LDS; each
+// thread has written the elements threadIdx.x + 256 i that it reads here.
+__device__ __forceinline__ void row_stats(const float* x, int D, int kind, float eps, float* sh, float& mean,
+                                          float& rs) {
+  mean = 0.f;
+  rs = 1.f;
+  if (kind == WAM_NORM_NONE) return;
+  if (kind == WAM_NORM_LAYER) {
+    float s = 0.f;
+    for (int i = threadIdx.x; i < D; i += 256) s += x[i];
+    mean = block_sum(s, sh) / (float)D;
+  }
+  float q = 0.f;
+  for (int i = threadIdx.x; i < D; i += 256) {
+    const float v = x[i] - mean;
+    q += v * v;
+  }
+  rs = rsqrt_newton(block_sum(q, sh) / (float)D + eps);
+}
+
+// One block per row, the row in LDS: any width, stride and alignment.
+__global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
+  extern __shared__ float x[];
+  __shared__ float sh[4];
+  const int t = blockIdx.x % a.T, b = blockIdx.x / a.T;
+  const int D = a.D;
+  const int64_t h0 = b * a.h_stride[0] + t * a.h_stride[1];
+  float mean, rs;
+  if (a.y) {
+    const int64_t y0 = b * a.y_stride[0] + t * a.y_stride[1];
+    for (int i = threadIdx.x; i < D; i += 256) x[i] = load1(a.y, y0 + i, a.y_dtype);
+    row_stats(x, D, a.post, a.eps, sh, mean, rs);
+  }
+  const float* gate = a.gate ? a.gate + b * a.gate_stride[0] + t * a.gate_stride[1] : nullptr;
+  for (int i = threadIdx.x; i < D; i += 256) {
+    float v = a.res_scale * load1(a.h, h0 + i, a.h_dtype);
+    if (a.y) {
+      float w = (x[i] - mean) * rs;
+      if (a.post_gain) w *= a.post_gain[i];
+      v += gate ? gate[i] * w : w;
+    }
+    x[i] = v;
+  }
+  if (a.h_out) {
+    const int64_t o0 = b * a.h_out_stride[0] + t * a.h_out_stride[1];
+    for (int i = threadIdx.x; i < D; i += 256) store1(a.h_out, o0 + i, a.h_dtype, x[i]);
+  }
+  if (!a.u) return;
+  row_stats(x, D, a.pre, a.eps, sh, mean, rs);
+  const float* scale = a.scale ? a.scale + b * a.scale_stride[0] + t * a.scale_stride[1] : nullptr;
+  const float* shift = a.shift ? a.shift + b * a.shift_stride[0] + t * a.shift_stride[1] : nullptr;
+  const int64_t u0 = b * a.u_stride[0] + t * a.u_stride[1];
+  auto value = [&](int i) {
+    float v = (x[i] - mean) * rs;
+    if (a.pre_gain) v *= a.pre_gain[i];
+    if (scale) v *= 1.0f + scale[i];
+    return shift ? v + shift[i] : v;
+  };
+  if (a.u_dtype != WAM_FP8) {
+    for (int i = threadIdx.x; i < D; i += 256) store1(a.u, u0 + i, a.u_dtype, value(i));
+    return;
+  }
+  // wave w takes the blocks w, w + 4, ..., lane l the columns l and l + 64 of each
+  __syncthreads();
+  float* us = a.u_scale + b * a.u_scale_stride[0] + t * a.u_scale_stride[1];
+  uint8_t* u = static_cast<uint8_t*>(a.u) + u0;
+  const int lane = threadIdx.x % kWave;
+  for (int blk = threadIdx.x / kWave; blk * kScaleBlock < D; blk += 4) {
+    const int i = blk * kScaleBlock + lane, j = i + kWave;
+    const float v = i < D ? value(i) : 0.f, w = j < D ? value(j) : 0.f;
+    const float s = block_scale(wave_max(max(abs_bits(v), abs_bits(w))));
+    if (i < D) u[i] = to_e4m3(v / s);
+    if (j < D) u[j] = to_e4m3(w / s);
+    if (lane == 0) us[blk] = s;
+  }
+}
+
+// ------------------------------------------------------------- quantisation
+// One block per scale, any width, stride and alignment: thread t of block_rows x
+// 128 values takes column t % 128 of every other row.
+__global__ __launch_bounds__(256) void quantize_kernel(wam_quantize_args a) {
+  __shared__ uint32_t top[4];
+  const int kb = (a.K + kScaleBlock - 1) / kScaleBlock;
+  const int bk = blockIdx.x % kb;
+  const int64_t bm = blockIdx.x / kb;
+  const int col = bk * kScaleBlock + threadIdx.x % kScaleBlock;
+  const int64_t m0 = bm * a.block_rows, m1 = min(m0 + a.block_rows, (int64_t)a.M);
+  uint32_t most = 0;
+  if (col < a.K)
+    for (int64_t m = m0 + threadIdx.x / kScaleBlock; m < m1; m += 2)
+      most = max(most, abs_bits(load1(a.x, m * a.x_stride + col, a.dtype)));
+  most = wave_max(most);
+  if (threadIdx.x % kWave == 0) top[threadIdx.x / kWave] = most;
+  __syncthreads();
+  const float s = block_scale(max(max(top[0], top[1]), max(top[2], top[3])));
+  if (threadIdx.x == 0) a.scale[bm * a.scale_stride + bk] = s;
+  if (col < a.K)
+    for (int64_t m = m0 + threadIdx.x / kScaleBlock; m < m1; m += 2)
+      static_cast<uint8_t*>(a.q)[m * a.q_stride + col] = to_e4m3(load1(a.x, m * a.x_stride + col, a.dtype) / s);
+}
+
+// ------------------------------------------------------------- argument checks
+constexpr int64_t kMaxStride = (int64_t)1 << 40;  // a larger one is no buffer of this machine
+
+// Elements of a strided result are distinct: by stride, each dimension of more
+// than one index steps over the whole of the smaller ones (the last, contiguous
+// one has `inner` elements).
+bool distinct(const int64_t* stride, const int64_t* size, int n, int64_t inner) {
+  bool used[3] = {false, false, false};
+  int64_t extent = inner;
+  for (int step = 0; step < n; ++step) {
+    int at = -1;
+    for (int i = 0; i < n; ++i)
+      if (!used[i] && size[i] > 1 && (at < 0 || stride[i] < stride[at])) at = i;
+    if (at < 0) return true;
+    if (stride[at] < extent) return false;
+    extent = stride[at] * (size[at] - 1) + extent;
+    used[at] = true;
+  }
+  return true;
+}
+// strides of at most 2^40 elements, so that no offset or extent passes 64 bits
+bool strides_ok(const int64_t* stride, int n) {
+  for (int i = 0; i < n; ++i)
+    if (stride[i] < 0 || stride[i] > kMaxStride) return false;
+  return true;
+}
+bool same(const int64_t* a, const int64_t* b, int n) {
+  for (int i = 0; i < n; ++i)
+    if (a[i] != b[i]) return false;
+  return true;
+}
+bool float_type(int t) { return t == WAM_FP32 || t == WAM_BF16; }
+int64_t type_size(int t) { return t == WAM_FP32 ? 4 : t == WAM_BF16 ? 2 : 1; }
+bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)n == 0; }
+
+// blocks of a one-dimensional grid
+constexpr int64_t kMaxGrid = 0x7fffffff;
+
+int check_heads(int H, const wam_rope_args* a, const void* x, const void* out, const int64_t* si,
+                const int64_t* so) {
+  if (H == 0) return WAM_OK;
+  if (!x || !out) return noalloc_fail(WAM_E_ARG, "wam_rope: null q, k or result");
+  if (!aligned_to(x, type_size(a->dtype)) || !aligned_to(out, type_size(a->dtype)))
+    return noalloc_fail(WAM_E_ARG, "wam_rope: buffers must be aligned to their elements");
+  if (!strides_ok(si, 3)) return noalloc_fail(WAM_E_ARG, "wam_rope: strides must be >= 0");
+  const int64_t size[3] = {a->B, a->T, H};
+  if (!strides_ok(so, 3) || !distinct(so, size, 3, a->dh))
+    return noalloc_fail(WAM_E_ARG, "wam_rope: the elements of a result must be distinct");
+  if (x == out && !same(si, so, 3))
+    return noalloc_fail(WAM_E_ARG, "wam_rope: a result in place needs the strides of its input");
+  return WAM_OK;
+}
+
+hipError_t launch_rope(const RopeParams& p, hipStream_t s) {
+  const int64_t items = (int64_t)p.a.B * p.a.T * (p.a.Hq + p.a.Hk);
+  launch_k(rope_kernel, dim3((unsigned)((items + 3) / 4)), 256, 0, s, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+}  // namespace wam
+
+using namespace wam;
+
+extern "C" {
+
+int wam_rope_frequencies(const int32_t* sections, double theta, int32_t shared, double* freq) {
+  if (!sections || !freq) return noalloc_fail(WAM_E_ARG, "wam_rope_frequencies: null argument");
+  if (!(theta > 0.0) || !(theta < INFINITY))
+    return noalloc_fail(WAM_E_ARG, "wam_rope_frequencies: theta must be positive and finite");
+  int64_t pairs = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (sections[a] < 0) return noalloc_fail(WAM_E_ARG, "wam_rope_frequencies: sections must be >= 0");
+    pairs += sections[a];
+  }
+  if (pairs > kMaxPairs) return noalloc_fail(WAM_E_SHAPE, "wam_rope_frequencies: at most WAM_MAX_HEAD / 2 pairs");
+  int i = 0;
+  for (int a = 0; a < 3; ++a)
+    for (int j = 0; j < sections[a]; ++j, ++i)
+      freq[i] = shared ? pow(theta, -(double)i / (double)pairs) : pow(theta, -(double)j / (double)sections[a]);
+  return WAM_OK;
+}
+
+int wam_rope(const wam_rope_args* a, void* hip_stream) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_rope: null argument");
+  if (a->B < 0 || a->T < 0 || a->Hq < 0 || a->Hk < 0) return noalloc_fail(WAM_E_ARG, "wam_rope: sizes must be >= 0");
+  if (a->dh < 1 || a->dh > WAM_MAX_HEAD) return noalloc_fail(WAM_E_SHAPE, "wam_rope: head size must be 1..WAM_MAX_HEAD");
+  if (!float_type(a->dtype)) return noalloc_fail(WAM_E_ARG, "wam_rope: dtype must be WAM_FP32 or WAM_BF16");
+  if (a->layout != WAM_ROPE_HALVES && a->layout != WAM_ROPE_PAIRS)
+    return noalloc_fail(WAM_E_ARG, "wam_rope: unknown layout");
+  int64_t pairs = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (a->sections[i] < 0) return noalloc_fail(WAM_E_ARG, "wam_rope: sections must be >= 0");
+    pairs += a->sections[i];
+  }
+  if (2 * pairs > a->dh) return noalloc_fail(WAM_E_SHAPE, "wam_rope: the sections' pairs must fit the head (2 P <= dh)");
+  if (pairs > 0 && !a->freq) return noalloc_fail(WAM_E_ARG, "wam_rope: null freq");
+  if ((a->q_gain || a->k_gain) && !(a->eps >= 0.f)) return noalloc_fail(WAM_E_ARG, "wam_rope: eps must be >= 0");
+  if ((int64_t)a->Hq + a->Hk > INT32_MAX) return noalloc_fail(WAM_E_SHAPE, "wam_rope: too many heads");
+  if (a->B == 0 || a->T == 0 || a->Hq + a->Hk == 0) return WAM_OK;
+  if (!a->pos || !aligned_to(a->pos, 4)) return noalloc_fail(WAM_E_ARG, "wam_rope: null or unaligned pos");
+  if (!strides_ok(&a->pos_stride, 1)) return noalloc_fail(WAM_E_ARG, "wam_rope: strides must be >= 0");
+  int st = check_heads(a->Hq, a, a->q, a->q_out, a->q_stride, a->q_out_stride);
+  if (!st) st = check_heads(a->Hk, a, a->k, a->k_out, a->k_stride, a->k_out_stride);
+  if (st) return st;
+  if ((double)a->B * a->T * ((double)a->Hq + a->Hk) / 4 >= (double)kMaxGrid)
+    return noalloc_fail(WAM_E_SHAPE, "wam_rope: too many head vectors for one launch");
+  RopeParams p{};
+  p.a = *a;
+  p.pairs = (int)pairs;
+  p.end0 = a->sections[0];
+  p.end1 = p.end0 + a->sections[1];
+  for (int i = 0; i < p.pairs; ++i) p.turns[i] = a->freq[i] * (0.5 / M_PI);
+  if (launch_rope(p, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+    return noalloc_fail(WAM_E_HIP, "wam_rope: kernel launch failed");
+  return WAM_OK;
+}
+
+int wam_norm_residual(const wam_norm_args* a, void* hip_stream) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: null argument");
+  if (a->B < 0 || a->T < 0) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: sizes must be >= 0");
+  if (a->D < 1 || a->D > WAM_MAX_NORM_D)
+    return noalloc_fail(WAM_E_SHAPE, "wam_norm_residual: D must be 1..WAM_MAX_NORM_D");
+  if (!float_type(a->h_dtype)) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: h must be WAM_FP32 or WAM_BF16");
+  if (!(a->eps >= 0.f)) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: eps must be >= 0");
+  auto kind = [](int k) { return k == WAM_NORM_NONE || k == WAM_NORM_RMS || k == WAM_NORM_LAYER; };
+  if (!kind(a->post) || !kind(a->pre)) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: unknown norm");
+  if ((int64_t)a->B * a->T > kMaxGrid) return noalloc_fail(WAM_E_SHAPE, "wam_norm_residual: too many rows");
+  if (a->B == 0 || a->T == 0) return WAM_OK;
+  const int64_t size[2] = {a->B, a->T};
+  if (!a->h) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: null h");
+  if (!a->h_out && !a->u) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: no result asked for");
+  auto in_ok = [&](const void* p, int64_t n, const int64_t* st) { return !p || (aligned_to(p, n) && strides_ok(st, 2)); };
+  auto out_ok = [&](const void* p, int64_t n, const int64_t* st, int64_t inner) {
+    return !p || (aligned_to(p, n) && strides_ok(st, 2) && distinct(st, size, 2, inner));
+  };
+  if (a->y && !float_type(a->y_dtype)) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: y must be WAM_FP32 or WAM_BF16");
+  if (a->u && !float_type(a->u_dtype) && a->u_dtype != WAM_FP8)
+    return noalloc_fail(WAM_E_ARG, "wam_norm_residual: u must be WAM_FP32, WAM_BF16 or WAM_FP8");
+  if (!in_ok(a->h, type_size(a->h_dtype), a->h_stride) || !in_ok(a->y, type_size(a->y_dtype), a->y_stride) ||
+      !in_ok(a->gate, 4, a->gate_stride) || !in_ok(a->scale, 4, a->scale_stride) ||
+      !in_ok(a->shift, 4, a->shift_stride) || !aligned_to(a->post_gain, 4) || !aligned_to(a->pre_gain, 4))
+    return noalloc_fail(WAM_E_ARG, "wam_norm_residual: strides must be >= 0 and buffers aligned to their elements");
+  if (!out_ok(a->h_out, type_size(a->h_dtype), a->h_out_stride, a->D) ||
+      !out_ok(a->u, type_size(a->u_dtype), a->u_stride, a->D))
+    return noalloc_fail(WAM_E_ARG, "wam_norm_residual: the elements of a result must be distinct and aligned");
+  if (a->u && a->u_dtype == WAM_FP8 &&
+      (!a->u_scale || !out_ok(a->u_scale, 4, a->u_scale_stride, (a->D + kScaleBlock - 1) / kScaleBlock)))
+    return noalloc_fail(WAM_E_ARG, "wam_norm_residual: u of WAM_FP8 needs u_scale with distinct elements");
+  if (a->h_out == a->h && !same(a->h_out_stride, a->h_stride, 2))
+    return noalloc_fail(WAM_E_ARG, "wam_norm_residual: h_out in place needs the strides of h");
+  if (a->u && (a->u == a->h || a->u == a->h_out))
+    return noalloc_fail(WAM_E_ARG, "wam_norm_residual: u must not be h or h_out");
+  if (a->y && (a->h_out == a->y || (a->u == a->y && (a->u_dtype != a->y_dtype || !same(a->u_stride, a->y_stride, 2)))))
+    return noalloc_fail(WAM_E_ARG, "wam_norm_residual: h_out must not be y, and u only with its type and strides");
+  launch_k(norm_residual_kernel, dim3((unsigned)((int64_t)a->B * a->T)), 256, (size_t)a->D * 4,
+           static_cast<hipStream_t>(hip_stream), *a);
+  if (hipGetLastError() != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_norm_residual: kernel launch failed");
+  return WAM_OK;
+}
+
+int wam_quantize_fp8(const wam_quantize_args* a, void* hip_stream) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: null argument");
+  if (a->M < 0 || a->K < 0) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: sizes must be >= 0");
+  if (!float_type(a->dtype)) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: x must be WAM_FP32 or WAM_BF16");
+  if (a->block_rows != 1 && a->block_rows != kScaleBlock)
+    return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: block_rows must be 1 or 128");
+  if (a->M == 0 || a->K == 0) return WAM_OK;
+  if (!a->x || !a->q || !a->scale) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: null buffer");
+  if (!aligned_to(a->x, type_size(a->dtype)) || !aligned_to(a->scale, 4))
+    return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: buffers must be aligned to their elements");
+  if (a->x == a->q) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: q must not be x");
+  const int64_t kb = ((int64_t)a->K + kScaleBlock - 1) / kScaleBlock;
+  const int64_t mb = ((int64_t)a->M + a->block_rows - 1) / a->block_rows;
+  if (!strides_ok(&a->x_stride, 1) || (a->M > 1 && a->q_stride < a->K) || (mb > 1 && a->scale_stride < kb))
+    return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: x_stride must be >= 0, and rows of the results distinct");
+  if (mb * kb > kMaxGrid) return noalloc_fail(WAM_E_SHAPE, "wam_quantize_fp8: too many blocks for one launch");
+  launch_k(quantize_kernel, dim3((unsigned)(mb * kb)), 256, 0, static_cast<hipStream_t>(hip_stream), *a);
+  if (hipGetLastError() != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_quantize_fp8: kernel launch failed");
+  return WAM_OK;
+}
+
+}  // extern "C"

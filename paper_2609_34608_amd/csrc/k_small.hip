@@ -3,8 +3,8 @@
 #include <math.h>
 
 #include <algorithm>
+#include <cstdio>
 #include <mutex>
-#include <string>
 
 #include "wam_internal.h"
 
@@ -998,12 +998,18 @@ __device__ __align__(256) double scratch[kNoAllocScratchDoubles];
 std::mutex g_scratch_mu;
 double* g_scratch_ptr[kMaxDevices] = {};
 
-thread_local std::string t_noalloc_err;
+// this thread's message of the last failing call without a handle; a plain
+// array, so that storing one cannot throw across the C boundary
+thread_local char t_noalloc_err[256];
+
+}  // namespace
 
 int noalloc_fail(int code, const char* msg) {
-  t_noalloc_err = msg;
+  snprintf(t_noalloc_err, sizeof(t_noalloc_err), "%s", msg);
   return code;
 }
+
+namespace {
 
 // Device address of this GPU's copy of `scratch` (looked up on first use).
 int scratch_for_current_device(double** out) {
@@ -1026,7 +1032,7 @@ int scratch_for_current_device(double** out) {
 
 extern "C" {
 
-const char* wam_noalloc_last_error(void) { return wam::t_noalloc_err.c_str(); }
+const char* wam_noalloc_last_error(void) { return wam::t_noalloc_err; }
 
 int wam_remap_noalloc(const wam_config* cfg, const wam_remap_args* a, void* hip_stream) {
   using namespace wam;

@@ -121,6 +121,9 @@ __device__ __forceinline__ float gelu_tanh_f(float x) {
   return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z));
 }
 
+// Message and status of a failing call without a handle (wam_noalloc_last_error).
+int noalloc_fail(int code, const char* msg);
+
 // ---------------------------------------------------------------- GEMM
 enum GemmEpilogue : int {
   EPI_BIAS_GELU = 1,  // out[m,n] = gelu(acc + bias[n])                 (act type)

@@ -349,6 +349,227 @@ def remap_noalloc(cfg: abi.WamConfig, x_bar, x_r, sigma_r, sigma_b0, shift_actio
     return x_out
 
 
+# ---------------------------------------------------------------- layer operators
+FP8 = torch.float8_e4m3fn
+_TYPES = {torch.float32: abi.WAM_FP32, torch.bfloat16: abi.WAM_BF16, FP8: abi.WAM_FP8}
+_LAYOUTS = {"halves": abi.WAM_ROPE_HALVES, "pairs": abi.WAM_ROPE_PAIRS}
+_NORMS = {"none": abi.WAM_NORM_NONE, "rms": abi.WAM_NORM_RMS, "layer": abi.WAM_NORM_LAYER}
+
+
+def _operand(t, what, dtypes, dev, shape=None):
+    """Checks an operator's tensor: on dev, of one of dtypes, of the given shape,
+    its last dimension contiguous."""
+    if not isinstance(t, torch.Tensor) or t.device != dev or not t.is_cuda:
+        raise WamError(f"{what}: needs a tensor on {dev}")
+    if t.dtype not in dtypes:
+        raise WamError(f"{what}: dtype {t.dtype} is not supported")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise WamError(f"{what}: shape {tuple(t.shape)} is not {tuple(shape)}")
+    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise WamError(f"{what}: the last dimension must be contiguous")
+    return t
+
+
+def _choice(table, key, what):
+    try:
+        return table[key]
+    except (KeyError, TypeError):
+        raise WamError(f"{what}: unknown value {key!r}") from None
+
+
+def _call(fn, args, dev, stream, what):
+    """Enqueues a handle-free operator on dev (stream: default torch's current one)."""
+    if stream is None:
+        stream = torch.cuda.current_stream(dev)
+    if dev.index == torch.cuda.current_device():
+        rc = fn(C.byref(args), C.c_void_p(stream.cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(C.byref(args), C.c_void_p(stream.cuda_stream))
+    if rc != abi.WAM_OK:
+        raise WamError(f"{what}: {abi.lib().wam_status_string(rc).decode()}: "
+                       f"{abi.lib().wam_noalloc_last_error().decode()}")
+
+
+def rope_frequencies(sections, theta=10000.0, shared=False) -> np.ndarray:
+    """Frequencies of the usual ladder for rope (wam_rope_frequencies): float64
+    [sum(sections)], theta^(-j / n) along each axis of n pairs, or one ladder
+    over all pairs."""
+    sec = (C.c_int32 * 3)(*sections)
+    freq = np.empty(max(sum(sec), 0), np.float64)
+    lib = abi.lib()
+    rc = lib.wam_rope_frequencies(sec, theta, int(bool(shared)), freq.ctypes.data_as(C.POINTER(C.c_double)))
+    if rc != abi.WAM_OK:
+        raise WamError(f"wam_rope_frequencies: {lib.wam_noalloc_last_error().decode()}")
+    return freq
+
+
+def rope(q, k, pos, sections, freq, *, layout="halves", q_gain=None, k_gain=None, eps=1e-6, q_out=None, k_out=None,
+         stream: torch.cuda.Stream | None = None):
+    """Rotary positions over up to three axes (wam_rope): q [B, T, Hq, dh] and k
+    [B, T, Hk, dh] (or None), float32 or bfloat16, any strides with dh contiguous;
+    pos float32 [T, 3] or [B, T, 3]; freq on the host, one value per pair.  With
+    gains, float32 [dh], the per-head RMS norm comes first.  q_out / k_out: the
+    results' buffers (q / k: in place; default: new ones).  Returns (q_out, k_out)."""
+    dev = q.device
+    _operand(q, "rope: q", (torch.float32, torch.bfloat16), dev)
+    if q.dim() != 4:
+        raise WamError("rope: q must be [B, T, H, dh]")
+    B, T, Hq, dh = q.shape
+    Hk = 0
+    if k is not None:
+        _operand(k, "rope: k", (q.dtype,), dev)
+        if k.dim() != 4:
+            raise WamError("rope: k must be [B, T, H, dh]")
+        Hk = k.shape[2]
+        _operand(k, "rope: k", (q.dtype,), dev, (B, T, Hk, dh))
+    _operand(pos, "rope: pos", (torch.float32,), dev, (T, 3) if pos.dim() == 2 else (B, T, 3))
+    if B > 0 and T > 1 and pos.stride(-2) != 3:
+        raise WamError("rope: rows of pos must be contiguous")
+    ladder = np.ascontiguousarray(freq, np.float64)
+    if len(sections) != 3 or ladder.shape != (sum(sections),):
+        raise WamError("rope: needs three sections and one frequency per pair")
+    for g, what in ((q_gain, "rope: q_gain"), (k_gain, "rope: k_gain")):
+        if g is not None:
+            _operand(g, what, (torch.float32,), dev, (dh,))
+    q_out = torch.empty_like(q) if q_out is None else _operand(q_out, "rope: q_out", (q.dtype,), dev, q.shape)
+    if k is not None:
+        k_out = torch.empty_like(k) if k_out is None else _operand(k_out, "rope: k_out", (q.dtype,), dev, k.shape)
+    strides = lambda t: (C.c_int64 * 3)(*t.stride()[:3]) if t is not None else (C.c_int64 * 3)()  # noqa: E731
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    a = abi.WamRopeArgs(B, T, Hq, Hk, dh, _TYPES[q.dtype], _choice(_LAYOUTS, layout, "rope: layout"),
+                        (C.c_int32 * 3)(*sections), ptr(q), ptr(k), ptr(q_out), ptr(k_out) if k is not None else None,
+                        strides(q), strides(k), strides(q_out), strides(k_out if k is not None else None), ptr(pos),
+                        pos.stride(0) if pos.dim() == 3 else 0, ladder.ctypes.data, ptr(q_gain), ptr(k_gain), eps)
+    _call(abi.lib().wam_rope, a, dev, stream, "wam_rope")
+    return q_out, k_out if k is not None else None
+
+
+def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale=1.0, pre="layer", pre_gain=None,
+                  scale=None, shift=None, eps=1e-6, h_out=None, u_dtype=None, u=None, u_scale=None,
+                  stream: torch.cuda.Stream | None = None):
+    """The norms around a block (wam_norm_residual), h and y [B, T, D] in float32 or
+    bfloat16: h_out = res_scale h + gate post(y), u = pre(h_out) (1 + scale) + shift.
+    post, pre: "none", "rms" or "layer"; pre None leaves u out.  gate, scale, shift:
+    float32, anything that broadcasts to [B, T, D] with D contiguous; gains float32
+    [D].  h_out: its buffer (h: in place; default: a new one).  u_dtype: float32,
+    bfloat16 or float8_e4m3fn (default: that of u, else bfloat16).  Returns
+    (h_out,), (h_out, u) or, for 8-bit blocks, (h_out, u, u_scale)."""
+    real = (torch.float32, torch.bfloat16)
+    dev = h.device
+    _operand(h, "norm_residual: h", real, dev)
+    if h.dim() != 3:
+        raise WamError("norm_residual: h must be [B, T, D]")
+    B, T, D = h.shape
+    if y is not None:
+        _operand(y, "norm_residual: y", real, dev, h.shape)
+    for g, what in ((post_gain, "norm_residual: post_gain"), (pre_gain, "norm_residual: pre_gain")):
+        if g is not None:
+            _operand(g, what, (torch.float32,), dev, (D,))
+    vectors = []
+    for v, what in ((gate, "norm_residual: gate"), (scale, "norm_residual: scale"), (shift, "norm_residual: shift")):
+        if v is not None:
+            _operand(v, what, (torch.float32,), dev)
+            try:
+                v = v.expand(B, T, D)
+            except RuntimeError:
+                raise WamError(f"{what}: shape {tuple(v.shape)} does not broadcast to {(B, T, D)}") from None
+            if D > 1 and v.stride(-1) != 1:
+                raise WamError(f"{what}: needs D values per row")
+        vectors.append(v)
+    h_out = torch.empty_like(h) if h_out is None else _operand(h_out, "norm_residual: h_out", (h.dtype,), dev, h.shape)
+    post = _choice(_NORMS, post, "norm_residual: post")
+    out = [h_out]
+    if pre is not None:
+        pre = _choice(_NORMS, pre, "norm_residual: pre")
+        if u is None:
+            u_dtype = torch.bfloat16 if u_dtype is None else u_dtype
+            u = _new_rows((B, T, D), _choice({t: t for t in _TYPES}, u_dtype, "norm_residual: u_dtype"), dev)
+        else:
+            _operand(u, "norm_residual: u", tuple(_TYPES) if u_dtype is None else (u_dtype,), dev, h.shape)
+        out.append(u)
+        if u.dtype == FP8:
+            shape = (B, T, -(-D // 128))
+            u_scale = (torch.empty(shape, dtype=torch.float32, device=dev) if u_scale is None else
+                       _operand(u_scale, "norm_residual: u_scale", (torch.float32,), dev, shape))
+            out.append(u_scale)
+        else:
+            u_scale = None
+    else:
+        u = u_scale = None
+    strides = lambda t: (C.c_int64 * 2)(*t.stride()[:2]) if t is not None else (C.c_int64 * 2)()  # noqa: E731
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    a = abi.WamNormArgs(B, T, D, _TYPES[h.dtype], _TYPES[y.dtype] if y is not None else 0,
+                        _TYPES[u.dtype] if u is not None else 0, post, pre or 0, ptr(h), ptr(y), ptr(h_out), ptr(u),
+                        ptr(u_scale), strides(h), strides(y), strides(h_out), strides(u), strides(u_scale),
+                        *(ptr(v) for v in vectors), *(strides(v) for v in vectors), ptr(post_gain), ptr(pre_gain),
+                        res_scale, eps)
+    _call(abi.lib().wam_norm_residual, a, dev, stream, "wam_norm_residual")
+    return tuple(out)
+
+
+def _new_rows(shape, dtype, dev):
+    """A new tensor; e4m3 rows start a multiple of 16 bytes apart, as matmul_fp8
+    takes them."""
+    if dtype != FP8 or shape[-1] % 16 == 0:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    padded = (*shape[:-1], -(-shape[-1] // 16) * 16)
+    return torch.empty(padded, dtype=dtype, device=dev)[..., :shape[-1]]
+
+
+def quantize_fp8(x, *, block_rows=1, q=None, scale=None, stream: torch.cuda.Stream | None = None):
+    """8-bit blocks (wam_quantize_fp8) of x [M, K], float32 or bfloat16: block_rows 1
+    for activations (1 x 128), 128 for weights (128 x 128).  Returns (q, scale):
+    float8_e4m3fn [M, K] with rows a multiple of 16 bytes apart and float32
+    [ceil(M / block_rows), ceil(K / 128)]; x stands for q * scale."""
+    dev = x.device
+    _operand(x, "quantize_fp8: x", (torch.float32, torch.bfloat16), dev)
+    if x.dim() != 2:
+        raise WamError("quantize_fp8: x must be [M, K]")
+    if block_rows not in (1, 128):
+        raise WamError("quantize_fp8: block_rows must be 1 or 128")
+    M, K = x.shape
+    q = _new_rows((M, K), FP8, dev) if q is None else _operand(q, "quantize_fp8: q", (FP8,), dev, x.shape)
+    shape = (-(-M // block_rows), -(-K // 128))
+    scale = (torch.empty(shape, dtype=torch.float32, device=dev) if scale is None else
+             _operand(scale, "quantize_fp8: scale", (torch.float32,), dev, shape))
+    a = abi.WamQuantizeArgs(M, K, _TYPES[x.dtype], block_rows, x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0),
+                            scale.data_ptr(), scale.stride(0))
+    _call(abi.lib().wam_quantize_fp8, a, dev, stream, "wam_quantize_fp8")
+    return q, scale
+
+
+def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_dtype=None,
+               stream: torch.cuda.Stream | None = None):
+    """out [M, N] = act((a * a_scale) (w * w_scale)^T + bias) of 8-bit blocks
+    (wam_matmul_fp8): a [M, K] with scales per row and 128 columns, w [N, K] with
+    scales per 128 x 128, both as quantize_fp8 gives them; bias float32 [N]; gelu:
+    the tanh form.  out float32 or bfloat16 (default: a new bfloat16 one)."""
+    dev = a.device
+    _operand(a, "matmul_fp8: a", (FP8,), dev)
+    _operand(w, "matmul_fp8: w", (FP8,), dev)
+    if a.dim() != 2 or w.dim() != 2 or a.shape[1] != w.shape[1]:
+        raise WamError("matmul_fp8: needs a [M, K] and w [N, K]")
+    (M, K), N = a.shape, w.shape[0]
+    _operand(a_scale, "matmul_fp8: a_scale", (torch.float32,), dev, (M, -(-K // 128)))
+    _operand(w_scale, "matmul_fp8: w_scale", (torch.float32,), dev, (-(-N // 128), -(-K // 128)))
+    if bias is not None:
+        _operand(bias, "matmul_fp8: bias", (torch.float32,), dev, (N,))
+    if out is None:
+        out = torch.empty((M, N), dtype=_choice({t: t for t in (torch.float32, torch.bfloat16)},
+                                                torch.bfloat16 if out_dtype is None else out_dtype,
+                                                "matmul_fp8: out_dtype"), device=dev)
+    else:
+        _operand(out, "matmul_fp8: out",
+                 (torch.float32, torch.bfloat16) if out_dtype is None else (out_dtype,), dev, (M, N))
+    args = abi.WamMatmulArgs(M, N, K, _TYPES[out.dtype], abi.WAM_ACT_GELU if gelu else abi.WAM_ACT_NONE, a.data_ptr(),
+                             a.stride(0), a_scale.data_ptr(), a_scale.stride(0), w.data_ptr(), w.stride(0),
+                             w_scale.data_ptr(), w_scale.stride(0), bias.data_ptr() if bias is not None else None,
+                             out.data_ptr(), out.stride(0))
+    _call(abi.lib().wam_matmul_fp8, args, dev, stream, "wam_matmul_fp8")
+    return out
+
+
 def probe_mfma_bf16(shape: int = 0, n_blocks: int = 1024, iters: int = 20000, device="cuda:0"):
     """Achievable bf16 MFMA rate (wam_probe_mfma_bf16): returns (TFLOP/s, ms)."""
     lib = abi.lib()

@@ -1,0 +1,502 @@
+"""The layer operators on the GPU against their plain float64 forms
+(layer_ops_ref), at the sizes, strides, types and values where they can go wrong;
+tolerances are the bounds derived there plus half a step of the result's type."""
+import numpy as np
+import pytest
+import torch
+
+import layer_ops_ref as F
+from gpu_common import device
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32, FP8 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return device()
+
+
+@pytest.fixture(scope="module")
+def R():
+    from paper_2609_34608_amd import runtime
+    return runtime
+
+
+def _rand(dev, seed, *shape, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (std * torch.randn(*shape, generator=g)).to(dev)
+
+
+def _strided(x, order, pad=0, offset=0):
+    """x with its leading dimensions laid out in `order` (outermost first), rows
+    `pad` elements further apart, its storage starting `offset` elements in."""
+    shape = [x.shape[i] for i in order] + [x.shape[-1] + pad]
+    n = int(np.prod(shape))
+    buf = torch.full((n + offset,), float("nan"), device=x.device).to(x.dtype)[offset:].view(shape)
+    view = buf[..., :x.shape[-1]].permute(*[list(order).index(i) for i in range(len(order))], len(order))
+    view.copy_(x)
+    return view
+
+
+# ------------------------------------------------------------- rotary positions
+ROPE = [
+    # B, T, Hq, Hk, dh, sections
+    (1, 1, 1, 1, 64, (8, 12, 12)),
+    (2, 33, 3, 2, 64, (8, 12, 12)),
+    (1, 7, 5, 5, 32, (4, 6, 6)),
+    (1, 130, 24, 24, 128, (16, 24, 24)),
+    (3, 5, 2, 1, 256, (32, 48, 48)),
+    (1, 9, 3, 3, 96, (16, 16, 16)),
+    (2, 6, 2, 2, 72, (12, 12, 12)),
+    (1, 5, 2, 2, 64, (16, 0, 0)),
+    (1, 4, 1, 2, 64, (5, 6, 7)),
+    (1, 3, 2, 2, 2, (1, 0, 0)),
+    (1, 6, 2, 3, 17, (3, 2, 3)),
+    (1, 4, 2, 2, 64, (0, 0, 0)),
+    (4, 1, 19, 19, 64, (0, 16, 16)),
+]
+
+
+def _positions(dev, T, B=None, far=0.0):
+    i = torch.arange(T, dtype=torch.float64)
+    p = torch.stack([0.75 * (i // 6) + far, (i // 3) % 2, i % 3 - 1], -1)
+    if B is not None:
+        p = torch.stack([p + 0.5 * b for b in range(B)])
+    return p.to(F32).to(dev)
+
+
+def _check_rope(R, q, k, pos, sec, layout, gains=(None, None), **kw):
+    freq = R.rope_frequencies(sec)
+    qo, ko = R.rope(q, k, pos, sec, freq, layout=layout, q_gain=gains[0], k_gain=gains[1], **kw)
+    for x, o, g in ((q, qo, gains[0]), (k, ko, gains[1])):
+        if x is not None:
+            F.check(o, *F.rope(x, pos, sec, freq, layout, g), dtype=x.dtype)
+    return qo, ko
+
+
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("norm", [False, True])
+@pytest.mark.parametrize("size", ROPE)
+def test_rope(dev, R, size, norm, dtype, layout):
+    B, T, Hq, Hk, dh, sec = size
+    q, k = _rand(dev, 1, B, T, Hq, dh).to(dtype), _rand(dev, 2, B, T, Hk, dh).to(dtype)
+    gains = (1 + 0.2 * _rand(dev, 3, dh), 1 + 0.2 * _rand(dev, 4, dh)) if norm else (None, None)
+    _check_rope(R, q, k, _positions(dev, T), sec, layout, gains)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("order,pad,offset", [((0, 2, 1), 0, 0), ((2, 1, 0), 8, 0), ((1, 0, 2), 0, 8), ((0, 1, 2), 3, 0),
+                                              ((0, 2, 1), 0, 1)])
+def test_rope_strides(dev, R, order, pad, offset, dtype):
+    """Heads before rows, samples last, padded rows, bases and rows off 16 bytes;
+    the elements between the rows stay as they are."""
+    q = _strided(_rand(dev, 1, 2, 21, 3, 64).to(dtype), order, pad, offset)
+    k = _strided(_rand(dev, 2, 2, 21, 3, 64).to(dtype), order, pad, offset)
+    gains = (1 + 0.2 * _rand(dev, 3, 64), None)
+    pos = _positions(dev, 21, 2)
+    out = [_strided(torch.zeros_like(t), order, pad, offset) for t in (q, k)]
+    _check_rope(R, q, k, pos, (8, 12, 12), "halves", gains, q_out=out[0], k_out=out[1])
+    _check_rope(R, q, k, pos, (8, 12, 12), "pairs", gains)
+    if pad:
+        for o in out:
+            whole = o.as_strided((o.numel() // 64 * (64 + pad),), (1,), o.storage_offset())
+            assert whole.view(-1, 64 + pad)[:, 64:].isnan().all()
+
+
+def test_rope_in_place_broadcast_and_alone(dev, R):
+    sec, freq = (8, 12, 12), R.rope_frequencies((8, 12, 12))
+    q, k = _rand(dev, 1, 2, 40, 4, 64).to(BF16), _rand(dev, 2, 2, 40, 2, 64).to(BF16)
+    pos = _positions(dev, 40)
+    want = R.rope(q, k, pos, sec, freq)
+    q2, k2 = q.clone(), k.clone()
+    got = R.rope(q2, k2, pos, sec, freq, q_out=q2, k_out=k2)
+    assert got[0] is q2 and torch.equal(q2, want[0]) and torch.equal(k2, want[1])
+    # q alone; one k head shared by several (stride 0)
+    alone = R.rope(q, None, pos, sec, freq)
+    assert alone[1] is None and torch.equal(alone[0], want[0])
+    shared = k[:, :, :1].expand(2, 40, 4, 64)
+    out = R.rope(q, shared, pos, sec, freq)[1]
+    assert out.shape == shared.shape
+    for h in range(4):
+        assert torch.equal(out[:, :, h], want[1][:, :, 0])
+
+
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+def test_rope_far_positions(dev, R, layout):
+    """Positions up to 1e6, fractions and negative ones: the angle is formed in 64 bits."""
+    q = _rand(dev, 1, 1, 64, 2, 64)
+    pos = torch.zeros(64, 3)
+    pos[:, 0] = torch.linspace(-1e6, 1e6, 64)
+    pos[:, 1] = 123456.78
+    pos[:, 2] = torch.arange(64) * 0.37
+    _check_rope(R, q, q, pos.to(dev), (8, 12, 12), layout)
+
+
+def test_rope_zero_rows_and_non_finite_values(dev, R):
+    """A zero head vector stays zero under the norm; NaN and infinity stay in their
+    head vector (norm) or pair (no norm)."""
+    sec, freq = (8, 12, 12), R.rope_frequencies((8, 12, 12))
+    q = _rand(dev, 1, 1, 8, 2, 64).to(BF16)
+    q[0, 1, 0] = 0
+    q[0, 2, 1, 5] = float("nan")
+    q[0, 3, 0, 7] = float("inf")
+    pos, g = _positions(dev, 8), torch.ones(64, device=dev)
+    o = R.rope(q, None, pos, sec, freq, q_gain=g)[0]
+    assert (o[0, 1, 0] == 0).all() and o[0, 2, 1].isnan().all()
+    keep = torch.ones(8, 2, dtype=torch.bool)
+    keep[2, 1] = keep[3, 0] = False
+    assert o[0][keep.to(dev)].isfinite().all()
+    o = R.rope(q, None, pos, sec, freq)[0]
+    bad = ~o.isfinite()
+    assert set(map(tuple, bad.nonzero().tolist())) <= {(0, 2, 1, 5), (0, 2, 1, 37), (0, 3, 0, 7), (0, 3, 0, 39)}
+    assert bad[0, 2, 1, 5] and bad[0, 2, 1, 37] and bad[0, 3, 0, 7]
+
+
+def test_rope_offsets_past_32_bits(dev, R):
+    """Rows more than 2^31 elements apart."""
+    step = (1 << 31) + 64
+    buf = torch.zeros(2 * step, dtype=BF16, device=dev)
+    q = buf.as_strided((1, 2, 2, 64), (0, step, 64, 1))
+    q.copy_(_rand(dev, 1, 1, 2, 2, 64).to(BF16))
+    _check_rope(R, q.clone(), None, _positions(dev, 2), (8, 12, 12), "halves")
+    freq = R.rope_frequencies((8, 12, 12))
+    want = R.rope(q.contiguous(), None, _positions(dev, 2), (8, 12, 12), freq)[0]
+    R.rope(q, None, _positions(dev, 2), (8, 12, 12), freq, q_out=q)
+    assert torch.equal(q, want)
+
+
+# ------------------------------------------------------------- norms around a block
+def _check_norm(R, h, y, u_dtype, **kw):
+    got = R.norm_residual(h, y, u_dtype=u_dtype, **kw)
+    plain = {n: v for n, v in kw.items() if n not in ("h_out", "u", "u_scale")}
+    (ho, eh), (u, eu) = F.norm_residual(h, y, **plain)
+    F.check(got[0], ho, eh, h.dtype)
+    if kw.get("pre", "layer") is None:
+        assert len(got) == 1
+    elif u_dtype == FP8:
+        D = h.shape[-1]
+        F.check_blocks(got[1].reshape(-1, D), got[2].reshape(-1, got[2].shape[-1]), u.reshape(-1, D), eu.reshape(-1, D))
+    else:
+        F.check(got[1], u, eu, u_dtype)
+    return got
+
+
+@pytest.mark.parametrize("u_dtype", [F32, BF16, FP8])
+@pytest.mark.parametrize("h_dtype,y_dtype", [(F32, BF16), (F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("D", [64, 256, 512, 1216, 2048])
+def test_norm_types(dev, R, D, h_dtype, y_dtype, u_dtype):
+    B, T = 2, 5
+    h, y = _rand(dev, 1, B, T, D, std=3).to(h_dtype), _rand(dev, 2, B, T, D, std=0.5).to(y_dtype)
+    v = dict(gate=0.3 * _rand(dev, 3, B, 1, D), scale=0.3 * _rand(dev, 4, B, 1, D), shift=0.3 * _rand(dev, 5, B, 1, D))
+    _check_norm(R, h, y, u_dtype, post_gain=1 + 0.1 * _rand(dev, 6, D), pre_gain=1 + 0.1 * _rand(dev, 7, D),
+                res_scale=0.7071067811865476, **v)
+
+
+@pytest.mark.parametrize("D", [1, 2, 7, 100, 127, 129, 333, 1000, 2047, 2049, 3000, 5120, 8191, 8192])
+@pytest.mark.parametrize("u_dtype", [F32, BF16, FP8])
+def test_norm_widths(dev, R, D, u_dtype):
+    h, y = _rand(dev, 1, 1, 3, D), _rand(dev, 2, 1, 3, D).to(BF16)
+    _check_norm(R, h, y, u_dtype, gate=_rand(dev, 3, D), shift=_rand(dev, 4, 1, 3, D))
+
+
+@pytest.mark.parametrize("post", ["none", "rms", "layer"])
+@pytest.mark.parametrize("pre", [None, "none", "rms", "layer"])
+@pytest.mark.parametrize("D", [192, 1024])
+def test_norm_kinds(dev, R, D, pre, post):
+    h, y = _rand(dev, 1, 2, 9, D), _rand(dev, 2, 2, 9, D).to(BF16)
+    _check_norm(R, h, y, F32, post=post, pre=pre, gate=_rand(dev, 3, 2, 9, D), res_scale=-0.5)
+    if pre is not None:
+        _check_norm(R, h, None, BF16, post=post, pre=pre, scale=_rand(dev, 4, D))
+
+
+@pytest.mark.parametrize("order,pad,offset", [((1, 0), 0, 0), ((0, 1), 8, 0), ((0, 1), 4, 4), ((1, 0), 1, 0),
+                                              ((0, 1), 0, 1)])
+@pytest.mark.parametrize("u_dtype", [F32, BF16, FP8])
+def test_norm_strides(dev, R, order, pad, offset, u_dtype):
+    h = _strided(_rand(dev, 1, 3, 4, 512), order, pad, offset)
+    y = _strided(_rand(dev, 2, 3, 4, 512).to(BF16), order, pad, offset)
+    ho = _strided(torch.zeros(3, 4, 512, device=dev), order, pad, offset)
+    u = _strided(torch.zeros(3, 4, 512, device=dev).to(BF16), order, pad, offset) if u_dtype == BF16 else None
+    scale = _strided(_rand(dev, 3, 3, 4, 512), order, pad, offset)
+    _check_norm(R, h, y, u_dtype, scale=scale, h_out=ho, u=u, gate=_rand(dev, 4, 3, 1, 512))
+    if pad:
+        for t in (ho,) if u is None else (ho, u):
+            whole = t.as_strided((t.numel() // 512 * (512 + pad),), (1,), t.storage_offset())
+            assert whole.view(-1, 512 + pad)[:, 512:].isnan().all()
+
+
+def test_norm_in_place(dev, R):
+    h, y = _rand(dev, 1, 2, 50, 768), _rand(dev, 2, 2, 50, 768).to(BF16)
+    want = R.norm_residual(h, y)
+    h2, y2 = h.clone(), y.clone()
+    got = R.norm_residual(h2, y2, h_out=h2, u=y2)
+    assert got[0] is h2 and got[1] is y2 and torch.equal(h2, want[0]) and torch.equal(y2, want[1])
+
+
+def test_norm_special_rows(dev, R):
+    """Zero rows, a constant row (variance 0), rows whose sum of squares passes the
+    float32 range, NaN and infinity: each row by itself, the others untouched."""
+    D = 512
+    h = _rand(dev, 1, 1, 8, D)
+    y = _rand(dev, 2, 1, 8, D)
+    want = R.norm_residual(h, y, u_dtype=F32)
+    h[0, 1], y[0, 1] = 0.0, 0.0
+    h[0, 2], y[0, 2] = 5.0, 0.0
+    y[0, 3] *= 1e30
+    h[0, 4, 9] = float("nan")
+    h[0, 5, 9] = float("inf")
+    ho, u = R.norm_residual(h, y, u_dtype=F32)
+    assert (u[0, 1] == 0).all() and (u[0, 2].abs() <= 512 * 5 * F.D * 1e3 * 2).all()
+    assert torch.equal(ho[0, 3], h[0, 3])  # an overflowing sum of squares gives scale 0
+    assert u[0, 4].isnan().all() and u[0, 5].isnan().any()
+    for t in (0, 6, 7):
+        assert torch.equal(ho[0, t], want[0][0, t]) and torch.equal(u[0, t], want[1][0, t])
+    q, s = R.norm_residual(h, y, u_dtype=FP8)[1:]
+    assert (s[0, 1] == 1).all() and (q[0, 1].float() == 0).all() and s[0, 4].isnan().all()
+
+
+def test_norm_many_rows(dev, R):
+    """More rows than one round of the chip, four samples, modulation per sample."""
+    B, T, D = 4, 1203, 320
+    h, y = _rand(dev, 1, B, T, D), _rand(dev, 2, B, T, D).to(BF16)
+    _check_norm(R, h, y, BF16, gate=_rand(dev, 3, B, 1, D), scale=_rand(dev, 4, B, 1, D), shift=_rand(dev, 5, B, 1, D))
+
+
+# ------------------------------------------------------------- 8-bit blocks
+@pytest.mark.parametrize("M,K", [(1, 1), (1, 128), (3, 127), (5, 129), (130, 1216), (257, 64), (2, 8200), (300, 300)])
+@pytest.mark.parametrize("rows", [1, 128])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_quantize(dev, R, M, K, rows, dtype):
+    x = (_rand(dev, 1, M, K) * torch.exp2(12 * _rand(dev, 2, M, 1))).to(dtype)
+    q, s = R.quantize_fp8(x, block_rows=rows)
+    assert q.shape == (M, K) and q.dtype == FP8 and (M == 1 or q.stride(0) % 16 == 0)
+    F.check_blocks(q, s, F.f64(x), torch.zeros(M, K, dtype=torch.float64), rows)
+
+
+@pytest.mark.parametrize("rows", [1, 128])
+def test_quantize_special_blocks(dev, R, rows):
+    x = _rand(dev, 1, 128, 640)
+    x[:, :128] = 0
+    x[:, 128:256] *= 1e-38
+    x[5, 300] = float("nan")
+    x[6, 400] = float("-inf")
+    x[7, 513] = 3e38
+    q, s = R.quantize_fp8(x, block_rows=rows)
+    assert (s[:, 0] == 1).all() and (q[:, :128].float() == 0).all()
+    assert (s[:, 1] >= 2.0 ** -126).all() and q[:, 128:256].float().isfinite().all()
+    full = s.repeat_interleave(rows, 0).repeat_interleave(128, 1)
+    bad = ~(q.float() * full).isfinite()
+    want = torch.zeros(128, 640, dtype=torch.bool, device=dev)
+    want[slice(0, 128) if rows == 128 else 5, 256:384] = True
+    want[slice(0, 128) if rows == 128 else 6, 384:512] = True
+    assert (q.float() * full)[want].isnan().all()
+    assert not bad[~want].any()
+
+
+def test_quantize_strides(dev, R):
+    x = _strided(_rand(dev, 1, 9, 300).to(BF16), (0,), 5, 1)
+    q = torch.full((9, 320), 7.0, device=dev).to(FP8)
+    s = torch.full((9, 5), -1.0, device=dev)
+    R.quantize_fp8(x, q=q[:, :300], scale=s[:, :3])
+    F.check_blocks(q[:, :300], s[:, :3], F.f64(x), torch.zeros(9, 300, dtype=torch.float64))
+    assert (q[:, 300:].float() == 7).all() and (s[:, 3:] == -1).all()
+    one = R.quantize_fp8(x[:1].expand(4, 300))
+    assert torch.equal(one[0][0].float(), one[0][3].float())
+
+
+# ------------------------------------------------------------- block product
+def _operands(R, dev, M, N, K, seed=1):
+    spread = torch.exp2(2 * _rand(dev, seed + 10, 1, -(-K // 128)).repeat_interleave(128, 1)[:, :K])
+    a, sa = R.quantize_fp8(_rand(dev, seed, M, K) * spread)
+    w, sw = R.quantize_fp8(0.02 * _rand(dev, seed + 1, N, K), block_rows=128)
+    return a, sa, w, sw
+
+
+def _check_matmul(R, ops, dtype, bias=None, gelu=False, **kw):
+    out = R.matmul_fp8(*ops, bias=bias, gelu=gelu, out_dtype=dtype, **kw)
+    F.check(out, *F.matmul(*ops, bias, gelu, dtype), dtype=dtype)
+    return out
+
+
+PRODUCTS = [(1, 1, 1), (1, 64, 128), (1, 4608, 1536), (3, 130, 200), (16, 256, 1024), (17, 100, 127), (33, 4096, 64),
+            (64, 640, 512), (65, 129, 129), (128, 128, 128), (129, 257, 384), (200, 500, 1000), (513, 1216, 640),
+            (1000, 768, 768), (2306, 320, 256)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,N,K", PRODUCTS)
+def test_matmul(dev, R, M, N, K, dtype):
+    ops = _operands(R, dev, M, N, K)
+    _check_matmul(R, ops, dtype)
+    _check_matmul(R, ops, dtype, bias=_rand(dev, 9, N), gelu=True)
+
+
+def test_matmul_strides_and_tail_bytes(dev, R):
+    """Padded rows whose bytes past K are NaN, strided scales, an odd result row
+    stride: none of it enters, the elements between stay."""
+    M, N, K = 70, 90, 333
+    a, sa, w, sw = _operands(R, dev, M, N, K)
+    want = R.matmul_fp8(a, sa, w, sw, out_dtype=F32)
+    pad = lambda q: torch.full((q.shape[0], 400), 127, dtype=torch.uint8, device=dev).view(FP8)  # noqa: E731
+    a2, w2 = pad(a), pad(w)
+    a2.view(torch.uint8)[:, :K] = a.view(torch.uint8)
+    w2.view(torch.uint8)[:, :K] = w.view(torch.uint8)
+    sa2, sw2 = torch.full((M, 7), float("nan"), device=dev), torch.full((1, 9), float("nan"), device=dev)
+    sa2[:, :3], sw2[:, :3] = sa, sw
+    out = torch.full((M, 95), -3.0, device=dev)
+    R.matmul_fp8(a2[:, :K], sa2[:, :3], w2[:, :K], sw2[:, :3], out=out[:, :N])
+    assert torch.equal(out[:, :N], want) and (out[:, N:] == -3).all()
+
+
+def test_matmul_non_finite_rows(dev, R):
+    """NaN in a row of a or w (value or scale) stays in that row or column."""
+    M, N, K = 40, 200, 256
+    a, sa, w, sw = _operands(R, dev, M, N, K)
+    want = R.matmul_fp8(a, sa, w, sw, out_dtype=F32)
+    a.view(torch.uint8)[3, 200] = 127
+    w.view(torch.uint8)[150, 7] = 127
+    sa[8, 1] = float("nan")
+    out = R.matmul_fp8(a, sa, w, sw, out_dtype=F32)
+    bad = torch.zeros(M, N, dtype=torch.bool, device=dev)
+    bad[3] = bad[8] = True
+    bad[:, 150] = True
+    assert out[bad].isnan().all() and torch.equal(out[~bad], want[~bad])
+
+
+def test_matmul_offsets_past_32_bits(dev, R):
+    M, N, K = 2, 70, 256
+    a, sa, w, sw = _operands(R, dev, M, N, K)
+    step = (1 << 31) + 256
+    far = torch.empty(step + K, dtype=torch.uint8, device=dev).view(FP8).as_strided((M, K), (step, 1))
+    far.copy_(a)
+    out = torch.empty(step + N, dtype=F32, device=dev).as_strided((M, N), (step, 1))
+    R.matmul_fp8(far, sa, w, sw, out=out)
+    assert torch.equal(out, R.matmul_fp8(a, sa, w, sw, out_dtype=F32))
+
+
+# ------------------------------------------------------------- as they are used
+def _half_layer(R, st):
+    """Residual and pre-norm into 8-bit blocks, QKV product, rotation of q and k."""
+    B, T, D, H = st["B"], st["T"], st["D"], st["H"]
+    h, u, s = R.norm_residual(st["h"], st["y"], gate=st["gate"], scale=st["scale"], shift=st["shift"], u_dtype=FP8,
+                              h_out=st["h_out"], u=st["u"], u_scale=st["s"])
+    qkv = R.matmul_fp8(u.view(B * T, D), s.view(B * T, -1), st["w"], st["sw"], bias=st["bias"], out=st["qkv"])
+    q, k, v = qkv.view(B, T, 3, H, D // H).unbind(2)
+    return R.rope(q, k, st["pos"], (8, 12, 12), st["freq"], q_gain=st["g"], k_gain=st["g"], q_out=st["q"], k_out=st["k"])
+
+
+def _half_layer_state(R, dev, seed=1):
+    B, T, D, H = 2, 75, 256, 4
+    w, sw = R.quantize_fp8(0.02 * _rand(dev, seed, 3 * D, D), block_rows=128)
+    st = dict(B=B, T=T, D=D, H=H, w=w, sw=sw, h=_rand(dev, seed + 1, B, T, D), y=_rand(dev, seed + 2, B, T, D).to(BF16),
+              gate=_rand(dev, seed + 3, B, 1, D), scale=0.3 * _rand(dev, seed + 4, B, 1, D),
+              shift=0.3 * _rand(dev, seed + 5, B, 1, D), bias=0.02 * _rand(dev, seed + 6, 3 * D),
+              pos=_positions(dev, T), freq=R.rope_frequencies((8, 12, 12)), g=1 + 0.1 * _rand(dev, seed + 7, D // H))
+    st.update(h_out=torch.empty_like(st["h"]), u=torch.empty(B, T, D, dtype=FP8, device=dev),
+              s=torch.empty(B, T, 2, device=dev), qkv=torch.empty(B * T, 3 * D, dtype=BF16, device=dev),
+              q=torch.empty(B, T, H, D // H, dtype=BF16, device=dev),
+              k=torch.empty(B, T, H, D // H, dtype=BF16, device=dev))
+    return st
+
+
+def test_together(dev, R):
+    st = _half_layer_state(R, dev)
+    q, k = _half_layer(R, st)
+    (ho, eh), (u, eu) = F.norm_residual(st["h"], st["y"], gate=st["gate"], scale=st["scale"], shift=st["shift"])
+    F.check(st["h_out"], ho, eh)
+    F.check_blocks(st["u"].view(-1, 256), st["s"].view(-1, 2), u.view(-1, 256), eu.view(-1, 256))
+    ops = (st["u"].view(-1, 256), st["s"].view(-1, 2), st["w"], st["sw"])
+    F.check(st["qkv"], *F.matmul(*ops, st["bias"], dtype=BF16), dtype=BF16)
+    parts = st["qkv"].view(2, 75, 3, 4, 64).unbind(2)
+    for got, x in ((q, parts[0]), (k, parts[1])):
+        F.check(got, *F.rope(x, st["pos"], (8, 12, 12), st["freq"], "halves", st["g"]), dtype=BF16)
+
+
+def test_other_stream_and_overlapping_calls(dev, R):
+    """Calls on two streams at once share nothing; results equal those of one stream."""
+    a, b = _half_layer_state(R, dev, 1), _half_layer_state(R, dev, 50)
+    want = [tuple(t.clone() for t in _half_layer(R, st)) for st in (a, b)]
+    for st in (a, b):
+        st["q"].zero_(), st["k"].zero_()
+    streams = [torch.cuda.Stream(dev) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for st, s in zip((a, b), streams):
+            with torch.cuda.stream(s):
+                _half_layer(R, st)
+    torch.cuda.synchronize()
+    for st, w in zip((a, b), want):
+        assert torch.equal(st["q"], w[0]) and torch.equal(st["k"], w[1])
+    # a stream given by hand
+    s = torch.cuda.Stream(dev)
+    s.wait_stream(torch.cuda.current_stream())
+    out = R.rope(a["q"], None, a["pos"], (8, 12, 12), a["freq"], stream=s)[0]
+    s.synchronize()
+    assert torch.equal(out, R.rope(a["q"], None, a["pos"], (8, 12, 12), a["freq"])[0])
+
+
+def test_captured_and_replayed(dev, R):
+    st, other = _half_layer_state(R, dev, 1), _half_layer_state(R, dev, 50)
+    _half_layer(R, st)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _half_layer(R, st)
+    for seed in range(3):
+        st["h"].copy_(_rand(dev, 100 + seed, 2, 75, 256))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [st[n].clone() for n in ("h_out", "u", "s", "qkv", "q", "k")]
+        _half_layer(R, other)  # eager work between the replays
+        _half_layer(R, st)
+        for g, n in zip(got, ("h_out", "u", "s", "qkv", "q", "k")):
+            assert torch.equal(g.float(), st[n].float()), n
+
+
+def test_same_bits_twice(dev, R):
+    st = _half_layer_state(R, dev)
+    first = [t.clone() for t in _half_layer(R, st)]
+    for t, g in zip(_half_layer(R, st), first):
+        assert torch.equal(t, g)
+
+
+# ------------------------------------------------------------- refusals in the binding
+def test_binding_refusals(dev, R):
+    x = _rand(dev, 1, 2, 4, 3, 64).to(BF16)
+    pos, sec, freq = _positions(dev, 4), (8, 12, 12), R.rope_frequencies((8, 12, 12))
+    for bad in (dict(pos=pos.double()), dict(pos=pos[:3]), dict(freq=freq[:-1]), dict(sections=(8, 24)),
+                dict(layout="other"), dict(q_gain=torch.ones(63, device=dev)), dict(k=x.float()), dict(k=x[:1]),
+                dict(q=x[0]), dict(q=x.transpose(2, 3)), dict(q=x.half()), dict(q_out=torch.empty_like(x)[:1]),
+                dict(q_out=x[:, :, :1].expand_as(x)), dict(sections=(20, 12, 1), freq=np.ones(33))):
+        kw = dict(q=x, k=x, pos=pos, sections=sec, freq=freq)
+        kw.update(bad)
+        with pytest.raises(R.WamError):
+            R.rope(kw.pop("q"), kw.pop("k"), kw.pop("pos"), kw.pop("sections"), kw.pop("freq"), **kw)
+    h = _rand(dev, 1, 2, 4, 64)
+    for bad in (dict(y=h[:1]), dict(gate=torch.ones(2, 64, device=dev)), dict(gate=torch.ones(2, 4, 1, device=dev)),
+                dict(post="x"), dict(pre="x"), dict(u_dtype=torch.float16), dict(post_gain=torch.ones(1, device=dev)),
+                dict(u=h), dict(h_out=torch.empty(2, 4, 64, dtype=BF16, device=dev)), dict(eps=-1.0)):
+        with pytest.raises(R.WamError):
+            R.norm_residual(h, **bad)
+    with pytest.raises(R.WamError):
+        R.quantize_fp8(h[0], block_rows=2)
+    a, sa, w, sw = _operands(R, dev, 8, 64, 256)
+    for bad in (dict(w=w[:, :128]), dict(a_scale=sa[:, :1]), dict(w_scale=sw.double()), dict(bias=torch.ones(65, device=dev)),
+                dict(out_dtype=torch.float16), dict(a=a.view(torch.uint8)), dict(a=a[:, 1:], w=w[:, 1:])):
+        kw = dict(a=a, a_scale=sa, w=w, w_scale=sw)
+        kw.update(bad)
+        with pytest.raises(R.WamError):
+            R.matmul_fp8(kw.pop("a"), kw.pop("a_scale"), kw.pop("w"), kw.pop("w_scale"), **kw)
+
+
+def test_empty_shapes(dev, R):
+    sec, freq = (8, 12, 12), R.rope_frequencies((8, 12, 12))
+    q = torch.empty(1, 0, 2, 64, device=dev)
+    assert R.rope(q, q, torch.empty(0, 3, device=dev), sec, freq)[0].shape == q.shape
+    assert R.norm_residual(torch.empty(0, 3, 64, device=dev))[1].shape == (0, 3, 64)
+    assert R.quantize_fp8(torch.empty(0, 64, device=dev))[0].shape == (0, 64)
+    a, sa, w, sw = _operands(R, dev, 4, 64, 128)
+    assert R.matmul_fp8(a[:0], sa[:0], w, sw).shape == (0, 64)

@@ -257,7 +257,8 @@ def _calls(case, t):
         return list(R.rope(t["q"], t["k"], t["pos"], t["sections"], t["ladder"], layout=case["layout"],
                            q_gain=t["q_gain"], k_gain=t["k_gain"], eps=EPS, q_out=t["q_out"], k_out=t["k_out"]))
     if kind == "norm":
-        return list(R.norm_residual(t["h"], t["y"], post=case["post"], post_gain=t["post_gain"], gate=t["gate"],
+        gain = t["post_gain"] if case["post"] != "none" else None
+        return list(R.norm_residual(t["h"], t["y"], post=case["post"], post_gain=gain, gate=t["gate"],
                                     res_scale=case["res_scale"], pre=case["pre"], scale=t["scale"], shift=t["shift"],
                                     eps=EPS, u_dtype=DTYPES[case["u"]]))
     if kind == "quantize":

@@ -21,10 +21,39 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return v;
 }
 
+// Maximum over aligned groups of N = 8 or 16 lanes, in every lane of the group,
+// on the data-parallel crossbar (lane ^ 1, lane ^ 2, mirrored 8, mirrored 16).
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, false);
+}
+template <int N>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  static_assert(N == 8 || N == 16, "group size");
+  v = max(v, dpp<0xb1>(v));
+  v = max(v, dpp<0x4e>(v));
+  v = max(v, dpp<0x141>(v));
+  if constexpr (N == 16) v = max(v, dpp<0x140>(v));
+  return v;
+}
+
+// x / s rounded to float32 from r, the rounded reciprocal of s: the quotient
+// estimate corrected by its exact remainder (three instructions; the compiler's
+// division takes ten).  Where s is infinite or NaN the result is NaN.
+__device__ __forceinline__ float divide_by(float x, float s, float r) {
+  const float q = x * r;
+  return fmaf(fmaf(-q, s, x), r, q);
+}
+
 // scale of a block whose largest magnitude has these bits
 __device__ __forceinline__ float block_scale(uint32_t most) {
   const float s = __uint_as_float(most) / kE4m3Max;
   return most == 0 ? 1.0f : s < kMinScale ? kMinScale : s;
+}
+
+// four nearest e4m3 values, ties to even, as the bytes of a word
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
 }
 
 // nearest e4m3 value, ties to even (|x| <= 448 but for a rounding; NaN stays)

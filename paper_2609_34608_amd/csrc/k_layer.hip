@@ -21,6 +21,25 @@ __device__ __forceinline__ void store1(void* p, int64_t i, int dtype, float v) {
   else static_cast<float*>(p)[i] = v;
 }
 
+// N consecutive elements at p, which needs only the alignment of an element:
+// global memory takes wide loads and stores at any address.  Elements from n on
+// are zero (not loaded) or left alone (not stored).
+template <typename T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) Pack {
+  T v[N];
+};
+template <int N, typename T>
+__device__ __forceinline__ void load_n(float (&x)[N], const T* p, int n) {
+  if (n >= N) {
+    const Pack<T, N> w = *reinterpret_cast<const Pack<T, N>*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = to_f32(w.v[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = i < n ? to_f32(p[i]) : 0.f;
+  }
+}
+
 // ------------------------------------------------------------- rotary positions
 constexpr int kMaxPairs = WAM_MAX_HEAD / 2;
 struct RopeParams {
@@ -40,8 +59,133 @@ __device__ __forceinline__ void axis_turn(const RopeParams& p, const float* pos,
   sincospif((float)(2.0 * t), &s, &c);
 }
 
-// One wave per head vector, element e = lane + 64 j: any head size, layout,
-// stride and alignment.
+// Sum over aligned groups of n lanes (a power of two up to 16), in every lane.
+__device__ __forceinline__ float lanes_sum(float v, int n) {
+  auto add = [&](auto CTRL) __attribute__((always_inline)) {
+    v += __uint_as_float(dpp<decltype(CTRL)::value>(__float_as_uint(v)));
+  };
+  if (n >= 2) add(std::integral_constant<int, 0xb1>{});
+  if (n >= 4) add(std::integral_constant<int, 0x4e>{});
+  if (n >= 8) add(std::integral_constant<int, 0x141>{});
+  if (n >= 16) add(std::integral_constant<int, 0x140>{});
+  return v;
+}
+
+// Which rows and heads a block and its waves take (rope_units_kernel).
+struct RopeTiling {
+  int lanes;        // lanes per head vector, a power of two >= dh / 16
+  int heads_wave;   // head vectors of one row side by side in a wave
+  int wave_rows;    // waves side by side along the rows (the others along the heads)
+  int heads_block;  // heads of a block
+};
+constexpr int kRopeTable = 2048;  // most (row, pair) angles of a block
+
+// Head vectors of whole units of 16 elements: eight pairs, or 16 elements past the
+// rotated ones.  A lane takes one unit with two 8-element loads (the two halves
+// of the pairs, or 16 neighbours), so that a pair never leaves its lane and only
+// the norm needs the other lanes of its vector.  The block's angles are computed
+// once, in LDS, while the first loads are in flight, and a lane keeps those of
+// its unit in registers for all the heads it visits.
+template <typename T, bool PAIRS, bool NORM>
+__global__ __launch_bounds__(256) void rope_units_kernel(RopeParams p, RopeTiling tl) {
+  __shared__ float2 turn[kRopeTable];
+  const wam_rope_args& a = p.a;
+  const bool isq = blockIdx.z == 0 && a.Hq > 0;
+  const int H = isq ? a.Hq : a.Hk;
+  const int64_t* si = isq ? a.q_stride : a.k_stride;
+  const int64_t* so = isq ? a.q_out_stride : a.k_out_stride;
+  const int h_end = min(((int)blockIdx.y + 1) * tl.heads_block, H);
+
+  const int lane = threadIdx.x % kWave, wid = threadIdx.x / kWave;
+  const int unit = lane % tl.lanes, slot = lane / tl.lanes;
+  const int rows_wave = kWave / tl.lanes / tl.heads_wave;
+  const int row_in_block = (wid % tl.wave_rows) * rows_wave + slot / tl.heads_wave;
+  const int rows_block = rows_wave * tl.wave_rows;
+  const int head_step = tl.heads_wave * (4 / tl.wave_rows);
+  int h = (int)blockIdx.y * tl.heads_block + (wid / tl.wave_rows) * tl.heads_wave + slot % tl.heads_wave;
+
+  const int64_t rows = (int64_t)a.B * a.T, row0 = (int64_t)blockIdx.x * rows_block;
+  const int64_t row = row0 + row_in_block;
+  const int b = (int)(row / a.T), t = (int)(row % a.T);
+  const bool live = row < rows && 16 * unit < a.dh;
+  const int turned = p.pairs / 8;  // units that turn
+  const int e1 = PAIRS || unit >= turned ? 16 * unit : 8 * unit;
+  const int e2 = PAIRS || unit >= turned ? e1 + 8 : e1 + p.pairs;
+  const T* x = static_cast<const T*>(isq ? a.q : a.k) + (live ? b * si[0] + t * si[1] : 0);
+  T* o = static_cast<T*>(isq ? a.q_out : a.k_out) + (live ? b * so[0] + t * so[1] : 0);
+
+  float x1[8], x2[8];
+  auto load = [&](int hh) __attribute__((always_inline)) {
+    if (live && hh < h_end) {
+      load_n(x1, x + hh * si[2] + e1, 8);
+      load_n(x2, x + hh * si[2] + e2, 8);
+    }
+  };
+  load(h);
+  for (int i = threadIdx.x; i < rows_block * p.pairs; i += 256) {
+    const int r = i / p.pairs;
+    const int64_t rr = min(row0 + r, rows - 1);
+    const float* pos = a.pos + rr / a.T * a.pos_stride + rr % a.T * 3;
+    float c, s;
+    axis_turn(p, pos, i % p.pairs, c, s);
+    turn[i] = make_float2(c, s);
+  }
+  float g1[8], g2[8];
+  if constexpr (NORM) {
+    const float* gain = isq ? a.q_gain : a.k_gain;
+    if (live && gain) {
+      load_n(g1, gain + e1, 8);
+      load_n(g2, gain + e2, 8);
+    }
+  }
+  __syncthreads();
+  float c[8], s[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float2 cs = unit < turned ? turn[row_in_block * p.pairs + 8 * unit + j] : make_float2(1.f, 0.f);
+    c[j] = cs.x, s[j] = cs.y;
+  }
+  const bool normed = NORM && (isq ? a.q_gain : a.k_gain);
+  for (int h0 = 0; h0 < tl.heads_block; h0 += head_step, h += head_step) {
+    float y1[8], y2[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y1[j] = x1[j], y2[j] = x2[j];
+    load(h + head_step);  // the next head's while this one is turned
+    if constexpr (NORM) {
+      if (normed) {
+        float ss = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) ss += y1[j] * y1[j] + y2[j] * y2[j];
+        const float rs = rsqrt_newton(lanes_sum(live && h < h_end ? ss : 0.f, tl.lanes) / (float)a.dh + a.eps);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y1[j] *= rs * g1[j], y2[j] *= rs * g2[j];
+      }
+    }
+    Pack<T, 8> o1, o2;
+    if constexpr (PAIRS) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o1.v[2 * j] = static_cast<T>(y1[2 * j] * c[j] - y1[2 * j + 1] * s[j]);
+        o1.v[2 * j + 1] = static_cast<T>(y1[2 * j] * s[j] + y1[2 * j + 1] * c[j]);
+        o2.v[2 * j] = static_cast<T>(y2[2 * j] * c[4 + j] - y2[2 * j + 1] * s[4 + j]);
+        o2.v[2 * j + 1] = static_cast<T>(y2[2 * j] * s[4 + j] + y2[2 * j + 1] * c[4 + j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        o1.v[j] = static_cast<T>(y1[j] * c[j] - y2[j] * s[j]);
+        o2.v[j] = static_cast<T>(y1[j] * s[j] + y2[j] * c[j]);
+      }
+    }
+    if (live && h < h_end) {
+      *reinterpret_cast<Pack<T, 8>*>(o + h * so[2] + e1) = o1;
+      *reinterpret_cast<Pack<T, 8>*>(o + h * so[2] + e2) = o2;
+    }
+  }
+}
+
+// Any other head size or sections: one wave per head vector, element e = lane +
+// 64 j.
 __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
   const wam_rope_args& a = p.a;
   const int heads = a.Hq + a.Hk;
@@ -183,27 +327,87 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
 }
 
 // ------------------------------------------------------------- quantisation
-// One block per scale, any width, stride and alignment: thread t of block_rows x
-// 128 values takes column t % 128 of every other row.
-__global__ __launch_bounds__(256) void quantize_kernel(wam_quantize_args a) {
-  __shared__ uint32_t top[4];
-  const int kb = (a.K + kScaleBlock - 1) / kScaleBlock;
-  const int bk = blockIdx.x % kb;
-  const int64_t bm = blockIdx.x / kb;
-  const int col = bk * kScaleBlock + threadIdx.x % kScaleBlock;
-  const int64_t m0 = bm * a.block_rows, m1 = min(m0 + a.block_rows, (int64_t)a.M);
+// A thread takes 16 columns of a row (two 16-byte loads of bf16, one 16-byte
+// store), eight neighbouring threads a scale block of the row, whose maximum
+// they share without LDS; the row is read once, from registers.
+constexpr int kQuantCols = 16, kQuantGroup = kScaleBlock / kQuantCols;
+
+__device__ __forceinline__ uint32_t most_of(const float (&x)[kQuantCols]) {
   uint32_t most = 0;
-  if (col < a.K)
-    for (int64_t m = m0 + threadIdx.x / kScaleBlock; m < m1; m += 2)
-      most = max(most, abs_bits(load1(a.x, m * a.x_stride + col, a.dtype)));
+#pragma unroll
+  for (int i = 0; i < kQuantCols; ++i) most = max(most, abs_bits(x[i]));
+  return most;
+}
+
+// e4m3 of x / s into the first n bytes at q
+__device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&x)[kQuantCols], float s, int n) {
+  const float r = 1.0f / s;
+  Pack<uint32_t, kQuantCols / 4> w;
+#pragma unroll
+  for (int i = 0; i < kQuantCols / 4; ++i)
+    w.v[i] = pack_e4m3(divide_by(x[4 * i], s, r), divide_by(x[4 * i + 1], s, r), divide_by(x[4 * i + 2], s, r),
+                       divide_by(x[4 * i + 3], s, r));
+  if (n >= kQuantCols) {
+    struct __attribute__((packed, aligned(1))) Bytes {
+      Pack<uint32_t, kQuantCols / 4> w;
+    };
+    *reinterpret_cast<Bytes*>(q) = Bytes{w};
+  } else {
+#pragma unroll
+    for (int i = 0; i < kQuantCols; ++i)
+      if (i < n) q[i] = (uint8_t)(w.v[i / 4] >> (8 * (i % 4)));
+  }
+}
+
+// blocks of 1 x 128
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(wam_quantize_args a, int kb) {
+  const uint32_t i = blockIdx.x * 32u + threadIdx.x / kQuantGroup;  // scale block
+  const int m = (int)(i / (uint32_t)kb), bk = (int)(i % (uint32_t)kb);
+  if (m >= a.M) return;
+  const int col = bk * kScaleBlock + (threadIdx.x % kQuantGroup) * kQuantCols;
+  float x[kQuantCols];
+  load_n(x, static_cast<const T*>(a.x) + m * a.x_stride + col, a.K - col);
+  const float s = block_scale(group_max<kQuantGroup>(most_of(x)));
+  if (threadIdx.x % kQuantGroup == 0) a.scale[m * a.scale_stride + bk] = s;
+  store_e4m3(static_cast<uint8_t*>(a.q) + m * a.q_stride + col, x, s, a.K - col);
+}
+
+// blocks of 128 x 128: one per thread block, four rows per thread in registers
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_tiles_kernel(wam_quantize_args a, int kb) {
+  __shared__ uint32_t top[4];
+  constexpr int kRows = kScaleBlock * kQuantGroup / 256;
+  const int bk = blockIdx.x % kb, bm = blockIdx.x / kb;
+  const int col = bk * kScaleBlock + (threadIdx.x % kQuantGroup) * kQuantCols;
+  const int64_t m0 = (int64_t)bm * kScaleBlock + threadIdx.x / kQuantGroup;
+  float x[kRows][kQuantCols];
+  uint32_t most = 0;
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) {
+    const int64_t m = m0 + j * (256 / kQuantGroup);
+    load_n(x[j], static_cast<const T*>(a.x) + m * a.x_stride + col, m < a.M ? a.K - col : 0);
+    most = max(most, most_of(x[j]));
+  }
   most = wave_max(most);
   if (threadIdx.x % kWave == 0) top[threadIdx.x / kWave] = most;
   __syncthreads();
   const float s = block_scale(max(max(top[0], top[1]), max(top[2], top[3])));
   if (threadIdx.x == 0) a.scale[bm * a.scale_stride + bk] = s;
-  if (col < a.K)
-    for (int64_t m = m0 + threadIdx.x / kScaleBlock; m < m1; m += 2)
-      static_cast<uint8_t*>(a.q)[m * a.q_stride + col] = to_e4m3(load1(a.x, m * a.x_stride + col, a.dtype) / s);
+#pragma unroll
+  for (int j = 0; j < kRows; ++j) {
+    const int64_t m = m0 + j * (256 / kQuantGroup);
+    if (m < a.M) store_e4m3(static_cast<uint8_t*>(a.q) + m * a.q_stride + col, x[j], s, a.K - col);
+  }
+}
+
+template <typename T>
+hipError_t launch_quantize(const wam_quantize_args& a, hipStream_t s) {
+  const int kb = (a.K + kScaleBlock - 1) / kScaleBlock;
+  const int64_t n = (int64_t)kb * ((a.M + a.block_rows - 1) / a.block_rows);
+  if (a.block_rows == 1) launch_k(quantize_rows_kernel<T>, dim3((unsigned)((n + 31) / 32)), 256, 0, s, a, kb);
+  else launch_k(quantize_tiles_kernel<T>, dim3((unsigned)n), 256, 0, s, a, kb);
+  return hipGetLastError();
 }
 
 // ------------------------------------------------------------- argument checks
@@ -259,9 +463,48 @@ int check_heads(int H, const wam_rope_args* a, const void* x, const void* out, c
   return WAM_OK;
 }
 
+template <typename T, bool PAIRS>
+void launch_rope_units(const RopeParams& p, const RopeTiling& tl, dim3 grid, hipStream_t s) {
+  if (p.a.q_gain || p.a.k_gain) launch_k(rope_units_kernel<T, PAIRS, true>, grid, 256, 0, s, p, tl);
+  else launch_k(rope_units_kernel<T, PAIRS, false>, grid, 256, 0, s, p, tl);
+}
+
 hipError_t launch_rope(const RopeParams& p, hipStream_t s) {
-  const int64_t items = (int64_t)p.a.B * p.a.T * (p.a.Hq + p.a.Hk);
-  launch_k(rope_kernel, dim3((unsigned)((items + 3) / 4)), 256, 0, s, p);
+  const wam_rope_args& a = p.a;
+  const int64_t rows = (int64_t)a.B * a.T;
+  const int H = a.Hq > a.Hk ? a.Hq : a.Hk;
+  if (a.dh % 16 || p.pairs % 8) {
+    const int64_t items = rows * (a.Hq + a.Hk);
+    launch_k(rope_kernel, dim3((unsigned)((items + 3) / 4)), 256, 0, s, p);
+    return hipGetLastError();
+  }
+  RopeTiling tl{};
+  tl.lanes = 1;
+  while (tl.lanes * 16 < a.dh) tl.lanes *= 2;
+  const int slots = kWave / tl.lanes;
+  // lanes side by side in memory: heads of a row, or rows of a head
+  const int64_t* st = a.Hq > 0 ? a.q_stride : a.k_stride;
+  const bool rows_first = a.T > 1 && st[1] < st[2];
+  tl.heads_wave = 1;
+  if (!rows_first)
+    while (tl.heads_wave < slots && tl.heads_wave < H) tl.heads_wave *= 2;
+  tl.wave_rows = rows_first || rows < 4 * 256 ? 1 : 4;
+  const int rows_block = slots / tl.heads_wave * tl.wave_rows, head_step = tl.heads_wave * 4 / tl.wave_rows;
+  const int64_t row_blocks = (rows + rows_block - 1) / rows_block;
+  // heads of a block: few enough for eight blocks per CU, if there are that many
+  int steps = (H + head_step - 1) / head_step;
+  while (steps > 1 && row_blocks * ((H + head_step * steps - 1) / (head_step * steps)) < 1024) --steps;
+  tl.heads_block = head_step * steps;
+  const int64_t head_blocks = (H + tl.heads_block - 1) / tl.heads_block;
+  if (row_blocks > 0x7fffffff || head_blocks > 65535) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)row_blocks, (unsigned)head_blocks, a.Hq > 0 && a.Hk > 0 ? 2 : 1);
+  if (a.dtype == WAM_BF16) {
+    if (a.layout == WAM_ROPE_PAIRS) launch_rope_units<bf16, true>(p, tl, grid, s);
+    else launch_rope_units<bf16, false>(p, tl, grid, s);
+  } else {
+    if (a.layout == WAM_ROPE_PAIRS) launch_rope_units<float, true>(p, tl, grid, s);
+    else launch_rope_units<float, false>(p, tl, grid, s);
+  }
   return hipGetLastError();
 }
 
@@ -384,8 +627,9 @@ int wam_quantize_fp8(const wam_quantize_args* a, void* hip_stream) {
   if (!strides_ok(&a->x_stride, 1) || (a->M > 1 && a->q_stride < a->K) || (mb > 1 && a->scale_stride < kb))
     return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: x_stride must be >= 0, and rows of the results distinct");
   if (mb * kb > kMaxGrid) return noalloc_fail(WAM_E_SHAPE, "wam_quantize_fp8: too many blocks for one launch");
-  launch_k(quantize_kernel, dim3((unsigned)(mb * kb)), 256, 0, static_cast<hipStream_t>(hip_stream), *a);
-  if (hipGetLastError() != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_quantize_fp8: kernel launch failed");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if ((a->dtype == WAM_BF16 ? launch_quantize<bf16>(*a, s) : launch_quantize<float>(*a, s)) != hipSuccess)
+    return noalloc_fail(WAM_E_HIP, "wam_quantize_fp8: kernel launch failed");
   return WAM_OK;
 }
 

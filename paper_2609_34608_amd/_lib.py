@@ -152,11 +152,11 @@ EXPORTS = {
                                    C.POINTER(C.c_double)]),
     "wam_remap_noalloc": (C.c_int, [C.POINTER(WamConfig), C.POINTER(WamRemapArgs), C.c_void_p]),
     "wam_noalloc_last_error": (C.c_char_p, []),
-    "wam_rope": (C.c_int, [C.POINTER(WamRopeArgs), C.c_void_p]),
+    "wam_rope": (C.c_int, [C.c_void_p, C.c_void_p]),  # the argument structs: as packed bytes (runtime) or by reference
     "wam_rope_frequencies": (C.c_int, [C.POINTER(C.c_int32), C.c_double, C.c_int32, C.POINTER(C.c_double)]),
-    "wam_norm_residual": (C.c_int, [C.POINTER(WamNormArgs), C.c_void_p]),
-    "wam_quantize_fp8": (C.c_int, [C.POINTER(WamQuantizeArgs), C.c_void_p]),
-    "wam_matmul_fp8": (C.c_int, [C.POINTER(WamMatmulArgs), C.c_void_p]),
+    "wam_norm_residual": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_quantize_fp8": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_matmul_fp8": (C.c_int, [C.c_void_p, C.c_void_p]),
     "wam_probe_mfma_bf16": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.POINTER(C.c_double),
                                       C.POINTER(C.c_double)]),
     "wam_probe_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.POINTER(C.c_double),

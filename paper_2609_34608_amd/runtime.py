@@ -6,6 +6,8 @@ denoising path and of the adaptation operators runs in libwam's kernels.
 from __future__ import annotations
 
 import ctypes as C
+import struct
+from array import array
 from dataclasses import dataclass
 
 import numpy as np
@@ -352,22 +354,43 @@ def remap_noalloc(cfg: abi.WamConfig, x_bar, x_r, sigma_r, sigma_b0, shift_actio
 # ---------------------------------------------------------------- layer operators
 FP8 = torch.float8_e4m3fn
 _TYPES = {torch.float32: abi.WAM_FP32, torch.bfloat16: abi.WAM_BF16, FP8: abi.WAM_FP8}
+_REAL = (torch.float32, torch.bfloat16)
+_F32 = (torch.float32,)
+_F8 = (FP8,)
 _LAYOUTS = {"halves": abi.WAM_ROPE_HALVES, "pairs": abi.WAM_ROPE_PAIRS}
 _NORMS = {"none": abi.WAM_NORM_NONE, "rms": abi.WAM_NORM_RMS, "layer": abi.WAM_NORM_LAYER}
 
+# The argument structs as the C compiler lays them out (their ctypes twins in _lib):
+# packing one takes a microsecond, filling its twin ten.
+_ROPE_ARGS = struct.Struct("@10i4P12qPqP2Pf")
+_NORM_ARGS = struct.Struct("@8i5P10q3P6q2P2f")
+_QUANTIZE_ARGS = struct.Struct("@4iPqPqPq")
+_MATMUL_ARGS = struct.Struct("@5iPqPqPqPqPPq")
 
-def _operand(t, what, dtypes, dev, shape=None):
-    """Checks an operator's tensor: on dev, of one of dtypes, of the given shape,
-    its last dimension contiguous."""
-    if not isinstance(t, torch.Tensor) or t.device != dev or not t.is_cuda:
-        raise WamError(f"{what}: needs a tensor on {dev}")
+
+def _operand(t, what, dtypes, index, shape=None):
+    """Checks an operator's tensor: on GPU `index`, of one of dtypes, of the given
+    shape, its last dimension contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != index:
+        raise WamError(f"{what}: needs a tensor on the GPU of the first operand")
     if t.dtype not in dtypes:
         raise WamError(f"{what}: dtype {t.dtype} is not supported")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise WamError(f"{what}: shape {tuple(t.shape)} is not {tuple(shape)}")
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise WamError(f"{what}: the last dimension must be contiguous")
     return t
+
+
+def _first(t, what, dtypes, dim):
+    """Checks an operator's first tensor and returns the index of its GPU."""
+    if not isinstance(t, torch.Tensor) or t.dim() != dim:
+        raise WamError(f"{what}: needs a tensor of {dim} dimensions")
+    if not t.is_cuda:
+        raise WamError(f"{what}: libwam takes device tensors only")
+    index = t.get_device()
+    _operand(t, what, dtypes, index)
+    return index
 
 
 def _choice(table, key, what):
@@ -377,31 +400,46 @@ def _choice(table, key, what):
         raise WamError(f"{what}: unknown value {key!r}") from None
 
 
-def _call(fn, args, dev, stream, what):
-    """Enqueues a handle-free operator on dev (stream: default torch's current one)."""
-    if stream is None:
-        stream = torch.cuda.current_stream(dev)
-    if dev.index == torch.cuda.current_device():
-        rc = fn(C.byref(args), C.c_void_p(stream.cuda_stream))
+def _call(fn, args, index, stream, what):
+    """Enqueues a handle-free operator on GPU `index` (stream: default torch's current one)."""
+    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if index == torch._C._cuda_getDevice():
+        rc = fn(args, handle)
     else:
-        with torch.cuda.device(dev):
-            rc = fn(C.byref(args), C.c_void_p(stream.cuda_stream))
+        with torch.cuda.device(index):
+            rc = fn(args, handle)
     if rc != abi.WAM_OK:
         raise WamError(f"{what}: {abi.lib().wam_status_string(rc).decode()}: "
                        f"{abi.lib().wam_noalloc_last_error().decode()}")
+
+
+def _pack(form, what, *values):
+    try:
+        return form.pack(*values)
+    except struct.error as e:
+        raise WamError(f"{what}: {e}") from None
+
+
+def _ptr_or_0(t):
+    return 0 if t is None else t.data_ptr()
 
 
 def rope_frequencies(sections, theta=10000.0, shared=False) -> np.ndarray:
     """Frequencies of the usual ladder for rope (wam_rope_frequencies): float64
     [sum(sections)], theta^(-j / n) along each axis of n pairs, or one ladder
     over all pairs."""
+    if len(sections) != 3:
+        raise WamError("rope_frequencies: needs three sections")
     sec = (C.c_int32 * 3)(*sections)
-    freq = np.empty(max(sum(sec), 0), np.float64)
+    freq = np.empty(min(max(sum(sec), 0), abi.WAM_MAX_HEAD // 2), np.float64)
     lib = abi.lib()
     rc = lib.wam_rope_frequencies(sec, theta, int(bool(shared)), freq.ctypes.data_as(C.POINTER(C.c_double)))
     if rc != abi.WAM_OK:
         raise WamError(f"wam_rope_frequencies: {lib.wam_noalloc_last_error().decode()}")
     return freq
+
+
+_NO_HEADS = (0, 0, 0)
 
 
 def rope(q, k, pos, sections, freq, *, layout="halves", q_gain=None, k_gain=None, eps=1e-6, q_out=None, k_out=None,
@@ -411,38 +449,56 @@ def rope(q, k, pos, sections, freq, *, layout="halves", q_gain=None, k_gain=None
     pos float32 [T, 3] or [B, T, 3]; freq on the host, one value per pair.  With
     gains, float32 [dh], the per-head RMS norm comes first.  q_out / k_out: the
     results' buffers (q / k: in place; default: new ones).  Returns (q_out, k_out)."""
-    dev = q.device
-    _operand(q, "rope: q", (torch.float32, torch.bfloat16), dev)
-    if q.dim() != 4:
-        raise WamError("rope: q must be [B, T, H, dh]")
+    index = _first(q, "rope: q", _REAL, 4)
     B, T, Hq, dh = q.shape
+    own = (q.dtype,)
     Hk = 0
     if k is not None:
-        _operand(k, "rope: k", (q.dtype,), dev)
-        if k.dim() != 4:
-            raise WamError("rope: k must be [B, T, H, dh]")
+        _operand(k, "rope: k", own, index)
+        if k.dim() != 4 or k.shape[0] != B or k.shape[1] != T or k.shape[3] != dh:
+            raise WamError("rope: k must be [B, T, H, dh] as q")
         Hk = k.shape[2]
-        _operand(k, "rope: k", (q.dtype,), dev, (B, T, Hk, dh))
-    _operand(pos, "rope: pos", (torch.float32,), dev, (T, 3) if pos.dim() == 2 else (B, T, 3))
-    if B > 0 and T > 1 and pos.stride(-2) != 3:
+    _operand(pos, "rope: pos", _F32, index, (T, 3) if pos.dim() == 2 else (B, T, 3))
+    if T > 1 and pos.stride(-2) != 3:
         raise WamError("rope: rows of pos must be contiguous")
-    ladder = np.ascontiguousarray(freq, np.float64)
-    if len(sections) != 3 or ladder.shape != (sum(sections),):
+    if len(sections) != 3 or len(freq) != sum(sections):
         raise WamError("rope: needs three sections and one frequency per pair")
-    for g, what in ((q_gain, "rope: q_gain"), (k_gain, "rope: k_gain")):
-        if g is not None:
-            _operand(g, what, (torch.float32,), dev, (dh,))
-    q_out = torch.empty_like(q) if q_out is None else _operand(q_out, "rope: q_out", (q.dtype,), dev, q.shape)
+    ladder = np.ascontiguousarray(freq, np.float64) if isinstance(freq, np.ndarray) else array("d", freq)
+    at = ladder.ctypes.data if isinstance(ladder, np.ndarray) else ladder.buffer_info()[0]
+    if q_gain is not None:
+        _operand(q_gain, "rope: q_gain", _F32, index, (dh,))
+    if k_gain is not None:
+        _operand(k_gain, "rope: k_gain", _F32, index, (dh,))
+    q_out = torch.empty_like(q) if q_out is None else _operand(q_out, "rope: q_out", own, index, q.shape)
     if k is not None:
-        k_out = torch.empty_like(k) if k_out is None else _operand(k_out, "rope: k_out", (q.dtype,), dev, k.shape)
-    strides = lambda t: (C.c_int64 * 3)(*t.stride()[:3]) if t is not None else (C.c_int64 * 3)()  # noqa: E731
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    a = abi.WamRopeArgs(B, T, Hq, Hk, dh, _TYPES[q.dtype], _choice(_LAYOUTS, layout, "rope: layout"),
-                        (C.c_int32 * 3)(*sections), ptr(q), ptr(k), ptr(q_out), ptr(k_out) if k is not None else None,
-                        strides(q), strides(k), strides(q_out), strides(k_out if k is not None else None), ptr(pos),
-                        pos.stride(0) if pos.dim() == 3 else 0, ladder.ctypes.data, ptr(q_gain), ptr(k_gain), eps)
-    _call(abi.lib().wam_rope, a, dev, stream, "wam_rope")
-    return q_out, k_out if k is not None else None
+        k_out = torch.empty_like(k) if k_out is None else _operand(k_out, "rope: k_out", own, index, k.shape)
+    else:
+        k_out = None
+    ks, kos = (k.stride()[:3], k_out.stride()[:3]) if k is not None else (_NO_HEADS, _NO_HEADS)
+    a = _pack(_ROPE_ARGS, "rope", B, T, Hq, Hk, dh, _TYPES[q.dtype], _choice(_LAYOUTS, layout, "rope: layout"),
+              *sections, q.data_ptr(), _ptr_or_0(k), q_out.data_ptr(), _ptr_or_0(k_out), *q.stride()[:3], *ks,
+              *q_out.stride()[:3], *kos, pos.data_ptr(), pos.stride(0) if pos.dim() == 3 else 0, at,
+              _ptr_or_0(q_gain), _ptr_or_0(k_gain), eps)
+    _call(abi.lib().wam_rope, a, index, stream, "wam_rope")
+    return q_out, k_out
+
+
+def _row_vectors(v, what, index, shape):
+    """Pointer and strides (sample, row) of float32 vectors that broadcast to shape."""
+    if v is None:
+        return 0, 0, 0
+    _operand(v, what, _F32, index)
+    try:
+        v = v.expand(shape)
+    except RuntimeError:
+        raise WamError(f"{what}: shape {tuple(v.shape)} does not broadcast to {tuple(shape)}") from None
+    s0, s1, s2 = v.stride()
+    if s2 != 1 and shape[2] > 1:
+        raise WamError(f"{what}: needs D values per row")
+    return v.data_ptr(), s0, s1
+
+
+_NO_ROWS = (0, 0)
 
 
 def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale=1.0, pre="layer", pre_gain=None,
@@ -455,62 +511,50 @@ def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale
     [D].  h_out: its buffer (h: in place; default: a new one).  u_dtype: float32,
     bfloat16 or float8_e4m3fn (default: that of u, else bfloat16).  Returns
     (h_out,), (h_out, u) or, for 8-bit blocks, (h_out, u, u_scale)."""
-    real = (torch.float32, torch.bfloat16)
-    dev = h.device
-    _operand(h, "norm_residual: h", real, dev)
-    if h.dim() != 3:
-        raise WamError("norm_residual: h must be [B, T, D]")
-    B, T, D = h.shape
+    index = _first(h, "norm_residual: h", _REAL, 3)
+    shape = h.shape
+    B, T, D = shape
     if y is not None:
-        _operand(y, "norm_residual: y", real, dev, h.shape)
-    for g, what in ((post_gain, "norm_residual: post_gain"), (pre_gain, "norm_residual: pre_gain")):
-        if g is not None:
-            _operand(g, what, (torch.float32,), dev, (D,))
-    vectors = []
-    for v, what in ((gate, "norm_residual: gate"), (scale, "norm_residual: scale"), (shift, "norm_residual: shift")):
-        if v is not None:
-            _operand(v, what, (torch.float32,), dev)
-            try:
-                v = v.expand(B, T, D)
-            except RuntimeError:
-                raise WamError(f"{what}: shape {tuple(v.shape)} does not broadcast to {(B, T, D)}") from None
-            if D > 1 and v.stride(-1) != 1:
-                raise WamError(f"{what}: needs D values per row")
-        vectors.append(v)
-    h_out = torch.empty_like(h) if h_out is None else _operand(h_out, "norm_residual: h_out", (h.dtype,), dev, h.shape)
+        _operand(y, "norm_residual: y", _REAL, index, shape)
+    if post_gain is not None:
+        _operand(post_gain, "norm_residual: post_gain", _F32, index, (D,))
+    if pre_gain is not None:
+        _operand(pre_gain, "norm_residual: pre_gain", _F32, index, (D,))
+    g, g0, g1 = _row_vectors(gate, "norm_residual: gate", index, shape)
+    c, c0, c1 = _row_vectors(scale, "norm_residual: scale", index, shape)
+    s, s0, s1 = _row_vectors(shift, "norm_residual: shift", index, shape)
+    h_out = torch.empty_like(h) if h_out is None else _operand(h_out, "norm_residual: h_out", (h.dtype,), index, shape)
     post = _choice(_NORMS, post, "norm_residual: post")
-    out = [h_out]
-    if pre is not None:
-        pre = _choice(_NORMS, pre, "norm_residual: pre")
+    if pre is None:
+        u = u_scale = None
+        kind = u_type = 0
+    else:
+        kind = _choice(_NORMS, pre, "norm_residual: pre")
         if u is None:
-            u_dtype = torch.bfloat16 if u_dtype is None else u_dtype
-            u = _new_rows((B, T, D), _choice({t: t for t in _TYPES}, u_dtype, "norm_residual: u_dtype"), dev)
+            u = _new_rows(shape, torch.bfloat16 if u_dtype is None else u_dtype, h.device, "norm_residual: u_dtype")
         else:
-            _operand(u, "norm_residual: u", tuple(_TYPES) if u_dtype is None else (u_dtype,), dev, h.shape)
-        out.append(u)
-        if u.dtype == FP8:
-            shape = (B, T, -(-D // 128))
-            u_scale = (torch.empty(shape, dtype=torch.float32, device=dev) if u_scale is None else
-                       _operand(u_scale, "norm_residual: u_scale", (torch.float32,), dev, shape))
-            out.append(u_scale)
+            _operand(u, "norm_residual: u", tuple(_TYPES) if u_dtype is None else (u_dtype,), index, shape)
+        u_type = _TYPES[u.dtype]
+        if u_type == abi.WAM_FP8:
+            blocks = (B, T, -(-D // 128))
+            u_scale = (torch.empty(blocks, dtype=torch.float32, device=h.device) if u_scale is None else
+                       _operand(u_scale, "norm_residual: u_scale", _F32, index, blocks))
         else:
             u_scale = None
-    else:
-        u = u_scale = None
-    strides = lambda t: (C.c_int64 * 2)(*t.stride()[:2]) if t is not None else (C.c_int64 * 2)()  # noqa: E731
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    a = abi.WamNormArgs(B, T, D, _TYPES[h.dtype], _TYPES[y.dtype] if y is not None else 0,
-                        _TYPES[u.dtype] if u is not None else 0, post, pre or 0, ptr(h), ptr(y), ptr(h_out), ptr(u),
-                        ptr(u_scale), strides(h), strides(y), strides(h_out), strides(u), strides(u_scale),
-                        *(ptr(v) for v in vectors), *(strides(v) for v in vectors), ptr(post_gain), ptr(pre_gain),
-                        res_scale, eps)
-    _call(abi.lib().wam_norm_residual, a, dev, stream, "wam_norm_residual")
-    return tuple(out)
+    rows = lambda t: _NO_ROWS if t is None else t.stride()[:2]  # noqa: E731
+    a = _pack(_NORM_ARGS, "norm_residual", B, T, D, _TYPES[h.dtype], 0 if y is None else _TYPES[y.dtype], u_type, post,
+              kind, h.data_ptr(), _ptr_or_0(y), h_out.data_ptr(), _ptr_or_0(u), _ptr_or_0(u_scale), *rows(h), *rows(y),
+              *rows(h_out), *rows(u), *rows(u_scale), g, c, s, g0, g1, c0, c1, s0, s1, _ptr_or_0(post_gain),
+              _ptr_or_0(pre_gain), res_scale, eps)
+    _call(abi.lib().wam_norm_residual, a, index, stream, "wam_norm_residual")
+    return (h_out,) if u is None else (h_out, u) if u_scale is None else (h_out, u, u_scale)
 
 
-def _new_rows(shape, dtype, dev):
+def _new_rows(shape, dtype, dev, what):
     """A new tensor; e4m3 rows start a multiple of 16 bytes apart, as matmul_fp8
     takes them."""
+    if dtype not in _TYPES:
+        raise WamError(f"{what}: dtype {dtype} is not supported")
     if dtype != FP8 or shape[-1] % 16 == 0:
         return torch.empty(shape, dtype=dtype, device=dev)
     padded = (*shape[:-1], -(-shape[-1] // 16) * 16)
@@ -522,20 +566,20 @@ def quantize_fp8(x, *, block_rows=1, q=None, scale=None, stream: torch.cuda.Stre
     for activations (1 x 128), 128 for weights (128 x 128).  Returns (q, scale):
     float8_e4m3fn [M, K] with rows a multiple of 16 bytes apart and float32
     [ceil(M / block_rows), ceil(K / 128)]; x stands for q * scale."""
-    dev = x.device
-    _operand(x, "quantize_fp8: x", (torch.float32, torch.bfloat16), dev)
-    if x.dim() != 2:
-        raise WamError("quantize_fp8: x must be [M, K]")
+    index = _first(x, "quantize_fp8: x", _REAL, 2)
     if block_rows not in (1, 128):
         raise WamError("quantize_fp8: block_rows must be 1 or 128")
     M, K = x.shape
-    q = _new_rows((M, K), FP8, dev) if q is None else _operand(q, "quantize_fp8: q", (FP8,), dev, x.shape)
+    if q is None:
+        q = _new_rows((M, K), FP8, x.device, "quantize_fp8: q")
+    else:
+        _operand(q, "quantize_fp8: q", _F8, index, x.shape)
     shape = (-(-M // block_rows), -(-K // 128))
-    scale = (torch.empty(shape, dtype=torch.float32, device=dev) if scale is None else
-             _operand(scale, "quantize_fp8: scale", (torch.float32,), dev, shape))
-    a = abi.WamQuantizeArgs(M, K, _TYPES[x.dtype], block_rows, x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0),
-                            scale.data_ptr(), scale.stride(0))
-    _call(abi.lib().wam_quantize_fp8, a, dev, stream, "wam_quantize_fp8")
+    scale = (torch.empty(shape, dtype=torch.float32, device=x.device) if scale is None else
+             _operand(scale, "quantize_fp8: scale", _F32, index, shape))
+    a = _pack(_QUANTIZE_ARGS, "quantize_fp8", M, K, _TYPES[x.dtype], block_rows, x.data_ptr(), x.stride(0), q.data_ptr(),
+              q.stride(0), scale.data_ptr(), scale.stride(0))
+    _call(abi.lib().wam_quantize_fp8, a, index, stream, "wam_quantize_fp8")
     return q, scale
 
 
@@ -545,28 +589,28 @@ def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_d
     (wam_matmul_fp8): a [M, K] with scales per row and 128 columns, w [N, K] with
     scales per 128 x 128, both as quantize_fp8 gives them; bias float32 [N]; gelu:
     the tanh form.  out float32 or bfloat16 (default: a new bfloat16 one)."""
-    dev = a.device
-    _operand(a, "matmul_fp8: a", (FP8,), dev)
-    _operand(w, "matmul_fp8: w", (FP8,), dev)
-    if a.dim() != 2 or w.dim() != 2 or a.shape[1] != w.shape[1]:
+    index = _first(a, "matmul_fp8: a", _F8, 2)
+    _operand(w, "matmul_fp8: w", _F8, index)
+    M, K = a.shape
+    if w.dim() != 2 or w.shape[1] != K:
         raise WamError("matmul_fp8: needs a [M, K] and w [N, K]")
-    (M, K), N = a.shape, w.shape[0]
-    _operand(a_scale, "matmul_fp8: a_scale", (torch.float32,), dev, (M, -(-K // 128)))
-    _operand(w_scale, "matmul_fp8: w_scale", (torch.float32,), dev, (-(-N // 128), -(-K // 128)))
+    N, kb = w.shape[0], -(-K // 128)
+    _operand(a_scale, "matmul_fp8: a_scale", _F32, index, (M, kb))
+    _operand(w_scale, "matmul_fp8: w_scale", _F32, index, (-(-N // 128), kb))
     if bias is not None:
-        _operand(bias, "matmul_fp8: bias", (torch.float32,), dev, (N,))
+        _operand(bias, "matmul_fp8: bias", _F32, index, (N,))
     if out is None:
-        out = torch.empty((M, N), dtype=_choice({t: t for t in (torch.float32, torch.bfloat16)},
-                                                torch.bfloat16 if out_dtype is None else out_dtype,
-                                                "matmul_fp8: out_dtype"), device=dev)
+        out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
+        if out_dtype not in _REAL:
+            raise WamError(f"matmul_fp8: out_dtype {out_dtype} is not supported")
+        out = torch.empty((M, N), dtype=out_dtype, device=a.device)
     else:
-        _operand(out, "matmul_fp8: out",
-                 (torch.float32, torch.bfloat16) if out_dtype is None else (out_dtype,), dev, (M, N))
-    args = abi.WamMatmulArgs(M, N, K, _TYPES[out.dtype], abi.WAM_ACT_GELU if gelu else abi.WAM_ACT_NONE, a.data_ptr(),
-                             a.stride(0), a_scale.data_ptr(), a_scale.stride(0), w.data_ptr(), w.stride(0),
-                             w_scale.data_ptr(), w_scale.stride(0), bias.data_ptr() if bias is not None else None,
-                             out.data_ptr(), out.stride(0))
-    _call(abi.lib().wam_matmul_fp8, args, dev, stream, "wam_matmul_fp8")
+        _operand(out, "matmul_fp8: out", _REAL if out_dtype is None else (out_dtype,), index, (M, N))
+    args = _pack(_MATMUL_ARGS, "matmul_fp8", M, N, K, _TYPES[out.dtype],
+                 abi.WAM_ACT_GELU if gelu else abi.WAM_ACT_NONE, a.data_ptr(), a.stride(0), a_scale.data_ptr(),
+                 a_scale.stride(0), w.data_ptr(), w.stride(0), w_scale.data_ptr(), w_scale.stride(0), _ptr_or_0(bias),
+                 out.data_ptr(), out.stride(0))
+    _call(abi.lib().wam_matmul_fp8, args, index, stream, "wam_matmul_fp8")
     return out
 
 

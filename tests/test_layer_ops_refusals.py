@@ -151,12 +151,28 @@ def test_frequencies():
 
 def test_binding_refuses_host_tensors():
     x = torch.zeros(1, 4, 2, 64)
-    with pytest.raises(R.WamError, match="needs a tensor on"):
+    with pytest.raises(R.WamError, match="device tensors only"):
         R.rope(x, None, torch.zeros(4, 3), (8, 12, 12), R.rope_frequencies((8, 12, 12)))
-    with pytest.raises(R.WamError, match="needs a tensor on"):
+    with pytest.raises(R.WamError, match="device tensors only"):
         R.norm_residual(torch.zeros(1, 4, 64))
-    with pytest.raises(R.WamError, match="needs a tensor on"):
+    with pytest.raises(R.WamError, match="device tensors only"):
         R.quantize_fp8(torch.zeros(4, 64))
     f8 = torch.zeros(4, 64).to(R.FP8)
-    with pytest.raises(R.WamError, match="needs a tensor on"):
+    with pytest.raises(R.WamError, match="device tensors only"):
         R.matmul_fp8(f8, torch.ones(4, 1), f8, torch.ones(1, 1))
+
+
+@pytest.mark.parametrize("packed,twin", [("_ROPE_ARGS", L.WamRopeArgs), ("_NORM_ARGS", L.WamNormArgs),
+                                         ("_QUANTIZE_ARGS", L.WamQuantizeArgs), ("_MATMUL_ARGS", L.WamMatmulArgs)])
+def test_packed_arguments_match_the_struct(packed, twin):
+    """The binding's packed bytes have every field where the C struct has it."""
+    form = getattr(R, packed)
+    flat = [n + 1 for n in range(len(form.unpack(bytes(form.size))))]
+    data = form.pack(*flat)
+    assert form.size <= C.sizeof(twin) <= form.size + 7
+    a = twin.from_buffer_copy(data + bytes(C.sizeof(twin) - form.size))
+    got = []
+    for name, _ in twin._fields_:
+        v = getattr(a, name)
+        got += list(v) if isinstance(v, C.Array) else [v]
+    assert got == flat

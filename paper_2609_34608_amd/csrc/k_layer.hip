@@ -39,6 +39,19 @@ __device__ __forceinline__ void load_n(float (&x)[N], const T* p, int n) {
     for (int i = 0; i < N; ++i) x[i] = i < n ? to_f32(p[i]) : 0.f;
   }
 }
+template <int N, typename T>
+__device__ __forceinline__ void store_n(T* p, const float (&x)[N], int n) {
+  Pack<T, N> w;
+#pragma unroll
+  for (int i = 0; i < N; ++i) w.v[i] = static_cast<T>(x[i]);
+  if (n >= N) {
+    *reinterpret_cast<Pack<T, N>*>(p) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) p[i] = w.v[i];
+  }
+}
 
 // ------------------------------------------------------------- rotary positions
 constexpr int kMaxPairs = WAM_MAX_HEAD / 2;
@@ -239,91 +252,188 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
   }
 }
 
+// ------------------------------------------------------------- 8-bit blocks
+template <int N>
+__device__ __forceinline__ uint32_t most_of(const float (&x)[N]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) most = max(most, abs_bits(x[i]));
+  return most;
+}
+
+// e4m3 of x / s into the first n bytes at q
+template <int N>
+__device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&x)[N], float s, int n) {
+  struct __attribute__((packed, aligned(1))) Bytes {
+    uint32_t v[N / 4];
+  };
+  const float r = 1.0f / s;
+  Bytes w;
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i)
+    w.v[i] = pack_e4m3(divide_by(x[4 * i], s, r), divide_by(x[4 * i + 1], s, r), divide_by(x[4 * i + 2], s, r),
+                       divide_by(x[4 * i + 3], s, r));
+  if (n >= N) {
+    *reinterpret_cast<Bytes*>(q) = w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) q[i] = (uint8_t)(w.v[i / 4] >> (8 * (i % 4)));
+  }
+}
+
 // ------------------------------------------------------------- norms around a block
-// Sum over the block (256 threads), the same in every thread.
-__device__ __forceinline__ float block_sum(float v, float* sh) {
-  v = wave_sum(v);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) sh[threadIdx.x / kWave] = v;
-  __syncthreads();
-  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
+// Sum over a wave, in every lane: sixteen lanes on the data-parallel crossbar,
+// then the four groups.
+__device__ __forceinline__ float wave_sum_fast(float v) {
+  v = lanes_sum(v, 16);
+  v += __shfl_xor(v, 16, 64);
+  return v + __shfl_xor(v, 32, 64);
 }
 
-// Mean to subtract and scale to multiply with of the row x[0 .. D) in LDS; each
-// thread has written the elements threadIdx.x + 256 i that it reads here.
-__device__ __forceinline__ void row_stats(const float* x, int D, int kind, float eps, float* sh, float& mean,
-                                          float& rs) {
-  mean = 0.f;
-  rs = 1.f;
-  if (kind == WAM_NORM_NONE) return;
-  if (kind == WAM_NORM_LAYER) {
-    float s = 0.f;
-    for (int i = threadIdx.x; i < D; i += 256) s += x[i];
-    mean = block_sum(s, sh) / (float)D;
-  }
-  float q = 0.f;
-  for (int i = threadIdx.x; i < D; i += 256) {
-    const float v = x[i] - mean;
-    q += v * v;
-  }
-  rs = rsqrt_newton(block_sum(q, sh) / (float)D + eps);
-}
+constexpr int kNormCols = 8;  // columns of a lane and chunk
 
-// One block per row, the row in LDS: any width, stride and alignment.
+// A row belongs to W waves (one up to 512 CH = 2048 columns, else four) and stays
+// in registers between its loads and stores: lane i holds the columns
+// 8 (i + 64 W c) .. + 7 of chunk c < CH = ceil(D / 512 W), 16-byte loads and
+// stores in bf16, twice that in float32, at any alignment.  Sums are over lanes,
+// and over the waves in LDS.  Sixteen lanes of a chunk are one block of 128
+// columns, which is what 8-bit results need.
+template <int CH, int W, typename TH, typename TY>
 __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
-  extern __shared__ float x[];
-  __shared__ float sh[4];
-  const int t = blockIdx.x % a.T, b = blockIdx.x / a.T;
+  __shared__ float part[2][4];
+  const int lane = threadIdx.x % kWave, wid = threadIdx.x / kWave;
+  const int64_t row = W == 1 ? (int64_t)blockIdx.x * (blockDim.x / kWave) + wid : blockIdx.x;
+  if (W == 1 && row >= (int64_t)a.B * a.T) return;
+  const int b = __builtin_amdgcn_readfirstlane((int)(row / a.T)), t = __builtin_amdgcn_readfirstlane((int)(row % a.T));
   const int D = a.D;
-  const int64_t h0 = b * a.h_stride[0] + t * a.h_stride[1];
-  float mean, rs;
-  if (a.y) {
-    const int64_t y0 = b * a.y_stride[0] + t * a.y_stride[1];
-    for (int i = threadIdx.x; i < D; i += 256) x[i] = load1(a.y, y0 + i, a.y_dtype);
-    row_stats(x, D, a.post, a.eps, sh, mean, rs);
-  }
-  const float* gate = a.gate ? a.gate + b * a.gate_stride[0] + t * a.gate_stride[1] : nullptr;
-  for (int i = threadIdx.x; i < D; i += 256) {
-    float v = a.res_scale * load1(a.h, h0 + i, a.h_dtype);
-    if (a.y) {
-      float w = (x[i] - mean) * rs;
-      if (a.post_gain) w *= a.post_gain[i];
-      v += gate ? gate[i] * w : w;
+  auto col = [&](int c) { return kNormCols * ((W == 1 ? lane : (int)threadIdx.x) + kWave * W * c); };
+  // columns of chunk c that the row has (all eight but in the last chunk)
+  auto have = [&](int c) { return c < CH - 1 ? kNormCols : D - col(c); };
+  int turn = 0;
+  auto row_sum = [&](float v) __attribute__((always_inline)) {
+    v = wave_sum_fast(v);
+    if constexpr (W > 1) {
+      if (lane == 0) part[turn][wid] = v;
+      __syncthreads();
+      v = (part[turn][0] + part[turn][1]) + (part[turn][2] + part[turn][3]);
+      turn ^= 1;
     }
-    x[i] = v;
+    return v;
+  };
+  // x <- (x - mean) / spread, as kind says
+  auto standardise = [&](float (&x)[CH][kNormCols], int kind) __attribute__((always_inline)) {
+    if (kind == WAM_NORM_NONE) return;
+    if (kind == WAM_NORM_LAYER) {
+      float s = 0.f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < kNormCols; ++j) s += x[c][j];  // zero past the row
+      const float mean = row_sum(s) / (float)D;
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int j = 0; j < kNormCols; ++j) x[c][j] = c < CH - 1 || j < have(c) ? x[c][j] - mean : 0.f;
+    }
+    float q = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < kNormCols; ++j) q += x[c][j] * x[c][j];
+    const float rs = rsqrt_newton(row_sum(q) / (float)D + a.eps);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < kNormCols; ++j) x[c][j] *= rs;
+  };
+
+  float x[CH][kNormCols], y[CH][kNormCols];
+  const TH* h = static_cast<const TH*>(a.h) + b * a.h_stride[0] + t * a.h_stride[1];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) load_n(x[c], h + col(c), have(c));
+  if (a.y) {
+    const TY* yr = static_cast<const TY*>(a.y) + b * a.y_stride[0] + t * a.y_stride[1];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load_n(y[c], yr + col(c), have(c));
+    standardise(y, a.post);
+    auto times = [&](const float* f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        float v[kNormCols];
+        load_n(v, f + col(c), have(c));
+#pragma unroll
+        for (int j = 0; j < kNormCols; ++j) y[c][j] *= v[j];
+      }
+    };
+    if (a.post_gain) times(a.post_gain);
+    if (a.gate) times(a.gate + b * a.gate_stride[0] + t * a.gate_stride[1]);
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < kNormCols; ++j) x[c][j] = a.res_scale * x[c][j] + y[c][j];
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < kNormCols; ++j) x[c][j] *= a.res_scale;
   }
   if (a.h_out) {
-    const int64_t o0 = b * a.h_out_stride[0] + t * a.h_out_stride[1];
-    for (int i = threadIdx.x; i < D; i += 256) store1(a.h_out, o0 + i, a.h_dtype, x[i]);
+    TH* o = static_cast<TH*>(a.h_out) + b * a.h_out_stride[0] + t * a.h_out_stride[1];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store_n(o + col(c), x[c], have(c));
   }
   if (!a.u) return;
-  row_stats(x, D, a.pre, a.eps, sh, mean, rs);
-  const float* scale = a.scale ? a.scale + b * a.scale_stride[0] + t * a.scale_stride[1] : nullptr;
-  const float* shift = a.shift ? a.shift + b * a.shift_stride[0] + t * a.shift_stride[1] : nullptr;
-  const int64_t u0 = b * a.u_stride[0] + t * a.u_stride[1];
-  auto value = [&](int i) {
-    float v = (x[i] - mean) * rs;
-    if (a.pre_gain) v *= a.pre_gain[i];
-    if (scale) v *= 1.0f + scale[i];
-    return shift ? v + shift[i] : v;
+  standardise(x, a.pre);
+  auto each = [&](const float* f, auto OP) __attribute__((always_inline)) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      float v[kNormCols];
+      load_n(v, f + col(c), have(c));
+#pragma unroll
+      for (int j = 0; j < kNormCols; ++j) x[c][j] = OP(x[c][j], v[j]);
+    }
   };
-  if (a.u_dtype != WAM_FP8) {
-    for (int i = threadIdx.x; i < D; i += 256) store1(a.u, u0 + i, a.u_dtype, value(i));
-    return;
+  if (a.pre_gain) each(a.pre_gain, [](float p, float q) { return p * q; });
+  if (a.scale) each(a.scale + b * a.scale_stride[0] + t * a.scale_stride[1], [](float p, float q) { return p * (1.0f + q); });
+  if (a.shift) each(a.shift + b * a.shift_stride[0] + t * a.shift_stride[1], [](float p, float q) { return p + q; });
+  const int64_t u0 = b * a.u_stride[0] + t * a.u_stride[1];
+  if (a.u_dtype == WAM_BF16) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store_n(static_cast<bf16*>(a.u) + u0 + col(c), x[c], have(c));
+  } else if (a.u_dtype == WAM_FP32) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store_n(static_cast<float*>(a.u) + u0 + col(c), x[c], have(c));
+  } else {
+    float* us = a.u_scale + b * a.u_scale_stride[0] + t * a.u_scale_stride[1];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int n = have(c);
+      const float s = block_scale(group_max<16>(most_of(x[c])));
+      store_e4m3(static_cast<uint8_t*>(a.u) + u0 + col(c), x[c], s, n);
+      if (lane % 16 == 0 && n > 0) us[col(c) / kScaleBlock] = s;
+    }
   }
-  // wave w takes the blocks w, w + 4, ..., lane l the columns l and l + 64 of each
-  __syncthreads();
-  float* us = a.u_scale + b * a.u_scale_stride[0] + t * a.u_scale_stride[1];
-  uint8_t* u = static_cast<uint8_t*>(a.u) + u0;
-  const int lane = threadIdx.x % kWave;
-  for (int blk = threadIdx.x / kWave; blk * kScaleBlock < D; blk += 4) {
-    const int i = blk * kScaleBlock + lane, j = i + kWave;
-    const float v = i < D ? value(i) : 0.f, w = j < D ? value(j) : 0.f;
-    const float s = block_scale(wave_max(max(abs_bits(v), abs_bits(w))));
-    if (i < D) u[i] = to_e4m3(v / s);
-    if (j < D) u[j] = to_e4m3(w / s);
-    if (lane == 0) us[blk] = s;
+}
+
+template <int W, typename TH, typename TY>
+hipError_t launch_norm_rows(const wam_norm_args& a, hipStream_t s) {
+  const int64_t rows = (int64_t)a.B * a.T;
+  // one wave per row: blocks of four rows, or of one while the chip has room
+  const int block = W > 1 || rows >= 1024 ? 256 : kWave;
+  const dim3 grid((unsigned)(W > 1 ? rows : (rows + block / kWave - 1) / (block / kWave)));
+  switch ((a.D + kNormCols * kWave * W - 1) / (kNormCols * kWave * W)) {
+    case 1: launch_k(norm_residual_kernel<1, W, TH, TY>, grid, block, 0, s, a); break;
+    case 2: launch_k(norm_residual_kernel<2, W, TH, TY>, grid, block, 0, s, a); break;
+    case 3: launch_k(norm_residual_kernel<3, W, TH, TY>, grid, block, 0, s, a); break;
+    case 4: launch_k(norm_residual_kernel<4, W, TH, TY>, grid, block, 0, s, a); break;
+    default: return hipErrorInvalidValue;
   }
+  return hipGetLastError();
+}
+template <typename TH, typename TY>
+hipError_t launch_norm(const wam_norm_args& a, hipStream_t s) {
+  return a.D <= 4 * kNormCols * kWave ? launch_norm_rows<1, TH, TY>(a, s) : launch_norm_rows<4, TH, TY>(a, s);
 }
 
 // ------------------------------------------------------------- quantisation
@@ -331,33 +441,6 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
 // store), eight neighbouring threads a scale block of the row, whose maximum
 // they share without LDS; the row is read once, from registers.
 constexpr int kQuantCols = 16, kQuantGroup = kScaleBlock / kQuantCols;
-
-__device__ __forceinline__ uint32_t most_of(const float (&x)[kQuantCols]) {
-  uint32_t most = 0;
-#pragma unroll
-  for (int i = 0; i < kQuantCols; ++i) most = max(most, abs_bits(x[i]));
-  return most;
-}
-
-// e4m3 of x / s into the first n bytes at q
-__device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&x)[kQuantCols], float s, int n) {
-  const float r = 1.0f / s;
-  Pack<uint32_t, kQuantCols / 4> w;
-#pragma unroll
-  for (int i = 0; i < kQuantCols / 4; ++i)
-    w.v[i] = pack_e4m3(divide_by(x[4 * i], s, r), divide_by(x[4 * i + 1], s, r), divide_by(x[4 * i + 2], s, r),
-                       divide_by(x[4 * i + 3], s, r));
-  if (n >= kQuantCols) {
-    struct __attribute__((packed, aligned(1))) Bytes {
-      Pack<uint32_t, kQuantCols / 4> w;
-    };
-    *reinterpret_cast<Bytes*>(q) = Bytes{w};
-  } else {
-#pragma unroll
-    for (int i = 0; i < kQuantCols; ++i)
-      if (i < n) q[i] = (uint8_t)(w.v[i / 4] >> (8 * (i % 4)));
-  }
-}
 
 // blocks of 1 x 128
 template <typename T>
@@ -605,9 +688,11 @@ int wam_norm_residual(const wam_norm_args* a, void* hip_stream) {
     return noalloc_fail(WAM_E_ARG, "wam_norm_residual: u must not be h or h_out");
   if (a->y && (a->h_out == a->y || (a->u == a->y && (a->u_dtype != a->y_dtype || !same(a->u_stride, a->y_stride, 2)))))
     return noalloc_fail(WAM_E_ARG, "wam_norm_residual: h_out must not be y, and u only with its type and strides");
-  launch_k(norm_residual_kernel, dim3((unsigned)((int64_t)a->B * a->T)), 256, (size_t)a->D * 4,
-           static_cast<hipStream_t>(hip_stream), *a);
-  if (hipGetLastError() != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_norm_residual: kernel launch failed");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const bool yf = a->y && a->y_dtype == WAM_FP32;
+  const hipError_t e = a->h_dtype == WAM_FP32 ? (yf ? launch_norm<float, float>(*a, s) : launch_norm<float, bf16>(*a, s))
+                                              : (yf ? launch_norm<bf16, float>(*a, s) : launch_norm<bf16, bf16>(*a, s));
+  if (e != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_norm_residual: kernel launch failed");
   return WAM_OK;
 }
 

@@ -36,6 +36,23 @@ namespace gemm {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
+// A wave's weight rows are dealt to its 16-row MFMA tiles so that the tiles 2 q and
+// 2 q + 1 together give a lane eight consecutive columns (one 16-byte store of
+// bf16), and the four lane groups 32: the row of tile j, index i (0..15), and the
+// first column of tile j in lane group g.  Tiles that have no pair stay in order.
+template <int TN>
+__host__ __device__ constexpr int tile_row(int j, int i) {
+  return TN % 2 ? j * 16 + i : (j / 2) * 32 + (i / 4) * 8 + (j % 2) * 4 + i % 4;
+}
+template <int TN>
+__host__ __device__ constexpr int tile_col(int j, int g) { return tile_row<TN>(j, 4 * g); }
+// XOR swizzle of a weight row's chunks: index i of every tile gets i & 7, as an
+// activation row does
+template <int TN>
+__host__ __device__ constexpr int weight_swizzle(int row) {
+  return TN % 2 ? row & 7 : (row & 3) | ((row >> 3) & 1) << 2;
+}
+
 struct Fp8Operands {
   const uint8_t *a, *w;
   const float *sa, *sw;
@@ -45,36 +62,9 @@ struct Fp8Operands {
 
 struct Fp8Out {
   const float* bias;  // or null
-  void* out;
+  void* out;          // bf16, or float32 of an EXACT product
   int64_t ld;
-  int bf16_out, gelu;
-  int vec;  // rows and base allow stores of four elements
 };
-
-__device__ __forceinline__ void store_out(const Fp8Out& o, int m, int n, int N, f32x4 v) {
-  if (o.gelu) v = gelu4(v);
-  const int64_t off = (int64_t)m * o.ld + n;
-  if (o.vec && n + 3 < N) {
-    if (o.bf16_out) store4(static_cast<bf16*>(o.out) + off, v);
-    else store4(static_cast<float*>(o.out) + off, v);
-    return;
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r)
-    if (n + r < N) {
-      if (o.bf16_out) static_cast<bf16*>(o.out)[off + r] = static_cast<bf16>(v[r]);
-      else static_cast<float*>(o.out)[off + r] = v[r];
-    }
-}
-
-__device__ __forceinline__ f32x4 bias4(const float* bias, int n, int N) {
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-  if (bias)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (n + r < N) v[r] = bias[n + r];
-  return v;
-}
 
 // bf16 values of the bytes 8 t .. 8 t + 7 of a lane's operand
 __device__ __forceinline__ bf16x8 to_bf16(const i32x8& v, int t) {
@@ -89,7 +79,8 @@ __device__ __forceinline__ bf16x8 to_bf16(const i32x8& v, int t) {
   return r;
 }
 
-template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT>
+// WIDE: rows further apart than 32-bit offsets inside a tile reach.
+template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool GELU, bool WIDE>
 __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, Fp8Out o) {
   constexpr int BK = kScaleBlock;              // bytes of a row per stage
   constexpr int NW = WGM * WGN;
@@ -101,50 +92,70 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
   static_assert(IPW * NW * 8 == ROWS, "stage rows / wave mismatch");
   static_assert(128 % WN == 0 && BN % WN == 0, "a wave's columns share a weight scale");
   static_assert(ST >= 2 && (ST - 2) * (IPW + SPW) < 64, "stage count");
+  typedef typename std::conditional<WIDE, int64_t, uint32_t>::type offset;
 
-  __shared__ __attribute__((aligned(1024))) uint8_t sm[ST][ROWS * BK];
-  __shared__ __attribute__((aligned(256))) float sc[ST][SPW * NW * 64];
+  // a stage: operand rows, then their scales.  One object: with the scales in a
+  // second one the compiler takes every LDS read to depend on the loads in flight
+  // and waits for all of them, which serialises loads and MFMAs.
+  constexpr int SCALES = ROWS * BK;
+  constexpr int STAGE = SCALES + SPW * NW * 64 * 4;
+  __shared__ __attribute__((aligned(1024))) uint8_t sm[ST][STAGE];
 
   const int tiles_m = (p.M + BM - 1) / BM, tiles_n = (p.N + BN - 1) / BN;
   int tm, tn;
   tile_coords(blockIdx.x, gridDim.x, tiles_m, tiles_n, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
-  const int tid = threadIdx.x, lane = tid % 64, wid = tid / 64;
+  const int tid = threadIdx.x, lane = tid % 64, wid = __builtin_amdgcn_readfirstlane(tid / 64);
   const int wm = wid / WGN, wn = wid % WGN;
   const int nk = (p.K + BK - 1) / BK;
-  const int last = (p.K - 1) / 16 * 16;  // first byte of a row's last 16-byte chunk
+  const uint32_t last = (p.K - 1) / 16 * 16;  // first byte of a row's last 16-byte chunk
 
   // Load j of this wave fills LDS rows 8 (wid + NW j) .. + 7 of the stage, lane l
-  // the chunk l % 8 of row l / 8, i.e. global chunk (l % 8) ^ swizzle.  Rows past
-  // M or N read the last one (never stored); chunks past K read the row's last
-  // one and are cleared in LDS before use.
-  const uint8_t* src[IPW];
-  int col[IPW];
+  // the chunk l % 8 of row l / 8, i.e. global chunk (l % 8) ^ swizzle (the same
+  // for every j).  Rows past M or N read the last one (never stored); chunks past
+  // K read the row's last one and are cleared in LDS before use.
+  const uint8_t* abase = p.a + (int64_t)m0 * p.lda;
+  const uint8_t* wbase = p.w + (int64_t)n0 * p.ldw;
+  const uint32_t col = ((lane % 8) ^ chunk_swizzle(lane / 8)) * 16;
+  auto wcol = [&](int j) {  // of a load of weight rows: the swizzle's bits from the lane and from the load
+    return (uint32_t)((lane % 8) ^ weight_swizzle<TN>(8 * (wid + NW * j) - BM + lane / 8)) * 16;
+  };
+  offset roff[IPW];
+  const float* ssrc[SPW];
 #pragma unroll
   for (int j = 0; j < IPW; ++j) {
     const int row = 8 * (wid + NW * j) + lane / 8;
-    col[j] = ((lane % 8) ^ chunk_swizzle(row)) * 16;
-    src[j] = row < BM ? p.a + (int64_t)min(m0 + row, p.M - 1) * p.lda
-                      : p.w + (int64_t)min(n0 + row - BM, p.N - 1) * p.ldw;
+    roff[j] = 8 * (wid + NW * j) < BM ? (offset)min(row, p.M - 1 - m0) * (offset)p.lda
+                                      : (offset)min(row - BM, p.N - 1 - n0) * (offset)p.ldw;
   }
-  const float* ssrc[SPW];
 #pragma unroll
   for (int j = 0; j < SPW; ++j) {
     const int row = min(64 * (wid + NW * j) + lane, ROWS - 1);
     ssrc[j] = row < BM ? p.sa + (int64_t)min(m0 + row, p.M - 1) * p.ldsa
                        : p.sw + (int64_t)(min(n0 + row - BM, p.N - 1) / kScaleBlock) * p.ldsw;
   }
-  auto issue = [&](auto S, int kt) __attribute__((always_inline)) {
+  // loads lo .. hi - 1 of this wave's LPS for stage kt, the scales' last
+  constexpr int LPS = IPW + SPW;
+  auto issue = [&](auto S, int kt, int lo, int hi) __attribute__((always_inline)) {
     constexpr int s = decltype(S)::value;
+    const uint32_t at = min(kt * BK + col, last);
 #pragma unroll
-    for (int j = 0; j < IPW; ++j)
-      __builtin_amdgcn_global_load_lds((const global_void*)(src[j] + min(kt * BK + col[j], last)),
+    for (int j = 0; j < IPW; ++j) {
+      if (j < lo || j >= hi) continue;
+      const bool act = 8 * (wid + NW * j) < BM;
+      const uint32_t c = act ? at : min(kt * BK + wcol(j), last);
+      __builtin_amdgcn_global_load_lds((const global_void*)((act ? abase : wbase) + (offset)(roff[j] + c)),
                                        (lds_void*)(&sm[s][(wid + NW * j) * 8 * BK]), 16, 0, 0);
+    }
 #pragma unroll
     for (int j = 0; j < SPW; ++j)
-      __builtin_amdgcn_global_load_lds((const global_void*)(ssrc[j] + kt), (lds_void*)(&sc[s][(wid + NW * j) * 64]), 4,
-                                       0, 0);
+      if (lo <= IPW + j && IPW + j < hi)
+        __builtin_amdgcn_global_load_lds((const global_void*)(ssrc[j] + kt),
+                                         (lds_void*)(&sm[s][SCALES + (wid + NW * j) * 64 * 4]), 4, 0, 0);
   };
+
+  // loads per row tile, spread over about 5/8 of them
+  constexpr int LPT = (8 * LPS + 5 * TM - 1) / (5 * TM);
 
   f32x4 acc[TN][TM];
 #pragma unroll
@@ -154,44 +165,68 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
 
   const int lr = lane % 16, lg = lane / 16;
   const int ch0 = (lg ^ chunk_swizzle(lr)) * 16, ch1 = ((lg + 4) ^ chunk_swizzle(lr)) * 16;
-  const int arow = (wm * WM + lr) * BK, wrow = (BM + wn * WN + lr) * BK;
+  const int arow = (wm * WM + lr) * BK, wrow = (BM + wn * WN + tile_row<TN>(0, lr)) * BK;
   auto operand = [&](const uint8_t* row) __attribute__((always_inline)) {
     const i32x4 x = *reinterpret_cast<const i32x4*>(row + ch0), y = *reinterpret_cast<const i32x4*>(row + ch1);
     return i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
   };
-  auto compute = [&](auto S) __attribute__((always_inline)) {
+  // The multiply-adds of row tile i run behind the MFMAs of row tile i + 1, one
+  // MFMA and four multiply-adds in turn, so that neither unit waits for the other.
+  // load(i) requests part of a later stage before the MFMAs of row tile i.
+  auto compute = [&](auto S, auto load) __attribute__((always_inline)) {
     constexpr int s = decltype(S)::value;
-    const float sw = sc[s][BM + wn * WN];
+    const float* sc = reinterpret_cast<const float*>(&sm[s][SCALES]);
+    const float sw = sc[BM + wn * WN];
+    float f[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) f[i] = sc[wm * WM + i * 16 + lr] * sw;
     i32x8 wf[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) wf[j] = operand(&sm[s][wrow + j * 16 * BK]);
-    bf16x8 wb[EXACT ? TN : 1][4];
+    for (int j = 0; j < TN; ++j) wf[j] = operand(&sm[s][wrow + tile_row<TN>(j, 0) * BK]);
     if constexpr (EXACT) {
+      bf16x8 wb[TN][4];
 #pragma unroll
       for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int t = 0; t < 4; ++t) wb[j][t] = to_bf16(wf[j], t);
-    }
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const i32x8 af = operand(&sm[s][arow + i * 16 * BK]);
-      const float f = sc[s][wm * WM + i * 16 + lr] * sw;
-      bf16x8 ab[4];
-      if constexpr (EXACT) {
+      for (int i = 0; i < TM; ++i) {
+        load(i);
+        const i32x8 af = operand(&sm[s][arow + i * 16 * BK]);
+        bf16x8 ab[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) ab[t] = to_bf16(af, t);
-      }
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (EXACT) {
+        for (int j = 0; j < TN; ++j) {
+          f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int t = 0; t < 4; ++t) v = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[j][t], ab[t], v, 0, 0, 0);
-        } else {
-          v = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[j], af, v, 0, 0, 0, 0, 0, 0);
-        }
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(v[r], f, acc[j][i][r]);
+          for (int r = 0; r < 4; ++r) acc[j][i][r] = fmaf(v[r], f[i], acc[j][i][r]);
+        }
+      }
+    } else {
+      const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+      f32x4 v[2][TN];
+      i32x8 af[2];
+      af[0] = operand(&sm[s][arow]);
+#pragma unroll
+      for (int i = 0; i <= TM; ++i) {
+        if (i + 1 < TM) af[(i + 1) & 1] = operand(&sm[s][arow + (i + 1) * 16 * BK]);
+        if (i < TM) load(i);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          if (i < TM)
+            v[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf[j], af[i & 1], z, 0, 0, 0, 0, 0, 0);
+          if (i > 0)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[j][i - 1][r] = fmaf(v[(i - 1) & 1][j][r], f[i - 1], acc[j][i - 1][r]);
+          if (i > 0 && i < TM) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);  // one MFMA
+            __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);  // four VALU
+            if (j == 0) __builtin_amdgcn_sched_group_barrier(0x10, LPT, 0);  // the loads
+          }
+        }
       }
     }
   };
@@ -201,7 +236,8 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
     constexpr int s = decltype(S)::value;
     const int used = p.K - (nk - 1) * BK;
     for (int c = tid; c < ROWS * 8; c += NW * 64) {
-      const int row = c / 8, at = ((c % 8) ^ chunk_swizzle(row)) * 16;  // first byte of K in this chunk
+      const int row = c / 8;
+      const int at = ((c % 8) ^ (row < BM ? chunk_swizzle(row) : weight_swizzle<TN>(row - BM))) * 16;  // first of K
       if (at + 16 <= used) continue;
       i32x4* q = reinterpret_cast<i32x4*>(&sm[s][row * BK + (c % 8) * 16]);
       i32x4 v = *q;
@@ -214,39 +250,91 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
     }
     __syncthreads();
   };
-  // one K step on stage slot J, as in gemm_tile.h
-  auto step = [&](auto J, int kt) __attribute__((always_inline)) {
+  // One K step on stage slot J: this wave's loads of stage kt have landed (the ST - 2
+  // newer stages may still be in flight) and its LDS reads are done; after the
+  // barrier everyone's are, and the slot read in the previous step is free for
+  // stage kt + ST - 1.  Its loads go out a few at a time between the MFMAs of the
+  // first row tiles: all at once they fill the load path and every wave waits for
+  // its turn before its first MFMA (M = 10176, N = 1536, K = 6144: 100 -> 90 us).
+  // Waves that have passed the barrier go before those that have not (90 -> 87 us).
+  // Past the last stage the loads repeat it into slots nobody reads again.
+  auto step = [&](auto J, int kt, bool tail) __attribute__((always_inline)) {
     constexpr int j = decltype(J)::value;
-    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((ST - 2) * (IPW + SPW)));
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((ST - 2) * LPS));
     compiler_fence();
     __builtin_amdgcn_s_barrier();
     compiler_fence();
-    issue(std::integral_constant<int, (j + ST - 1) % ST>{}, min(kt + ST - 1, nk - 1));
-    __builtin_amdgcn_sched_barrier(0);
-    if (kt == nk - 1 && p.K % BK) clear_tail(J);
-    compute(J);
+    __builtin_amdgcn_s_setprio(1);
+    if (tail) clear_tail(J);
+    compute(J, [&](int i) __attribute__((always_inline)) {
+      issue(std::integral_constant<int, (j + ST - 1) % ST>{}, min(kt + ST - 1, nk - 1), i * LPT,
+            i < TM - 1 ? (i + 1) * LPT : LPS);
+    });
   };
 
-  static_for<ST - 1>([&](auto P) __attribute__((always_inline)) { issue(P, min((int)decltype(P)::value, nk - 1)); });
-  const int nfull = nk / ST * ST;
+  static_for<ST - 1>([&](auto P) __attribute__((always_inline)) { issue(P, min((int)decltype(P)::value, nk - 1), 0, LPS); });
+  // whole rounds of the slots, then what is left; a ragged last stage is among the
+  // latter, out of the main loop
+  const bool ragged = p.K % BK != 0;
+  const int nfull = (nk - ragged) / ST * ST;
   for (int kt0 = 0; kt0 < nfull; kt0 += ST)
-    static_for<ST>([&](auto J) __attribute__((always_inline)) { step(J, kt0 + decltype(J)::value); });
-  static_for<ST - 1>([&](auto J) __attribute__((always_inline)) {
+    static_for<ST>([&](auto J) __attribute__((always_inline)) { step(J, kt0 + decltype(J)::value, false); });
+  static_for<ST>([&](auto J) __attribute__((always_inline)) {
     const int kt = nfull + decltype(J)::value;
-    if (kt < nk) step(J, kt);
+    if (kt < nk) step(J, kt, ragged && kt == nk - 1);
   });
   // no load may still be writing this block's LDS when the block retires
   __builtin_amdgcn_s_waitcnt(0);
 
+  // G tiles side by side hold W consecutive columns of a lane.  Global memory takes
+  // wide stores at any address, so rows of any stride do; only columns that N cuts
+  // off go one by one, in a pass of their own that most blocks skip.
+  constexpr int G = TN % 2 ? 1 : 2, W = 4 * G;
+  typedef typename std::conditional<EXACT, float, bf16>::type T;
+  struct __attribute__((packed, aligned(sizeof(T)))) Row {
+    T v[W];
+  };
+  float bias[TN / G][W];
 #pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int n = n0 + wn * WN + j * 16 + lg * 4;
-    if (n >= p.N) continue;
-    const f32x4 bias = bias4(o.bias, n, p.N);
+  for (int j = 0; j < TN / G; ++j)
+#pragma unroll
+    for (int r = 0; r < W; ++r) bias[j][r] = 0.f;
+  if (o.bias)
+#pragma unroll
+    for (int j = 0; j < TN / G; ++j)
+#pragma unroll
+      for (int r = 0; r < W; ++r) bias[j][r] = o.bias[min(n0 + wn * WN + tile_col<TN>(j * G, lg) + r, p.N - 1)];
+  auto value = [&](int j, int i, int r) __attribute__((always_inline)) {
+    const float v = acc[j * G + r / 4][i][r % 4] + bias[j][r];
+    return static_cast<T>(GELU ? gelu_tanh_f(v) : v);
+  };
+  T* out = static_cast<T*>(o.out);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = m0 + wm * WM + i * 16 + lr;
+    if (m >= p.M) continue;
+#pragma unroll
+    for (int j = 0; j < TN / G; ++j) {
+      const int n = n0 + wn * WN + tile_col<TN>(j * G, lg);
+      Row x;
+#pragma unroll
+      for (int r = 0; r < W; ++r) x.v[r] = value(j, i, r);
+      if (n + W <= p.N) *reinterpret_cast<Row*>(out + (int64_t)m * o.ld + n) = x;
+    }
+  }
+  if (p.N % W && n0 + BN > p.N) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int m = m0 + wm * WM + i * 16 + lr;
-      if (m < p.M) store_out(o, m, n, p.N, acc[j][i] + bias);
+#pragma unroll
+      for (int j = 0; j < TN / G; ++j) {
+        const int n = n0 + wn * WN + tile_col<TN>(j * G, lg);
+        if (m >= p.M || n >= p.N || n + W <= p.N) continue;
+#pragma unroll
+        for (int r = 0; r < W; ++r)
+          if (n + r < p.N) out[(int64_t)m * o.ld + n + r] = value(j, i, r);
+      }
     }
   }
 }

@@ -1,19 +1,54 @@
 // Product of e4m3 matrices with block scales: checks and dispatch of
 // wam_matmul_fp8 for the kernels of gemm_fp8.h.
+#include <utility>
+
 #include "gemm_fp8.h"
 
 namespace wam {
 
 namespace {
 
-template <int BM, int BN, int WGM, int WGN, int ST>
-hipError_t launch_fp8(const gemm::Fp8Operands& p, const gemm::Fp8Out& o, hipStream_t s) {
+using gemm::Fp8Operands;
+using gemm::Fp8Out;
+
+template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool WIDE>
+hipError_t launch_tile(const Fp8Operands& p, const Fp8Out& o, bool gelu, hipStream_t s) {
   const int64_t blocks = (int64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN);
   if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks);
-  if (o.bf16_out) launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, false>, grid, WGM * WGN * 64, 0, s, p, o);
-  else launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, true>, grid, WGM * WGN * 64, 0, s, p, o);
+  const dim3 grid((unsigned)blocks), block(WGM * WGN * 64);
+  if (gelu) launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, EXACT, true, WIDE>, grid, block, 0, s, p, o);
+  else launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, EXACT, false, WIDE>, grid, block, 0, s, p, o);
   return hipGetLastError();
+}
+
+template <bool EXACT, int C>
+hipError_t launch_cfg(const Fp8Operands& p, const Fp8Out& o, bool gelu, hipStream_t s) {
+  constexpr TileCfg t = EXACT ? kFp8ExactCfgs[EXACT ? C : 0] : kFp8Cfgs[C];
+  return launch_tile<t.bm, t.bn, t.wgm, t.wgn, t.st, EXACT, false>(p, o, gelu, s);
+}
+
+template <bool EXACT, int... C>
+hipError_t launch_any(const Fp8Operands& p, const Fp8Out& o, int cfg, bool gelu, hipStream_t s,
+                      std::integer_sequence<int, C...>) {
+  hipError_t e = hipErrorInvalidValue;
+  ((cfg == C ? (void)(e = launch_cfg<EXACT, C>(p, o, gelu, s)) : (void)0), ...);
+  return e;
+}
+
+constexpr int kCfgCount = sizeof(kFp8Cfgs) / sizeof(kFp8Cfgs[0]);
+constexpr int kExactCfgCount = sizeof(kFp8ExactCfgs) / sizeof(kFp8ExactCfgs[0]);
+
+hipError_t launch_fp8(const Fp8Operands& p, const Fp8Out& o, bool exact, bool gelu, hipStream_t s) {
+  // offsets of up to 256 rows inside a tile in 32 bits, else rows by 64-bit offsets
+  constexpr int64_t kNear = (int64_t)1 << 23;
+  if (p.lda > kNear || p.ldw > kNear || p.K > kNear)
+    return exact ? launch_tile<64, 64, 2, 2, 2, true, true>(p, o, gelu, s)
+                 : launch_tile<64, 64, 2, 2, 2, false, true>(p, o, gelu, s);
+  if (exact)
+    return launch_any<true>(p, o, plan_fp8(kFp8ExactCfgs, p.M, p.N, p.K), gelu, s,
+                            std::make_integer_sequence<int, kExactCfgCount>{});
+  return launch_any<false>(p, o, plan_fp8(kFp8Cfgs, p.M, p.N, p.K), gelu, s,
+                           std::make_integer_sequence<int, kCfgCount>{});
 }
 
 bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)n == 0; }
@@ -52,9 +87,9 @@ extern "C" int wam_matmul_fp8(const wam_matmul_args* a, void* hip_stream) {
   if (a->out == a->a || a->out == a->w) return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: out must not be a or w");
   gemm::Fp8Operands p{static_cast<const uint8_t*>(a->a), static_cast<const uint8_t*>(a->w), a->a_scale, a->w_scale,
                       a->a_stride, a->w_stride, a->a_scale_stride, a->w_scale_stride, a->M, a->N, a->K};
-  gemm::Fp8Out o{a->bias, a->out, a->out_stride, a->out_dtype == WAM_BF16, a->act == WAM_ACT_GELU,
-                 aligned_to(a->out, 4 * esize) && a->out_stride % 4 == 0};
-  if (launch_fp8<128, 128, 2, 2, 2>(p, o, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+  gemm::Fp8Out o{a->bias, a->out, a->out_stride};
+  if (launch_fp8(p, o, a->out_dtype == WAM_FP32, a->act == WAM_ACT_GELU, static_cast<hipStream_t>(hip_stream)) !=
+      hipSuccess)
     return noalloc_fail(WAM_E_HIP, "wam_matmul_fp8: kernel launch failed");
   return WAM_OK;
 }

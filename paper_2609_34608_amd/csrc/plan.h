@@ -83,6 +83,43 @@ int plan_gemm(const TileCfg (&cfgs)[NC], int M, int N, int K, bool qkv) {
   return best;
 }
 
+// ---------------------------------------------------------------- 8-bit products
+// Tiles of gemm_fp8.h, the cost of a tile as above with a stage of 128 of K (bk
+// in bytes; per is per stage).  Least-squares fits to 187 sizes (16 to 10176 rows, N
+// and K 512 to 6144), standard deviation 8-13%; the choice is 2.6% slower than
+// the fastest of 21 configurations on average.  bf16 results run on the 8-bit
+// matrix instruction, float32 ones on bf16 operands converted from the stages,
+// whose registers leave no room for 256-column tiles (1.1% off the fastest).
+constexpr TileCfg kFp8Cfgs[] = {
+    {256, 256, 2, 4, 2, 128, 1, {1.27f}, {6.01f}},
+    {192, 256, 2, 4, 2, 128, 1, {1.08f}, {5.01f}},
+    {128, 256, 2, 4, 3, 128, 1, {0.77f}, {4.60f}},
+    {160, 128, 2, 2, 2, 128, 2, {0.63f, 1.14f}, {3.97f, 4.92f}},
+    {64, 128, 2, 2, 2, 128, 3, {0.42f, 0.59f, 0.95f}, {2.86f, 3.44f, 2.65f}},
+    {96, 64, 2, 2, 3, 128, 2, {0.30f, 0.54f}, {2.90f, 2.11f}},
+    {64, 64, 2, 2, 3, 128, 3, {0.24f, 0.38f, 0.62f}, {2.83f, 3.11f, 1.54f}},
+    {32, 32, 2, 2, 4, 128, 4, {0.15f, 0.18f, 0.26f, 0.36f}, {2.56f, 2.70f, 3.09f, 1.26f}},
+};
+constexpr TileCfg kFp8ExactCfgs[] = {
+    {160, 128, 2, 2, 2, 128, 2, {1.12f, 1.88f}, {5.02f, 7.14f}},
+    {128, 128, 2, 2, 2, 128, 2, {0.98f, 1.55f}, {4.66f, 6.36f}},
+    {96, 128, 2, 2, 2, 128, 2, {0.76f, 1.21f}, {3.89f, 5.07f}},
+    {96, 64, 2, 2, 3, 128, 2, {0.53f, 0.79f}, {3.12f, 3.16f}},
+    {64, 64, 2, 2, 2, 128, 4, {0.41f, 0.60f, 0.84f, 1.08f}, {2.90f, 3.86f, 4.54f, 2.74f}},
+    {32, 32, 2, 2, 4, 128, 4, {0.21f, 0.27f, 0.36f, 0.43f}, {2.59f, 2.97f, 3.37f, 1.56f}},
+};
+
+template <int NC>
+int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K) {
+  int best = 0;
+  double bc = 0.0;
+  for (int c = 0; c < NC; ++c) {
+    const double v = tile_cost(cfgs[c], M, N, (K + 127) / 128 * 64);  // tile_cost counts stages of 64
+    if (c == 0 || v < bc) best = c, bc = v;
+  }
+  return best;
+}
+
 // ---------------------------------------------------------------- attention
 // bf16 kernel forms: running max; and with a bound on the scores the fixed
 // reference in a software-pipelined loop, a plain loop (also with two wave

@@ -12,6 +12,11 @@ def f64(t):
     return None if t is None else t.detach().cpu().to(torch.float64)
 
 
+def f64_there(t):
+    """The same, left on its device."""
+    return None if t is None else t.detach().to(torch.float64)
+
+
 def rope(x, pos, sections, freq, layout, gain=None, eps=EPS):
     """(result, bound): x [B, T, H, dh], pos [T, 3] or [B, T, 3]."""
     x, pos = f64(x), f64(pos)
@@ -87,9 +92,9 @@ def norm_residual(h, y=None, post="rms", post_gain=None, gate=None, res_scale=1.
     return (out, err), (u, eu)
 
 
-def check(got, ref, bound, dtype=None):
+def check(got, ref, bound, dtype=None, wide=f64):
     """|got - ref| within the bound and half a step of the result's type."""
-    got = f64(got)
+    got = wide(got)
     tol = bound * (1 + 2.0 ** -8) + HALF[dtype or torch.float32] * (ref.abs() + bound) + 2.0 ** -133
     assert got.shape == ref.shape
     bad = ~((got - ref).abs() <= tol)
@@ -118,47 +123,47 @@ def check_blocks(q, s, x, bound, rows=1):
     assert (off <= tol).all(), float((off / tol).max())
 
 
-def values(q, s, rows):
+def values(q, s, rows, wide=f64):
     """The float64 matrix that blocks of (rows x 128) stand for."""
-    q, s = f64(q), f64(s)
+    q, s = wide(q), wide(s)
     M, K = q.shape
     return q * s.repeat_interleave(rows, 0)[:M].repeat_interleave(128, 1)[:, :K]
 
 
-def _cut(a, a_scale, w, w_scale):
+def _cut(a, a_scale, w, w_scale, wide):
     """What the 8-bit matrix instruction may cut off a bf16 result's sums: in a group
     of 8 consecutive k, with E the largest sum of the two operands' exponents (of
     subnormals and normals below 2^-6: -6), each of at most 8 products loses less
     than 2^(E - 13)."""
     def power(q):  # 2^exponent, 0 for a zero
-        q = f64(q).abs()
+        q = wide(q).abs()
         e = torch.exp2(torch.floor(torch.log2(q.clamp_min(2.0 ** -20))).clamp_min(-6.0))
         return torch.where(q > 0, e, torch.zeros_like(q))
     (M, K), N = a.shape, w.shape[0]
     pa, pw = power(a), power(w)
-    total = torch.zeros(M, N, dtype=torch.float64)
-    sa, sw = f64(a_scale), f64(w_scale).repeat_interleave(128, 0)[:N]
+    total = torch.zeros(M, N, dtype=torch.float64, device=pa.device)
+    sa, sw = wide(a_scale), wide(w_scale).repeat_interleave(128, 0)[:N]
     for k in range(0, K, 8):
-        top = torch.zeros(M, N, dtype=torch.float64)
+        top = torch.zeros_like(total)
         for i in range(k, min(K, k + 8)):
             top = torch.maximum(top, pa[:, i:i + 1] * pw[:, i])
         total += 8 * 2.0 ** -13 * top * sa[:, k // 128, None] * sw[:, k // 128]
     return total
 
 
-def matmul(a, a_scale, w, w_scale, bias=None, gelu=False, dtype=torch.float32):
+def matmul(a, a_scale, w, w_scale, bias=None, gelu=False, dtype=torch.float32, wide=f64):
     """(product, bound): the 128 products of a block are exact in float32; their sum
     takes 128 roundings (of a full step each at most), its scaling and the sum over
     the blocks four half steps a block.  With a bf16 result the products are cut
     first (_cut)."""
-    A, W = values(a, a_scale, 1), values(w, w_scale, 128)
+    A, W = values(a, a_scale, 1, wide), values(w, w_scale, 128, wide)
     c, most = A @ W.t(), A.abs() @ W.abs().t()
     blocks = -(-A.shape[1] // 128)
     err = most * D * (2 * 128 + 4 * blocks)
     if dtype == torch.bfloat16:
-        err = err + _cut(a, a_scale, w, w_scale)
+        err = err + _cut(a, a_scale, w, w_scale, wide)
     if bias is not None:
-        c = c + f64(bias)
+        c = c + wide(bias)
         err = err + D * c.abs()
     if gelu:
         x, z = c, 2.0 * (2.0 / torch.pi) ** 0.5 * (c + 0.044715 * c ** 3)

@@ -334,6 +334,37 @@ def test_matmul(dev, R, M, N, K, dtype):
     _check_matmul(R, ops, dtype, bias=_rand(dev, 9, N), gelu=True)
 
 
+# sizes that take each tile of the planner (tests/test_plan_fp8.py), with whole and
+# ragged stages, rows and columns off the tile: exact (float32 result), M, N, K
+TILES = [
+    (0, 6609, 916, 200), (0, 8236, 642, 640), (0, 8222, 648, 512),        # 128x256
+    (0, 8291, 452, 1216), (0, 5498, 641, 640), (0, 9430, 1566, 512),      # 160x128
+    (0, 6701, 1056, 200), (0, 8648, 797, 333), (0, 8807, 835, 512),       # 192x256
+    (0, 9864, 1071, 200), (0, 5522, 2075, 512), (0, 9798, 1093, 1216),    # 256x256
+    (0, 599, 4880, 200), (0, 8388, 335, 333), (0, 4942, 597, 640),        # 64x128
+    (0, 8302, 38, 333), (0, 8577, 40, 200), (0, 9141, 33, 512),           # 64x64
+    (0, 6818, 129, 333), (0, 8617, 99, 512), (0, 6740, 131, 1216),        # 96x64
+    (0, 36, 31, 333), (0, 33, 32, 1216),                                  # 32x32
+    (1, 8949, 651, 200), (1, 8209, 687, 333), (1, 4042, 1432, 512),       # 128x128
+    (1, 9513, 390, 200), (1, 8321, 449, 512), (1, 6139, 654, 640),        # 160x128
+    (1, 6218, 769, 200), (1, 8250, 521, 512), (1, 962, 4623, 1216),       # 96x128
+    (1, 6714, 131, 200), (1, 8462, 99, 512), (1, 6575, 130, 1216),        # 96x64
+    (1, 8853, 35, 200), (1, 8198, 33, 512), (1, 297, 4249, 1216),         # 64x64
+    (1, 34, 32, 333), (1, 33, 30, 640),                                   # 32x32
+]
+
+
+@pytest.mark.parametrize("exact,M,N,K", TILES)
+def test_matmul_tiles(dev, R, exact, M, N, K):
+    """Every tile, every element (the float64 product on the GPU)."""
+    dtype = F32 if exact else BF16
+    ops = _operands(R, dev, M, N, K)
+    bias = _rand(dev, 9, N)
+    for gelu in (False, True):
+        out = R.matmul_fp8(*ops, bias=bias, gelu=gelu, out_dtype=dtype)
+        F.check(out, *F.matmul(*ops, bias, gelu, dtype, wide=F.f64_there), dtype=dtype, wide=F.f64_there)
+
+
 def test_matmul_strides_and_tail_bytes(dev, R):
     """Padded rows whose bytes past K are NaN, strided scales, an odd result row
     stride: none of it enters, the elements between stay."""

@@ -4,6 +4,8 @@
 // each reads its inputs once and writes its results once.
 #include <math.h>
 
+#include <algorithm>
+
 #include "fp8.h"
 #include "wam_internal.h"
 
@@ -291,14 +293,18 @@ __device__ __forceinline__ float wave_sum_fast(float v) {
   return v + __shfl_xor(v, 32, 64);
 }
 
-constexpr int kNormCols = 8;  // columns of a lane and chunk
+constexpr int kNormCols = 4;  // columns of a lane and chunk
 
-// A row belongs to W waves (one up to 512 CH = 2048 columns, else four) and stays
+// A row belongs to W waves (one up to 256 CH = 2048 columns, else four) and stays
 // in registers between its loads and stores: lane i holds the columns
-// 8 (i + 64 W c) .. + 7 of chunk c < CH = ceil(D / 512 W), 16-byte loads and
-// stores in bf16, twice that in float32, at any alignment.  Sums are over lanes,
-// and over the waves in LDS.  Sixteen lanes of a chunk are one block of 128
-// columns, which is what 8-bit results need.
+// 4 (i + 64 W c) .. + 3 of chunk c < CH = ceil(D / 256 W), 16-byte loads and
+// stores in float32 that a wave makes without a gap, 8-byte ones in bf16, at any
+// alignment (with eight columns a lane, 16 bytes of bf16 but two strided loads of
+// float32: 4 x 2306 rows of 1024 31.7 against 29.7 us).  Sums are over lanes, and over
+// the waves in LDS.  32 lanes of a chunk are one block of 128 columns, which is
+// what 8-bit results need.  HBM bound: 10 to 12 bytes an element at 3.8-4.5 TB/s
+// over buffers larger than the last-level cache, 5.1 with modulation per row;
+// requesting gate and modulation ahead of the sums was 3-5% slower (registers).
 template <int CH, int W, typename TH, typename TY>
 __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
   __shared__ float part[2][4];
@@ -409,9 +415,11 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int n = have(c);
-      const float s = block_scale(group_max<16>(most_of(x[c])));
+      uint32_t most = group_max<16>(most_of(x[c]));
+      most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
+      const float s = block_scale(most);
       store_e4m3(static_cast<uint8_t*>(a.u) + u0 + col(c), x[c], s, n);
-      if (lane % 16 == 0 && n > 0) us[col(c) / kScaleBlock] = s;
+      if (lane % 32 == 0 && n > 0) us[col(c) / kScaleBlock] = s;
     }
   }
 }
@@ -422,18 +430,26 @@ hipError_t launch_norm_rows(const wam_norm_args& a, hipStream_t s) {
   // one wave per row: blocks of four rows, or of one while the chip has room
   const int block = W > 1 || rows >= 1024 ? 256 : kWave;
   const dim3 grid((unsigned)(W > 1 ? rows : (rows + block / kWave - 1) / (block / kWave)));
-  switch ((a.D + kNormCols * kWave * W - 1) / (kNormCols * kWave * W)) {
-    case 1: launch_k(norm_residual_kernel<1, W, TH, TY>, grid, block, 0, s, a); break;
-    case 2: launch_k(norm_residual_kernel<2, W, TH, TY>, grid, block, 0, s, a); break;
-    case 3: launch_k(norm_residual_kernel<3, W, TH, TY>, grid, block, 0, s, a); break;
-    case 4: launch_k(norm_residual_kernel<4, W, TH, TY>, grid, block, 0, s, a); break;
-    default: return hipErrorInvalidValue;
-  }
+  const int chunks = (a.D + kNormCols * kWave * W - 1) / (kNormCols * kWave * W);
+  auto launch = [&](auto CH) {
+    constexpr int c = decltype(CH)::value;
+    if constexpr (W == 1 || c > 2) {  // four waves: past 2048 columns
+      if (chunks == c) launch_k(norm_residual_kernel<c, W, TH, TY>, grid, block, 0, s, a);
+    }
+  };
+  launch(std::integral_constant<int, 1>{});
+  launch(std::integral_constant<int, 2>{});
+  launch(std::integral_constant<int, 3>{});
+  launch(std::integral_constant<int, 4>{});
+  launch(std::integral_constant<int, 5>{});
+  launch(std::integral_constant<int, 6>{});
+  launch(std::integral_constant<int, 7>{});
+  launch(std::integral_constant<int, 8>{});
   return hipGetLastError();
 }
 template <typename TH, typename TY>
 hipError_t launch_norm(const wam_norm_args& a, hipStream_t s) {
-  return a.D <= 4 * kNormCols * kWave ? launch_norm_rows<1, TH, TY>(a, s) : launch_norm_rows<4, TH, TY>(a, s);
+  return a.D <= 8 * kNormCols * kWave ? launch_norm_rows<1, TH, TY>(a, s) : launch_norm_rows<4, TH, TY>(a, s);
 }
 
 // ------------------------------------------------------------- quantisation
@@ -564,19 +580,18 @@ hipError_t launch_rope(const RopeParams& p, hipStream_t s) {
   RopeTiling tl{};
   tl.lanes = 1;
   while (tl.lanes * 16 < a.dh) tl.lanes *= 2;
+  // Four heads side by side, two waves along the rows, up to three steps over the
+  // heads: within 2% of the fastest tiling at 10176 rows of 24 heads (28 us; the worst
+  // 56), 2 x 2877 of 19 (13.5; 37), 4 x 2306 of 16 and 4000 float32 rows of 8 heads
+  // of 128, rows or heads innermost in memory alike.  Few rows: one step, so that
+  // more blocks share them.
   const int slots = kWave / tl.lanes;
-  // lanes side by side in memory: heads of a row, or rows of a head
-  const int64_t* st = a.Hq > 0 ? a.q_stride : a.k_stride;
-  const bool rows_first = a.T > 1 && st[1] < st[2];
   tl.heads_wave = 1;
-  if (!rows_first)
-    while (tl.heads_wave < slots && tl.heads_wave < H) tl.heads_wave *= 2;
-  tl.wave_rows = rows_first || rows < 4 * 256 ? 1 : 4;
+  while (tl.heads_wave < 4 && tl.heads_wave < H) tl.heads_wave *= 2;
+  tl.wave_rows = 2;
   const int rows_block = slots / tl.heads_wave * tl.wave_rows, head_step = tl.heads_wave * 4 / tl.wave_rows;
   const int64_t row_blocks = (rows + rows_block - 1) / rows_block;
-  // heads of a block: few enough for eight blocks per CU, if there are that many
-  int steps = (H + head_step - 1) / head_step;
-  while (steps > 1 && row_blocks * ((H + head_step * steps - 1) / (head_step * steps)) < 1024) --steps;
+  const int steps = row_blocks < 256 ? 1 : std::min(3, (H + head_step - 1) / head_step);
   tl.heads_block = head_step * steps;
   const int64_t head_blocks = (H + tl.heads_block - 1) / tl.heads_block;
   if (row_blocks > 0x7fffffff || head_blocks > 65535) return hipErrorInvalidValue;

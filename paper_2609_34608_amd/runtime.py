@@ -371,7 +371,7 @@ _MATMUL_ARGS = struct.Struct("@5iPqPqPqPqPPq")
 def _operand(t, what, dtypes, index, shape=None):
     """Checks an operator's tensor: on GPU `index`, of one of dtypes, of the given
     shape, its last dimension contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != index:
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:  # -1: not on a GPU
         raise WamError(f"{what}: needs a tensor on the GPU of the first operand")
     if t.dtype not in dtypes:
         raise WamError(f"{what}: dtype {t.dtype} is not supported")
@@ -488,14 +488,11 @@ def _row_vectors(v, what, index, shape):
     if v is None:
         return 0, 0, 0
     _operand(v, what, _F32, index)
-    try:
-        v = v.expand(shape)
-    except RuntimeError:
-        raise WamError(f"{what}: shape {tuple(v.shape)} does not broadcast to {tuple(shape)}") from None
-    s0, s1, s2 = v.stride()
-    if s2 != 1 and shape[2] > 1:
-        raise WamError(f"{what}: needs D values per row")
-    return v.data_ptr(), s0, s1
+    n, own = v.dim(), v.shape
+    if not 1 <= n <= 3 or own[-1] != shape[2] or any(own[i] not in (1, shape[3 - n + i]) for i in range(n - 1)):
+        raise WamError(f"{what}: shape {tuple(own)} does not broadcast to {tuple(shape)} with D values per row")
+    s = v.stride()
+    return (v.data_ptr(), s[0] if n == 3 and own[0] != 1 else 0, s[-2] if n >= 2 and own[-2] != 1 else 0)
 
 
 _NO_ROWS = (0, 0)

@@ -63,7 +63,11 @@ extern "C" {
 #define WAM_BF16 1 /* projection / attention operands bf16, fp32 accumulate;
                       residual stream, trajectory, layer state, norms and all
                       reductions stay float32 (or float64 for gate sums)      */
-#define WAM_FP8 2  /* as an element type: e4m3 (layer operators)               */
+#define WAM_FP8 2  /* as WAM_BF16, but the four projections of a layer multiply
+                      e4m3 blocks: weights 128 x 128, packed by wam_init,
+                      activations 1 x 128, each with a float32 scale (as
+                      wam_quantize_fp8 makes them); modulation, attention and
+                      everything else stay as they are.  As an element type: e4m3 */
 
 /* ---- Residual Rescaling modes ------------------------------------------ */
 #define WAM_RR_OFF 0        /* plain full forward, no layer state kept        */
@@ -118,6 +122,11 @@ extern "C" {
 /* A bounded form asked for on a layer whose gains allow no bound (mref > 60)
    runs the running-max kernel. */
 
+/* pairs of rotary positions in a head (wam_rope) */
+#define WAM_ROPE_HALVES 0 /* elements i and i + P      */
+#define WAM_ROPE_PAIRS 1  /* elements 2 i and 2 i + 1  */
+#define WAM_MAX_HEAD 256
+
 #define WAM_MAX_BATCH 16
 #define WAM_MAX_COMPONENTS 8
 #define WAM_MAX_STEPS 64
@@ -136,7 +145,7 @@ extern "C" {
 typedef struct wam_handle *wam_t;
 
 /* Model configuration.  D % 64 == 0 (D <= 2048), D % H == 0, head size D/H in
- * {32, 64}, Cv <= 16, A <= 16, Co <= 64; bf16 mode additionally needs
+ * {32, 64}, Cv <= 16, A <= 16, Co <= 64; bf16 and fp8 modes additionally need
  * D/H == 64 and F % 128 == 0 (any head count, odd ones included).  Nv >= 0, Na >= 0, Nv + Na >= 1:
  * a model of an independently executed pair has only video (Na = 0) or only
  * action (Nv = 0) tokens; Cv and A stay >= 1 (their weights exist). */
@@ -149,7 +158,7 @@ typedef struct {
   int32_t Nv, Cv;  /* video-latent tokens, channels per token               */
   int32_t Na, A;   /* action tokens (chunk length), action dimension        */
   int32_t No, Co;  /* observation tokens, channels per token                */
-  int32_t dtype;   /* WAM_FP32 | WAM_BF16                                   */
+  int32_t dtype;   /* WAM_FP32 | WAM_BF16 | WAM_FP8                         */
   int32_t qk_norm; /* 1: RMS-normalise q and k per head (with gains)        */
   float ln_eps;    /* epsilon of LayerNorm and QK RMSNorm                   */
 } wam_config;
@@ -292,6 +301,29 @@ const char *wam_status_string(int status);
  * and WAM_E_UNSUPPORTED for graphs on the default (null) stream. */
 int wam_set_option(wam_t h, int option, int value);
 
+/* Rotary positions of the model's rows: from the next step on every layer turns
+ * q and k (after their norm) by wam_rope's rule, row t of every sample by pos[t].
+ * The additive sinusoidal table of the embedding is left out unless keep_table is
+ * set.  pos is read by every step (also by replayed graphs) and stays the
+ * caller's; freq is copied.  2 P <= head size.  args NULL: back to the table
+ * alone.  Drops the retained layer state and captured graphs; WAM_E_STATE while a
+ * replan is open. */
+typedef struct {
+  const float *pos;     /* device [T][3] (time, height, width)              */
+  int32_t sections[3];  /* pairs of each axis                               */
+  int32_t layout;       /* WAM_ROPE_*                                       */
+  const double *freq;   /* host [P]: radians per unit of position           */
+  int32_t keep_table;
+} wam_rotary_args;
+int wam_set_rotary(wam_t h, const wam_rotary_args *args);
+/* Post-norms: from the next step on the output of a layer's attention and MLP
+ * blocks (their last projection with its bias) is divided by its root mean square
+ * (ln_eps) and multiplied by its gains before gate and residual:
+ *   h <- h + gate * gain * y / sqrt(mean(y^2) + ln_eps).
+ * gains: device [L][2][D] (attention, MLP), read by every step, caller-owned;
+ * NULL: none.  State as for wam_set_rotary. */
+int wam_set_post_norm(wam_t h, const float *gains);
+
 /* Noise levels sigma_0 = 1 > ... > sigma_K = 0 of the flow schedule
  * (host float[K+1]); K <= WAM_MAX_STEPS.  Required before any step. */
 int wam_set_schedule(wam_t h, const float *sigmas, int K);
@@ -413,9 +445,6 @@ const char *wam_noalloc_last_error(void);
  * root mean square and multiplied by the gain: x gain / sqrt(mean(x^2) + eps);
  * NULL leaves it out.  Results are rounded once.  q_out may be q and k_out may be k
  * (with the same strides).  Hk = 0 leaves k out (Hq = 0: q).  dh <= 256. */
-#define WAM_ROPE_HALVES 0
-#define WAM_ROPE_PAIRS 1
-#define WAM_MAX_HEAD 256
 typedef struct {
   int32_t B, T, Hq, Hk, dh;
   int32_t dtype;              /* of q, k and the results: WAM_FP32 | WAM_BF16  */

@@ -60,6 +60,11 @@ class WamRebindArgs(C.Structure):
     _fields_ = [("cond", C.c_void_p)]
 
 
+class WamRotaryArgs(C.Structure):
+    _fields_ = [("pos", C.c_void_p), ("sections", C.c_int32 * 3), ("layout", C.c_int32), ("freq", C.c_void_p),
+                ("keep_table", C.c_int32)]
+
+
 class WamReplanStateArgs(C.Structure):
     _fields_ = [("x_bar", C.c_void_p), ("x_r", C.c_void_p), ("kappa", C.c_int32)]
 
@@ -129,6 +134,8 @@ EXPORTS = {
     "wam_last_error": (C.c_char_p, [C.c_void_p]),
     "wam_status_string": (C.c_char_p, [C.c_int]),
     "wam_set_option": (C.c_int, [C.c_void_p, C.c_int, C.c_int]),
+    "wam_set_rotary": (C.c_int, [C.c_void_p, C.POINTER(WamRotaryArgs)]),
+    "wam_set_post_norm": (C.c_int, [C.c_void_p, C.c_void_p]),
     "wam_set_schedule": (C.c_int, [C.c_void_p, C.POINTER(C.c_float), C.c_int]),
     "wam_velocity": (C.c_int, [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p,
                                C.POINTER(WamRRProfile), C.POINTER(WamStepInfo)]),

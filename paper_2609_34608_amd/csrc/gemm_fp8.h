@@ -36,21 +36,15 @@ namespace gemm {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// A wave's weight rows are dealt to its 16-row MFMA tiles so that the tiles 2 q and
-// 2 q + 1 together give a lane eight consecutive columns (one 16-byte store of
-// bf16), and the four lane groups 32: the row of tile j, index i (0..15), and the
-// first column of tile j in lane group g.  Tiles that have no pair stay in order.
+// Weight rows are dealt to the MFMA tiles in pairs (tile_row) where a wave has an
+// even number of them.
 template <int TN>
-__host__ __device__ constexpr int tile_row(int j, int i) {
-  return TN % 2 ? j * 16 + i : (j / 2) * 32 + (i / 4) * 8 + (j % 2) * 4 + i % 4;
-}
-template <int TN>
-__host__ __device__ constexpr int tile_col(int j, int g) { return tile_row<TN>(j, 4 * g); }
+constexpr bool kPaired = TN % 2 == 0;
 // XOR swizzle of a weight row's chunks: index i of every tile gets i & 7, as an
 // activation row does
 template <int TN>
 __host__ __device__ constexpr int weight_swizzle(int row) {
-  return TN % 2 ? row & 7 : (row & 3) | ((row >> 3) & 1) << 2;
+  return kPaired<TN> ? (row & 3) | ((row >> 3) & 1) << 2 : row & 7;
 }
 
 struct Fp8Operands {
@@ -79,9 +73,11 @@ __device__ __forceinline__ bf16x8 to_bf16(const i32x8& v, int t) {
   return r;
 }
 
-// WIDE: rows further apart than 32-bit offsets inside a tile reach.
-template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool GELU, bool WIDE>
-__global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, Fp8Out o) {
+// The product of one block's tile; epilogue(acc, m, n, lane) takes a wave's
+// accumulators, whose rows start at m and columns at n.  WIDE: rows further apart
+// than 32-bit offsets inside a tile reach.
+template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool WIDE, typename EPILOGUE>
+__device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epilogue) {
   constexpr int BK = kScaleBlock;              // bytes of a row per stage
   constexpr int NW = WGM * WGN;
   constexpr int WM = BM / WGM, WN = BN / WGN;  // wave tile
@@ -165,7 +161,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
 
   const int lr = lane % 16, lg = lane / 16;
   const int ch0 = (lg ^ chunk_swizzle(lr)) * 16, ch1 = ((lg + 4) ^ chunk_swizzle(lr)) * 16;
-  const int arow = (wm * WM + lr) * BK, wrow = (BM + wn * WN + tile_row<TN>(0, lr)) * BK;
+  const int arow = (wm * WM + lr) * BK, wrow = (BM + wn * WN + tile_row<kPaired<TN>>(0, lr)) * BK;
   auto operand = [&](const uint8_t* row) __attribute__((always_inline)) {
     const i32x4 x = *reinterpret_cast<const i32x4*>(row + ch0), y = *reinterpret_cast<const i32x4*>(row + ch1);
     return i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
@@ -182,7 +178,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
     for (int i = 0; i < TM; ++i) f[i] = sc[wm * WM + i * 16 + lr] * sw;
     i32x8 wf[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) wf[j] = operand(&sm[s][wrow + tile_row<TN>(j, 0) * BK]);
+    for (int j = 0; j < TN; ++j) wf[j] = operand(&sm[s][wrow + tile_row<kPaired<TN>>(j, 0) * BK]);
     if constexpr (EXACT) {
       bf16x8 wb[TN][4];
 #pragma unroll
@@ -287,6 +283,15 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
   // no load may still be writing this block's LDS when the block retires
   __builtin_amdgcn_s_waitcnt(0);
 
+  epilogue(acc, m0 + wm * WM, n0 + wn * WN, lane);
+}
+
+// Bias, activation and rounding of a wave's accumulators into a result of any row
+// stride.
+template <int TN, int TM, bool EXACT, bool GELU>
+__device__ __forceinline__ void store_product(const Fp8Operands& p, const Fp8Out& o, const f32x4 (&acc)[TN][TM],
+                                              int mb, int nb, int lane) {
+  const int lr = lane % 16, lg = lane / 16;
   // G tiles side by side hold W consecutive columns of a lane.  Global memory takes
   // wide stores at any address, so rows of any stride do; only columns that N cuts
   // off go one by one, in a pass of their own that most blocks skip.
@@ -304,7 +309,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
 #pragma unroll
     for (int j = 0; j < TN / G; ++j)
 #pragma unroll
-      for (int r = 0; r < W; ++r) bias[j][r] = o.bias[min(n0 + wn * WN + tile_col<TN>(j * G, lg) + r, p.N - 1)];
+      for (int r = 0; r < W; ++r) bias[j][r] = o.bias[min(nb + tile_col<kPaired<TN>>(j * G, lg) + r, p.N - 1)];
   auto value = [&](int j, int i, int r) __attribute__((always_inline)) {
     const float v = acc[j * G + r / 4][i][r % 4] + bias[j][r];
     return static_cast<T>(GELU ? gelu_tanh_f(v) : v);
@@ -312,24 +317,24 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
   T* out = static_cast<T*>(o.out);
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int m = m0 + wm * WM + i * 16 + lr;
+    const int m = mb + i * 16 + lr;
     if (m >= p.M) continue;
 #pragma unroll
     for (int j = 0; j < TN / G; ++j) {
-      const int n = n0 + wn * WN + tile_col<TN>(j * G, lg);
+      const int n = nb + tile_col<kPaired<TN>>(j * G, lg);
       Row x;
 #pragma unroll
       for (int r = 0; r < W; ++r) x.v[r] = value(j, i, r);
       if (n + W <= p.N) *reinterpret_cast<Row*>(out + (int64_t)m * o.ld + n) = x;
     }
   }
-  if (p.N % W && n0 + BN > p.N) {
+  if (p.N % W && nb + TN * 16 > p.N) {
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int m = m0 + wm * WM + i * 16 + lr;
+      const int m = mb + i * 16 + lr;
 #pragma unroll
       for (int j = 0; j < TN / G; ++j) {
-        const int n = n0 + wn * WN + tile_col<TN>(j * G, lg);
+        const int n = nb + tile_col<kPaired<TN>>(j * G, lg);
         if (m >= p.M || n >= p.N || n + W <= p.N) continue;
 #pragma unroll
         for (int r = 0; r < W; ++r)
@@ -337,6 +342,27 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, 
       }
     }
   }
+}
+
+template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool GELU, bool WIDE>
+__global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, Fp8Out o) {
+  constexpr int TM = BM / WGM / 16, TN = BN / WGN / 16;
+  gemm_fp8_body<BM, BN, WGM, WGN, ST, EXACT, WIDE>(
+      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane) __attribute__((always_inline)) {
+        store_product<TN, TM, EXACT, GELU>(p, o, acc, m, n, lane);
+      });
+}
+
+// A projection of the DiT block (store_tile's epilogues, N a multiple of 64).
+template <int BM, int BN, int WGM, int WGN, int ST, int EPI>
+__global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_layer_kernel(Fp8Operands p, GemmArgs g) {
+  constexpr int TM = BM / WGM / 16, TN = BN / WGN / 16;
+  static_assert(EPI != EPI_QKV || TN == 4, "QKV epilogue needs whole heads per wave");
+  if (g.skip && *g.skip) return;
+  gemm_fp8_body<BM, BN, WGM, WGN, ST, false, false>(
+      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane) __attribute__((always_inline)) {
+        if (n < p.N) store_tile<bf16, EPI, 64, TN, TM, kPaired<TN>>(g, acc, m, n, lane);
+      });
 }
 
 }  // namespace gemm

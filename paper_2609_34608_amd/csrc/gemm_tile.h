@@ -99,9 +99,20 @@ __device__ __forceinline__ f32x4 gelu4(f32x4 v) {
   return f32x4{gelu_tanh_f(v[0]), gelu_tanh_f(v[1]), gelu_tanh_f(v[2]), gelu_tanh_f(v[3])};
 }
 
+// Weight row of index i (0..15) of a wave's MFMA tile j, and the first column of
+// tile j in lane group g.  In order, or (PAIRED, an even number of tiles) dealt so
+// that the tiles 2 q and 2 q + 1 together give a lane eight consecutive columns, one
+// 16-byte store of bf16, and the four lane groups 32.
+template <bool PAIRED>
+__host__ __device__ constexpr int tile_row(int j, int i) {
+  return PAIRED ? (j / 2) * 32 + (i / 4) * 8 + (j % 2) * 4 + i % 4 : j * 16 + i;
+}
+template <bool PAIRED>
+__host__ __device__ constexpr int tile_col(int j, int g) { return tile_row<PAIRED>(j, 4 * g); }
+
 // Epilogue of one wave's accumulators: acc[j][i] element r is the product at
-// row mb + i*16 + lane%16, column nb + j*16 + 4*(lane/16) + r.
-template <typename E, int EPI, int DH, int TN, int TM>
+// row mb + i*16 + lane%16, column nb + tile_col(j, lane/16) + r.
+template <typename E, int EPI, int DH, int TN, int TM, bool PAIRED = false>
 __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x4 (&acc)[TN][TM], int mb, int nb, int lane) {
   const int lr = lane % 16, lg = lane / 16;
   if constexpr (EPI == EPI_QKV) {
@@ -109,16 +120,16 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x4 (&acc)
     const QkvOut& qo = a.qkv;
     const int D = qo.D;
     // per-lane constants hoisted out of the store loop: bias of the lane's
-    // columns and the q / k gains of its head dims (d = jj*16 + 4*lg + r)
+    // columns and the q / k gains of its head dims
     f32x4 bias[TN], qg[JH], kg[JH];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) bias[j] = *reinterpret_cast<const f32x4*>(a.bias + nb + j * 16 + lg * 4);
+    for (int j = 0; j < TN; ++j) bias[j] = *reinterpret_cast<const f32x4*>(a.bias + nb + tile_col<PAIRED>(j, lg));
 #pragma unroll
     for (int jj = 0; jj < JH; ++jj) {
       qg[jj] = kg[jj] = f32x4{1.f, 1.f, 1.f, 1.f};
       if (qo.qk_norm) {
-        qg[jj] = *reinterpret_cast<const f32x4*>(qo.q_g + jj * 16 + lg * 4);
-        kg[jj] = *reinterpret_cast<const f32x4*>(qo.k_g + jj * 16 + lg * 4);
+        qg[jj] = *reinterpret_cast<const f32x4*>(qo.q_g + tile_col<PAIRED>(jj, lg));
+        kg[jj] = *reinterpret_cast<const f32x4*>(qo.k_g + tile_col<PAIRED>(jj, lg));
       }
       qg[jj] *= q_log2_scale(DH);  // attention scores come out in log2 units
     }
@@ -146,7 +157,7 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x4 (&acc)
           if (m < a.M) {
             E* dst = static_cast<E*>(sec == 0 ? qo.q : qo.k) + (((size_t)b * qo.H + head) * qo.Tpad + t) * DH;
 #pragma unroll
-            for (int jj = 0; jj < JH; ++jj) store4(dst + jj * 16 + lg * 4, v[jj] * rs * gain[jj]);
+            for (int jj = 0; jj < JH; ++jj) store4(dst + tile_col<PAIRED>(jj, lg), v[jj] * rs * gain[jj]);
           }
         } else if (m < a.M) {
           // V^T row d; bf16: the tokens of each 64-key block in vt_key_pos order
@@ -156,7 +167,7 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x4 (&acc)
           for (int jj = 0; jj < JH; ++jj)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-              dst[(size_t)(jj * 16 + lg * 4 + r) * qo.Tpad] = static_cast<E>(v[jj][r]);
+              dst[(size_t)(tile_col<PAIRED>(jj, lg) + r) * qo.Tpad] = static_cast<E>(v[jj][r]);
         }
       }
     }
@@ -167,7 +178,7 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x4 (&acc)
     f32x4 bias[TN], gate[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int n = nb + j * 16 + lg * 4;
+      const int n = nb + tile_col<PAIRED>(j, lg);
       bias[j] = *reinterpret_cast<const f32x4*>(a.bias + n);
       if constexpr (EPI == EPI_GATED_RES) gate[j] = *reinterpret_cast<const f32x4*>(a.gate + n);
     }
@@ -181,25 +192,26 @@ __device__ __forceinline__ void store_tile(const GemmArgs& a, const f32x4 (&acc)
         const size_t off = (size_t)m * a.N + nb + lg * 4;
         const f32x4* rrow = reinterpret_cast<const f32x4*>(a.res + off);
         f32x4* hrow = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + off);
+        auto at = [&](int j) { return (tile_col<PAIRED>(j, lg) - lg * 4) / 4; };
         f32x4 hv[TN];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) hv[j] = rrow[j * 4];
+        for (int j = 0; j < TN; ++j) hv[j] = rrow[at(j)];
 #pragma unroll
         for (int j = 0; j < TN; ++j) hv[j] = hv[j] + gate[j] * (acc[j][i] + bias[j]);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) hrow[j * 4] = hv[j];
+        for (int j = 0; j < TN; ++j) hrow[at(j)] = hv[j];
         if (a.copy) {
           f32x4* crow = reinterpret_cast<f32x4*>(a.copy + off);
 #pragma unroll
-          for (int j = 0; j < TN; ++j) crow[j * 4] = hv[j];
+          for (int j = 0; j < TN; ++j) crow[at(j)] = hv[j];
         }
       } else {
-        E* orow = static_cast<E*>(a.out) + (size_t)m * a.N + nb + lg * 4;
+        E* orow = static_cast<E*>(a.out) + (size_t)m * a.N + nb;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
           const f32x4 v = acc[j][i] + bias[j];
-          if constexpr (EPI == EPI_BIAS_GELU) store4(orow + j * 16, gelu4(v));
-          else store4(orow + j * 16, v);
+          if constexpr (EPI == EPI_BIAS_GELU) store4(orow + tile_col<PAIRED>(j, lg), gelu4(v));
+          else store4(orow + tile_col<PAIRED>(j, lg), v);
         }
       }
     }
@@ -338,7 +350,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_f32_kernel(GemmArgs a) {
 }
 
 // The four projections: role 0 QKV, 1 attention output, 2 MLP-up, 3 MLP-down,
-// each with its own epilogue.
+// each with its own epilogue; 1 and 3 in front of a post-norm only add the bias.
 template <int BM, int BN, int WGM, int WGN, int ST, int BK>
 hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
   const int blocks = ((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN);
@@ -354,6 +366,8 @@ hipError_t launch_tile(const GemmArgs& a, hipStream_t s) {
     launch_k(gemm_bf16_kernel<BM, BN, WGM, WGN, ST, BK, EPI_BIAS_GELU, 2>, blocks, NT, 0, s, a);
   } else if (a.role == 3 && a.epi == EPI_GATED_RES) {
     launch_k(gemm_bf16_kernel<BM, BN, WGM, WGN, ST, BK, EPI_GATED_RES, 3>, blocks, NT, 0, s, a);
+  } else if (a.epi == EPI_BIAS) {
+    launch_k(gemm_bf16_kernel<BM, BN, WGM, WGN, ST, BK, EPI_BIAS, 1>, blocks, NT, 0, s, a);
   } else {
     return hipErrorInvalidValue;
   }
@@ -367,6 +381,9 @@ hipError_t launch_tile_f32(const GemmArgs& a, hipStream_t s) {
   switch (a.epi) {
     case EPI_BIAS_GELU:
       launch_k(gemm_f32_kernel<BM, BN, WGM, WGN, ST, BK, EPI_BIAS_GELU, 64>, blocks, NT, 0, s, a);
+      break;
+    case EPI_BIAS:
+      launch_k(gemm_f32_kernel<BM, BN, WGM, WGN, ST, BK, EPI_BIAS, 64>, blocks, NT, 0, s, a);
       break;
     case EPI_GATED_RES:
       launch_k(gemm_f32_kernel<BM, BN, WGM, WGN, ST, BK, EPI_GATED_RES, 64>, blocks, NT, 0, s, a);

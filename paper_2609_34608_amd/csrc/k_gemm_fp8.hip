@@ -1,5 +1,6 @@
 // Product of e4m3 matrices with block scales: checks and dispatch of
-// wam_matmul_fp8 for the kernels of gemm_fp8.h.
+// wam_matmul_fp8, and the projections of the 8-bit mode, for the kernels of
+// gemm_fp8.h.
 #include <utility>
 
 #include "gemm_fp8.h"
@@ -51,9 +52,47 @@ hipError_t launch_fp8(const Fp8Operands& p, const Fp8Out& o, bool exact, bool ge
                            std::make_integer_sequence<int, kCfgCount>{});
 }
 
+template <int C>
+hipError_t launch_layer_cfg(const Fp8Operands& p, const GemmArgs& g, hipStream_t s) {
+  constexpr TileCfg t = kFp8Cfgs[C];
+  const int64_t blocks = (int64_t)((p.M + t.bm - 1) / t.bm) * ((p.N + t.bn - 1) / t.bn);
+  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)blocks), block(t.wgm * t.wgn * 64);
+  auto go = [&](auto EPI) {
+    launch_k(gemm::gemm_fp8_layer_kernel<t.bm, t.bn, t.wgm, t.wgn, t.st, decltype(EPI)::value>, grid, block, 0, s, p, g);
+    return hipGetLastError();
+  };
+  switch (g.epi) {
+    case EPI_BIAS: return go(std::integral_constant<int, EPI_BIAS>{});
+    case EPI_BIAS_GELU: return go(std::integral_constant<int, EPI_BIAS_GELU>{});
+    case EPI_GATED_RES: return go(std::integral_constant<int, EPI_GATED_RES>{});
+    case EPI_QKV:
+      if constexpr (t.bn / t.wgn == 64) return go(std::integral_constant<int, EPI_QKV>{});
+  }
+  return hipErrorInvalidValue;
+}
+
+template <int... C>
+hipError_t launch_layer_any(const Fp8Operands& p, const GemmArgs& g, int cfg, hipStream_t s,
+                            std::integer_sequence<int, C...>) {
+  hipError_t e = hipErrorInvalidValue;
+  ((cfg == C ? (void)(e = launch_layer_cfg<C>(p, g, s)) : (void)0), ...);
+  return e;
+}
+
 bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)n == 0; }
 
 }  // namespace
+
+hipError_t launch_gemm_fp8(const GemmArgs& a, const float* a_scale, const float* w_scale, hipStream_t s) {
+  if (a.M <= 0) return hipSuccess;
+  if (a.N % 64 || a.K % 16) return hipErrorInvalidValue;
+  const int kb = (a.K + kScaleBlock - 1) / kScaleBlock;
+  const Fp8Operands p{static_cast<const uint8_t*>(a.A), static_cast<const uint8_t*>(a.W), a_scale, w_scale, a.K, a.K,
+                      kb, kb, a.M, a.N, a.K};
+  return launch_layer_any(p, a, plan_fp8(kFp8Cfgs, a.M, a.N, a.K, a.epi == EPI_QKV), s,
+                          std::make_integer_sequence<int, kCfgCount>{});
+}
 
 }  // namespace wam
 

@@ -60,6 +60,7 @@ constexpr int kMaxPairs = WAM_MAX_HEAD / 2;
 struct RopeParams {
   wam_rope_args a;
   int pairs, end0, end1;     // pairs of axis 0 end at end0, of axis 1 at end1
+  const int* skip;
   double turns[kMaxPairs];   // revolutions per unit of position
 };
 
@@ -104,6 +105,7 @@ constexpr int kRopeTable = 2048;  // most (row, pair) angles of a block
 template <typename T, bool PAIRS, bool NORM>
 __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams p, RopeTiling tl) {
   __shared__ float2 turn[kRopeTable];
+  if (p.skip && *p.skip) return;
   const wam_rope_args& a = p.a;
   const bool isq = blockIdx.z == 0 && a.Hq > 0;
   const int H = isq ? a.Hq : a.Hk;
@@ -202,6 +204,7 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams p, RopeTilin
 // Any other head size or sections: one wave per head vector, element e = lane +
 // 64 j.
 __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
+  if (p.skip && *p.skip) return;
   const wam_rope_args& a = p.a;
   const int heads = a.Hq + a.Hk;
   const int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
@@ -306,8 +309,9 @@ constexpr int kNormCols = 4;  // columns of a lane and chunk
 // over buffers larger than the last-level cache, 5.1 with modulation per row;
 // requesting gate and modulation ahead of the sums was 3-5% slower (registers).
 template <int CH, int W, typename TH, typename TY>
-__global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
+__global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, const int* skip) {
   __shared__ float part[2][4];
+  if (skip && *skip) return;
   const int lane = threadIdx.x % kWave, wid = threadIdx.x / kWave;
   const int64_t row = W == 1 ? (int64_t)blockIdx.x * (blockDim.x / kWave) + wid : blockIdx.x;
   if (W == 1 && row >= (int64_t)a.B * a.T) return;
@@ -425,7 +429,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a) {
 }
 
 template <int W, typename TH, typename TY>
-hipError_t launch_norm_rows(const wam_norm_args& a, hipStream_t s) {
+hipError_t launch_norm_rows(const wam_norm_args& a, hipStream_t s, const int* skip) {
   const int64_t rows = (int64_t)a.B * a.T;
   // one wave per row: blocks of four rows, or of one while the chip has room
   const int block = W > 1 || rows >= 1024 ? 256 : kWave;
@@ -434,7 +438,7 @@ hipError_t launch_norm_rows(const wam_norm_args& a, hipStream_t s) {
   auto launch = [&](auto CH) {
     constexpr int c = decltype(CH)::value;
     if constexpr (W == 1 || c > 2) {  // four waves: past 2048 columns
-      if (chunks == c) launch_k(norm_residual_kernel<c, W, TH, TY>, grid, block, 0, s, a);
+      if (chunks == c) launch_k(norm_residual_kernel<c, W, TH, TY>, grid, block, 0, s, a, skip);
     }
   };
   launch(std::integral_constant<int, 1>{});
@@ -448,8 +452,8 @@ hipError_t launch_norm_rows(const wam_norm_args& a, hipStream_t s) {
   return hipGetLastError();
 }
 template <typename TH, typename TY>
-hipError_t launch_norm(const wam_norm_args& a, hipStream_t s) {
-  return a.D <= 8 * kNormCols * kWave ? launch_norm_rows<1, TH, TY>(a, s) : launch_norm_rows<4, TH, TY>(a, s);
+hipError_t launch_norm(const wam_norm_args& a, hipStream_t s, const int* skip) {
+  return a.D <= 8 * kNormCols * kWave ? launch_norm_rows<1, TH, TY>(a, s, skip) : launch_norm_rows<4, TH, TY>(a, s, skip);
 }
 
 // ------------------------------------------------------------- quantisation
@@ -460,7 +464,8 @@ constexpr int kQuantCols = 16, kQuantGroup = kScaleBlock / kQuantCols;
 
 // blocks of 1 x 128
 template <typename T>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(wam_quantize_args a, int kb) {
+__global__ __launch_bounds__(256) void quantize_rows_kernel(wam_quantize_args a, int kb, const int* skip) {
+  if (skip && *skip) return;
   const uint32_t i = blockIdx.x * 32u + threadIdx.x / kQuantGroup;  // scale block
   const int m = (int)(i / (uint32_t)kb), bk = (int)(i % (uint32_t)kb);
   if (m >= a.M) return;
@@ -501,10 +506,10 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(wam_quantize_args a
 }
 
 template <typename T>
-hipError_t launch_quantize(const wam_quantize_args& a, hipStream_t s) {
+hipError_t launch_blocks(const wam_quantize_args& a, hipStream_t s, const int* skip) {
   const int kb = (a.K + kScaleBlock - 1) / kScaleBlock;
   const int64_t n = (int64_t)kb * ((a.M + a.block_rows - 1) / a.block_rows);
-  if (a.block_rows == 1) launch_k(quantize_rows_kernel<T>, dim3((unsigned)((n + 31) / 32)), 256, 0, s, a, kb);
+  if (a.block_rows == 1) launch_k(quantize_rows_kernel<T>, dim3((unsigned)((n + 31) / 32)), 256, 0, s, a, kb, skip);
   else launch_k(quantize_tiles_kernel<T>, dim3((unsigned)n), 256, 0, s, a, kb);
   return hipGetLastError();
 }
@@ -568,7 +573,7 @@ void launch_rope_units(const RopeParams& p, const RopeTiling& tl, dim3 grid, hip
   else launch_k(rope_units_kernel<T, PAIRS, false>, grid, 256, 0, s, p, tl);
 }
 
-hipError_t launch_rope(const RopeParams& p, hipStream_t s) {
+hipError_t launch_rope_params(const RopeParams& p, hipStream_t s) {
   const wam_rope_args& a = p.a;
   const int64_t rows = (int64_t)a.B * a.T;
   const int H = a.Hq > a.Hk ? a.Hq : a.Hk;
@@ -607,6 +612,27 @@ hipError_t launch_rope(const RopeParams& p, hipStream_t s) {
 }
 
 }  // namespace
+
+hipError_t launch_rope(const wam_rope_args& a, hipStream_t s, const int* skip) {
+  RopeParams p{};
+  p.a = a;
+  p.skip = skip;
+  p.end0 = a.sections[0];
+  p.end1 = p.end0 + a.sections[1];
+  p.pairs = p.end1 + a.sections[2];
+  for (int i = 0; i < p.pairs; ++i) p.turns[i] = a.freq[i] * (0.5 / M_PI);
+  return launch_rope_params(p, s);
+}
+
+hipError_t launch_norm_residual(const wam_norm_args& a, hipStream_t s, const int* skip) {
+  const bool yf = a.y && a.y_dtype == WAM_FP32;
+  if (a.h_dtype == WAM_FP32) return yf ? launch_norm<float, float>(a, s, skip) : launch_norm<float, bf16>(a, s, skip);
+  return yf ? launch_norm<bf16, float>(a, s, skip) : launch_norm<bf16, bf16>(a, s, skip);
+}
+
+hipError_t launch_quantize(const wam_quantize_args& a, hipStream_t s, const int* skip) {
+  return a.dtype == WAM_BF16 ? launch_blocks<bf16>(a, s, skip) : launch_blocks<float>(a, s, skip);
+}
 
 }  // namespace wam
 
@@ -655,13 +681,7 @@ int wam_rope(const wam_rope_args* a, void* hip_stream) {
   if (st) return st;
   if ((double)a->B * a->T * ((double)a->Hq + a->Hk) / 4 >= (double)kMaxGrid)
     return noalloc_fail(WAM_E_SHAPE, "wam_rope: too many head vectors for one launch");
-  RopeParams p{};
-  p.a = *a;
-  p.pairs = (int)pairs;
-  p.end0 = a->sections[0];
-  p.end1 = p.end0 + a->sections[1];
-  for (int i = 0; i < p.pairs; ++i) p.turns[i] = a->freq[i] * (0.5 / M_PI);
-  if (launch_rope(p, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+  if (launch_rope(*a, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
     return noalloc_fail(WAM_E_HIP, "wam_rope: kernel launch failed");
   return WAM_OK;
 }
@@ -703,11 +723,8 @@ int wam_norm_residual(const wam_norm_args* a, void* hip_stream) {
     return noalloc_fail(WAM_E_ARG, "wam_norm_residual: u must not be h or h_out");
   if (a->y && (a->h_out == a->y || (a->u == a->y && (a->u_dtype != a->y_dtype || !same(a->u_stride, a->y_stride, 2)))))
     return noalloc_fail(WAM_E_ARG, "wam_norm_residual: h_out must not be y, and u only with its type and strides");
-  hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const bool yf = a->y && a->y_dtype == WAM_FP32;
-  const hipError_t e = a->h_dtype == WAM_FP32 ? (yf ? launch_norm<float, float>(*a, s) : launch_norm<float, bf16>(*a, s))
-                                              : (yf ? launch_norm<bf16, float>(*a, s) : launch_norm<bf16, bf16>(*a, s));
-  if (e != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_norm_residual: kernel launch failed");
+  if (launch_norm_residual(*a, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
+    return noalloc_fail(WAM_E_HIP, "wam_norm_residual: kernel launch failed");
   return WAM_OK;
 }
 
@@ -727,8 +744,7 @@ int wam_quantize_fp8(const wam_quantize_args* a, void* hip_stream) {
   if (!strides_ok(&a->x_stride, 1) || (a->M > 1 && a->q_stride < a->K) || (mb > 1 && a->scale_stride < kb))
     return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: x_stride must be >= 0, and rows of the results distinct");
   if (mb * kb > kMaxGrid) return noalloc_fail(WAM_E_SHAPE, "wam_quantize_fp8: too many blocks for one launch");
-  hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if ((a->dtype == WAM_BF16 ? launch_quantize<bf16>(*a, s) : launch_quantize<float>(*a, s)) != hipSuccess)
+  if (launch_quantize(*a, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
     return noalloc_fail(WAM_E_HIP, "wam_quantize_fp8: kernel launch failed");
   return WAM_OK;
 }

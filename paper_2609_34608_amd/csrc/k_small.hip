@@ -132,11 +132,11 @@ __global__ void embed_kernel(EmbedArgs a) {
       tok[threadIdx.x] = a.cond[((size_t)b * a.No + (t - a.Nv - a.Na)) * a.Co + threadIdx.x];
   }
   __syncthreads();
-  const float* pe = a.pe + (size_t)t * a.D;
+  const float* pe = a.pe ? a.pe + (size_t)t * a.D : nullptr;
   for (int d = threadIdx.x; d < a.D; d += blockDim.x) {
     float s = bias[d];
     for (int j = 0; j < c; ++j) s += tok[j] * w[(size_t)j * a.D + d];
-    a.h[(size_t)row * a.D + d] = s + pe[d];
+    a.h[(size_t)row * a.D + d] = pe ? s + pe[d] : s;
   }
 }
 
@@ -189,7 +189,8 @@ __global__ __launch_bounds__(512) void embed_v4_kernel(EmbedArgs a) {
   for (int k = 0; k < kEmbedC; ++k) w4[k] = *reinterpret_cast<const f32x4*>(w + (size_t)min(k, c - 1) * a.D + cc);
 #pragma unroll
   for (int r = 0; r < kEmbedRows; ++r)
-    p4[r] = *reinterpret_cast<const f32x4*>(a.pe + (size_t)(t0 + min(r, n - 1)) * a.D + cc);
+    p4[r] = a.pe ? *reinterpret_cast<const f32x4*>(a.pe + (size_t)(t0 + min(r, n - 1)) * a.D + cc)
+                 : f32x4{0.f, 0.f, 0.f, 0.f};
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kEmbedRows; ++r) {

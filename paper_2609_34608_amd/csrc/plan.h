@@ -99,6 +99,7 @@ constexpr TileCfg kFp8Cfgs[] = {
     {96, 64, 2, 2, 3, 128, 2, {0.30f, 0.54f}, {2.90f, 2.11f}},
     {64, 64, 2, 2, 3, 128, 3, {0.24f, 0.38f, 0.62f}, {2.83f, 3.11f, 1.54f}},
     {32, 32, 2, 2, 4, 128, 4, {0.15f, 0.18f, 0.26f, 0.36f}, {2.56f, 2.70f, 3.09f, 1.26f}},
+    {32, 64, 2, 1, 4, 128, 3, {0.19f, 0.26f, 0.39f}, {3.09f, 3.50f, 1.69f}},  // short sequences' QKV
 };
 constexpr TileCfg kFp8ExactCfgs[] = {
     {160, 128, 2, 2, 2, 128, 2, {1.12f, 1.88f}, {5.02f, 7.14f}},
@@ -109,13 +110,16 @@ constexpr TileCfg kFp8ExactCfgs[] = {
     {32, 32, 2, 2, 4, 128, 4, {0.21f, 0.27f, 0.36f, 0.43f}, {2.59f, 2.97f, 3.37f, 1.56f}},
 };
 
+// qkv: only tiles whose waves take whole heads of 64 columns
 template <int NC>
-int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K) {
-  int best = 0;
+int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K, bool qkv = false) {
+  int best = -1;
   double bc = 0.0;
   for (int c = 0; c < NC; ++c) {
-    const double v = tile_cost(cfgs[c], M, N, (K + 127) / 128 * 64);  // tile_cost counts stages of 64
-    if (c == 0 || v < bc) best = c, bc = v;
+    const TileCfg& t = cfgs[c];
+    if (qkv && t.bn / t.wgn != 64) continue;
+    const double v = tile_cost(t, M, N, (K + 127) / 128 * 64);  // tile_cost counts stages of 64
+    if (best < 0 || v < bc) best = c, bc = v;
   }
   return best;
 }

@@ -30,11 +30,34 @@ uint16_t f32_to_bf16_bits(float f) {
   return (uint16_t)(u >> 16);
 }
 
+constexpr float kE4m3Most = 448.0f, kE4m3MinScale = 1.17549435e-38f;
+
+// nearest e4m3 value of |f| <= 448 (a rounding over it at most), ties to even
+uint8_t f32_to_e4m3_bits(float f) {
+  uint32_t u;
+  memcpy(&u, &f, 4);
+  const uint8_t sign = (uint8_t)(u >> 31 << 7);
+  u &= 0x7fffffffu;
+  if (u > 0x7f800000u) return 0x7f;
+  if (u < 0x3c800000u) {  // below 2^-6: multiples of 2^-9
+    float a;
+    memcpy(&a, &u, 4);
+    return sign | (uint8_t)nearbyintf(a * 512.0f);
+  }
+  u += 0x7ffffu + ((u >> 20) & 1u);
+  const uint32_t q = (u >> 20) - ((127u - 7u) << 3);
+  return sign | (uint8_t)std::min(q, 0x7eu);
+}
+
 struct Dims {
   int B, L, D, H, F, Nv, Cv, Na, A, No, Co, T, M, dh, Tpad, traj, Nmod;
-  bool bf;
+  bool bf;     // bf16 activations (WAM_BF16, and WAM_FP8 around its projections)
+  bool f8;     // projections of e4m3 blocks
   size_t act;  // bytes per activation element
 };
+
+constexpr int kBlock = 128;  // columns (and weight rows) that share an e4m3 scale
+size_t blocks_of(size_t n) { return (n + kBlock - 1) / kBlock; }
 
 int make_dims(const wam_config* c, Dims* d, std::string* why) {
   auto bad = [&](const char* m) {
@@ -52,12 +75,13 @@ int make_dims(const wam_config* c, Dims* d, std::string* why) {
   if (c->Cv > 16 || c->A > 16 || c->Co > 64) return bad("Cv and A must be <= 16, Co <= 64");
   if (c->D % c->H) return bad("D must be divisible by H");
   if (c->D % 64 || c->D > 2048) return bad("D must be a multiple of 64 and <= 2048");
-  if (c->dtype != WAM_FP32 && c->dtype != WAM_BF16) return bad("dtype must be WAM_FP32 or WAM_BF16");
+  if (c->dtype != WAM_FP32 && c->dtype != WAM_BF16 && c->dtype != WAM_FP8)
+    return bad("dtype must be WAM_FP32, WAM_BF16 or WAM_FP8");
   const int dh = c->D / c->H;
   if (dh != 32 && dh != 64) return bad("head size D/H must be 32 or 64");
-  if (c->dtype == WAM_BF16) {
-    if (dh != 64) return bad("bf16 mode needs head size 64");
-    if (c->F % 128) return bad("bf16 mode needs F a multiple of 128");
+  if (c->dtype != WAM_FP32) {
+    if (dh != 64) return bad("bf16 and fp8 modes need head size 64");
+    if (c->F % 128) return bad("bf16 and fp8 modes need F a multiple of 128");
   } else {
     if (c->F % 64) return bad("F must be a multiple of 64");
   }
@@ -70,7 +94,8 @@ int make_dims(const wam_config* c, Dims* d, std::string* why) {
   d->Tpad = (d->T + 63) / 64 * 64;
   d->traj = c->Nv * c->Cv + c->Na * c->A;
   d->Nmod = c->L * 6 * c->D + 2 * c->D;
-  d->bf = c->dtype == WAM_BF16;
+  d->bf = c->dtype != WAM_FP32;
+  d->f8 = c->dtype == WAM_FP8;
   d->act = d->bf ? 2 : 4;
   return WAM_OK;
 }
@@ -129,6 +154,8 @@ struct DevLayout {
   // activation-typed region
   size_t wmod;                        // [D][Nmod]
   size_t lw0, lw_stride;              // per layer: qkv_wT [3D][D], proj_wT [D][D], fc1_wT [F][D], fc2_wT [D][F]
+  size_t lproj[4];                    // where each starts in its layer
+  size_t lscale[4];                   // WAM_FP8: its scales [ceil(N/128)][ceil(K/128)]
   size_t total;
 };
 
@@ -154,7 +181,20 @@ DevLayout dev_layout(const Dims& d) {
   w.pe = f32((size_t)d.T * D);
   w.wmod = o;
   o = align_up(o + D * d.Nmod * d.act);
-  w.lw_stride = align_up((3 * D * D + D * D + F * D + D * F) * d.act);
+  {
+    const size_t N[4] = {3 * D, D, F, D}, K[4] = {D, D, D, F};
+    const size_t el = d.f8 ? 1 : d.act;
+    size_t l = 0;
+    for (int i = 0; i < 4; ++i) {
+      w.lproj[i] = l;
+      l += N[i] * K[i] * el;
+    }
+    for (int i = 0; i < 4 && d.f8; ++i) {
+      w.lscale[i] = l = align_up(l);
+      l += blocks_of(N[i]) * blocks_of(K[i]) * 4;
+    }
+    w.lw_stride = align_up(l);
+  }
   w.lw0 = o;
   o += w.lw_stride * d.L;
   w.total = o;
@@ -166,6 +206,7 @@ struct WsLayout {
   size_t x_bar, x_r, x_init, x_work, rr_rows, rr_res, tr_rms, total;
   size_t rr_flag, hist_stats, hist_flag, cond_buf;
   size_t gpart_floats;
+  size_t u_s, mlp8, mlp_s;  // WAM_FP8: scales of u (e4m3), blocks of the MLP hidden layer
 };
 
 WsLayout ws_layout(const Dims& d) {
@@ -178,7 +219,7 @@ WsLayout ws_layout(const Dims& d) {
   };
   const size_t MD = (size_t)d.M * d.D;
   w.h = take(MD * 4); w.hq = take(MD * 4); w.pa = take(MD * 4); w.Ra = take(MD * 4);
-  w.u = take(MD * d.act);
+  w.u = take(MD * (d.f8 ? 1 : d.act));
   const size_t head = (size_t)d.B * d.H * d.Tpad * d.dh;
   w.q = take(head * d.act); w.k = take(head * d.act); w.vt = take(head * d.act);
   w.attn = take(MD * d.act);
@@ -201,6 +242,11 @@ WsLayout ws_layout(const Dims& d) {
   w.hist_flag = take((size_t)WAM_MAX_STEPS * 4);
   // condition staging buffer read by captured step graphs
   w.cond_buf = take((size_t)d.B * d.No * d.Co * 4 + 4);
+  if (d.f8) {
+    w.u_s = take((size_t)d.M * blocks_of(d.D) * 4);
+    w.mlp8 = take((size_t)d.M * d.F);
+    w.mlp_s = take((size_t)d.M * blocks_of(d.F) * 4);
+  }
   w.total = o;
   return w;
 }
@@ -242,6 +288,11 @@ struct wam_handle {
   // -1 where the scores have no usable bound
   std::vector<float> attn_mref;
   int attn_variant = WAM_ATTN_AUTO;
+  // layer variants: rotary positions of q and k (pos null: none) and post-norm
+  // gains of the two blocks of every layer (null: none)
+  wam_rotary_args rotary{};
+  double rotary_freq[WAM_MAX_HEAD / 2] = {};
+  const float* post_gains = nullptr;
   bool dev_decision = false;  // RR decision kept on the device (no host round trip per step)
   bool use_graphs = false;    // replay captured step graphs inside wam_replan
   bool capturing = false;
@@ -343,10 +394,102 @@ int embed(wam_t h, const float* x, const float* cond) {
   a.wv = h->W(wl.in_wv); a.bv = h->W(wl.in_bv);
   a.wa = h->W(wl.in_wa); a.ba = h->W(wl.in_ba);
   a.wo = h->W(wl.in_wo); a.bo = h->W(wl.in_bo);
-  a.pe = h->W(wl.pe);
+  a.pe = h->rotary.pos && !h->rotary.keep_table ? nullptr : h->W(wl.pe);
   a.h = h->S(h->ws.h);
   a.B = d.B; a.T = d.T; a.D = d.D; a.Nv = d.Nv; a.Cv = d.Cv; a.Na = d.Na; a.A = d.A; a.No = d.No; a.Co = d.Co;
   HIPCHK(h, launch_embed(a, h->stream));
+  return WAM_OK;
+}
+
+// One projection of layer l: i 0 QKV, 1 attention output, 2 MLP-up, 3 MLP-down.  g
+// has everything but its operands' places: A is the activation, bf16 or float32
+// as the mode has it, or (WAM_FP8) e4m3 with its scales.
+int project(wam_t h, int l, int i, GemmArgs g, const void* A, const float* a_scale) {
+  const DevLayout& wl = h->wl;
+  const size_t lw = wl.lw0 + wl.lw_stride * l;
+  g.A = A;
+  g.W = h->W<char>(lw + wl.lproj[i]);
+  g.role = i;
+  if (h->d.f8) HIPCHK(h, launch_gemm_fp8(g, a_scale, h->W(lw + wl.lscale[i]), h->stream));
+  else HIPCHK(h, launch_gemm(g, h->d.bf, h->stream));
+  return WAM_OK;
+}
+
+// Rows of [M][n] bf16 activations into e4m3 blocks.
+int quantize_rows(wam_t h, const void* x, int n, void* q, float* scale, const int* skip) {
+  const wam_quantize_args a{h->d.M, n, WAM_BF16, 1, x, n, q, n, scale, (int64_t)blocks_of(n)};
+  HIPCHK(h, launch_quantize(a, h->stream, skip));
+  return WAM_OK;
+}
+
+// u = LN(h) (1 + scale) + shift of the rows of h, the input of a projection.  With a
+// block's output y (bf16 or float32, in front of a post-norm): h <- h + gate
+// post(y) first, into h_out, and u only where shift and scale are given.
+int norm_rows(wam_t h, const float* shift, const float* scale, const void* y, const float* post_gain,
+              const float* gate, float* h_out, const int* skip) {
+  const Dims& d = h->d;
+  const WsLayout& ws = h->ws;
+  float* hh = h->S(ws.h);
+  if (!y && !d.f8) {
+    HIPCHK(h, launch_ln_modulate(hh, shift, scale, h->S<char>(ws.u), d.M, d.D, h->cfg.ln_eps, d.bf, h->stream, skip));
+    return WAM_OK;
+  }
+  wam_norm_args a{};
+  a.B = 1;
+  a.T = d.M;
+  a.D = d.D;
+  a.h_dtype = WAM_FP32;
+  a.h = hh;
+  a.h_stride[1] = d.D;
+  a.res_scale = 1.0f;
+  a.eps = h->cfg.ln_eps;
+  if (y) {
+    a.y = y;
+    a.y_dtype = d.bf ? WAM_BF16 : WAM_FP32;
+    a.y_stride[1] = d.D;
+    a.post = WAM_NORM_RMS;
+    a.post_gain = post_gain;
+    a.gate = gate;
+    a.h_out = h_out;
+    a.h_out_stride[1] = d.D;
+  }
+  if (shift) {
+    a.pre = WAM_NORM_LAYER;
+    a.shift = shift;
+    a.scale = scale;
+    a.u = h->S<char>(ws.u);
+    a.u_dtype = d.f8 ? WAM_FP8 : d.bf ? WAM_BF16 : WAM_FP32;
+    a.u_stride[1] = d.D;
+    if (d.f8) {
+      a.u_scale = h->S(ws.u_s);
+      a.u_scale_stride[1] = blocks_of(d.D);
+    }
+  }
+  HIPCHK(h, launch_norm_residual(a, h->stream, skip));
+  return WAM_OK;
+}
+
+// q and k of the layer turned in place by the rows' positions.
+int rotate_heads(wam_t h, const int* skip) {
+  const Dims& d = h->d;
+  wam_rope_args a{};
+  a.B = d.B;
+  a.T = d.T;
+  a.Hq = a.Hk = d.H;
+  a.dh = d.dh;
+  a.dtype = d.bf ? WAM_BF16 : WAM_FP32;
+  a.layout = h->rotary.layout;
+  for (int i = 0; i < 3; ++i) a.sections[i] = h->rotary.sections[i];
+  a.q = a.q_out = h->S<char>(h->ws.q);
+  a.k = a.k_out = h->S<char>(h->ws.k);
+  for (int64_t* st : {a.q_stride, a.k_stride, a.q_out_stride, a.k_out_stride}) {
+    st[0] = (int64_t)d.H * d.Tpad * d.dh;
+    st[1] = d.dh;
+    st[2] = (int64_t)d.Tpad * d.dh;
+  }
+  a.pos = h->rotary.pos;
+  a.freq = h->rotary_freq;
+  HIPCHK(h, launch_rope(a, h->stream, skip));
   return WAM_OK;
 }
 
@@ -354,11 +497,14 @@ int embed(wam_t h, const float* x, const float* cond) {
 // also stores the layer's output h there.  out: when non-null, that epilogue
 // stores the layer's output there instead of in h, which then holds the
 // residual stream before the MLP.
+//
+// With post-norms the two projections in front of the residual only add their
+// bias, and the norm, gate and residual are one pass over the rows together with
+// the LayerNorm of the MLP behind the first one.
 int run_layer(wam_t h, int l, const int* skip = nullptr, float* copy = nullptr, float* out = nullptr) {
   const Dims& d = h->d;
   const DevLayout& wl = h->wl;
   const WsLayout& ws = h->ws;
-  hipStream_t s = h->stream;
   const size_t D = d.D;
   const float* mod = mod_table(h) + (size_t)l * 6 * D;
   const float* lb = h->W(wl.lbias0 + wl.lbias_stride * l);
@@ -368,55 +514,64 @@ int run_layer(wam_t h, int l, const int* skip = nullptr, float* copy = nullptr, 
   const float* fc2_b = fc1_b + d.F;
   const float* q_g = fc2_b + D;
   const float* k_g = q_g + d.dh;
-  const char* lw = h->W<char>(wl.lw0 + wl.lw_stride * l);
-  const char* qkv_w = lw;
-  const char* proj_w = qkv_w + 3 * D * D * d.act;
-  const char* fc1_w = proj_w + D * D * d.act;
-  const char* fc2_w = fc1_w + (size_t)d.F * D * d.act;
   float* hh = h->S(ws.h);
   const double M = d.M;
+  const float* post = h->post_gains ? h->post_gains + (size_t)l * 2 * D : nullptr;
+  // operands of the projections, and where they leave a block's output for its
+  // post-norm: buffers whose content the block has consumed
+  void* u = h->S<char>(ws.u);
+  float* u_s = h->S(ws.u_s);
+  void* attn = h->S<char>(ws.attn);
+  void* y_attn = d.f8 ? attn : u;
+  void* y_mlp = attn;
+  int st;
 
-  HIPCHK(h, launch_ln_modulate(hh, mod + 0 * D, mod + 1 * D, h->S<char>(ws.u), d.M, d.D, h->cfg.ln_eps, d.bf, s,
-                               skip));
+  if ((st = norm_rows(h, mod + 0 * D, mod + 1 * D, nullptr, nullptr, nullptr, nullptr, skip))) return st;
   {
     ProfScope ps(h, WAM_KC_GEMM_QKV, 2.0 * M * D * 3 * D);
     GemmArgs g{};
-    g.A = h->S<char>(ws.u); g.W = qkv_w; g.bias = qkv_b; g.M = d.M; g.N = (int)(3 * D); g.K = (int)D;
-    g.role = 0; g.skip = skip;
+    g.bias = qkv_b; g.M = d.M; g.N = (int)(3 * D); g.K = (int)D;
+    g.skip = skip;
     // projection with q/k RMS-norm and the head-major layout fused in
     g.epi = EPI_QKV;
     g.qkv = QkvOut{h->S<char>(ws.q), h->S<char>(ws.k), h->S<char>(ws.vt), q_g, k_g,
                    d.T, d.Tpad, d.H, d.D, d.dh, h->cfg.qk_norm, h->cfg.ln_eps};
-    HIPCHK(h, launch_gemm(g, d.bf, s));
+    if ((st = project(h, l, 0, g, u, u_s))) return st;
   }
+  if (h->rotary.pos && (st = rotate_heads(h, skip))) return st;
   {
     ProfScope ps(h, WAM_KC_ATTENTION, 4.0 * d.B * (double)d.T * d.T * D);
-    AttnArgs at{h->S<char>(ws.q), h->S<char>(ws.k), h->S<char>(ws.vt), h->S<char>(ws.attn),
+    AttnArgs at{h->S<char>(ws.q), h->S<char>(ws.k), h->S<char>(ws.vt), attn,
                 d.B, d.H, d.T, d.Tpad, d.dh, d.D, skip};
     at.mref = h->attn_mref[l];
     at.bounded = d.bf && at.mref >= 0.f;
     at.variant = h->attn_variant;
-    HIPCHK(h, launch_attention(at, d.bf, s));
+    HIPCHK(h, launch_attention(at, d.bf, h->stream));
   }
+  if (d.f8 && (st = quantize_rows(h, attn, d.D, u, u_s, skip))) return st;
   {
     ProfScope ps(h, WAM_KC_GEMM_PROJ, 2.0 * M * D * D);
-    GemmArgs g{h->S<char>(ws.attn), proj_w, proj_b, mod + 2 * D, hh, d.M, (int)D, (int)D, EPI_GATED_RES, 1,
-               {}, skip, hh};
-    HIPCHK(h, launch_gemm(g, d.bf, s));
+    GemmArgs g{nullptr, nullptr, proj_b, mod + 2 * D, hh, d.M, (int)D, (int)D, EPI_GATED_RES, 1, {}, skip, hh};
+    if (post) g.epi = EPI_BIAS, g.out = y_attn;
+    if ((st = project(h, l, 1, g, d.f8 ? u : attn, u_s))) return st;
   }
-  HIPCHK(h, launch_ln_modulate(hh, mod + 3 * D, mod + 4 * D, h->S<char>(ws.u), d.M, d.D, h->cfg.ln_eps, d.bf, s,
-                               skip));
+  if ((st = norm_rows(h, mod + 3 * D, mod + 4 * D, post ? y_attn : nullptr, post, mod + 2 * D, hh, skip))) return st;
   {
     ProfScope ps(h, WAM_KC_GEMM_FC1, 2.0 * M * D * d.F);
-    GemmArgs g{h->S<char>(ws.u), fc1_w, fc1_b, nullptr, h->S<char>(ws.mlp), d.M, d.F, (int)D, EPI_BIAS_GELU, 2,
-               {}, skip};
-    HIPCHK(h, launch_gemm(g, d.bf, s));
+    GemmArgs g{nullptr, nullptr, fc1_b, nullptr, h->S<char>(ws.mlp), d.M, d.F, (int)D, EPI_BIAS_GELU, 2, {}, skip};
+    if ((st = project(h, l, 2, g, u, u_s))) return st;
   }
+  if (d.f8 && (st = quantize_rows(h, h->S<char>(ws.mlp), d.F, h->S<char>(ws.mlp8), h->S(ws.mlp_s), skip))) return st;
   {
     ProfScope ps(h, WAM_KC_GEMM_FC2, 2.0 * M * D * d.F);
-    GemmArgs g{h->S<char>(ws.mlp), fc2_w, fc2_b, mod + 5 * D, out ? out : hh, d.M, (int)D, d.F, EPI_GATED_RES, 3,
-               {}, skip, hh, copy};
-    HIPCHK(h, launch_gemm(g, d.bf, s));
+    GemmArgs g{nullptr, nullptr, fc2_b, mod + 5 * D, out ? out : hh, d.M, (int)D, d.F, EPI_GATED_RES, 3, {}, skip,
+               hh, copy};
+    if (post) g.epi = EPI_BIAS, g.out = y_mlp;
+    if ((st = project(h, l, 3, g, h->S<char>(d.f8 ? ws.mlp8 : ws.mlp), h->S(ws.mlp_s)))) return st;
+  }
+  if (post) {
+    if ((st = norm_rows(h, nullptr, nullptr, y_mlp, post + D, mod + 5 * D, out ? out : hh, skip))) return st;
+    if (copy) HIPCHK(h, launch_copy_f32(out ? out : hh, copy, (int64_t)d.M * d.D, h->stream));
   }
   return WAM_OK;
 }
@@ -853,6 +1008,27 @@ int wam_init(const wam_config* cfg, const float* hw, size_t n_hw, void* dev_weig
         for (size_t r = r0; r < std::min(rows, r0 + tb); ++r)
           for (size_t c = c0; c < std::min(cols, c0 + tb); ++c) put_act(dst_off, c * rows + r, src[r * cols + c]);
   };
+  // the same into e4m3 blocks of 128 x 128 with their scales, as wam_quantize_fp8
+  // makes them
+  auto put_blocks = [&](size_t q_off, size_t s_off, const float* src, size_t rows, size_t cols) {
+    uint8_t* q = reinterpret_cast<uint8_t*>(buf.data() + q_off);
+    float* s = reinterpret_cast<float*>(buf.data() + s_off);
+    for (size_t c0 = 0; c0 < cols; c0 += kBlock)
+      for (size_t r0 = 0; r0 < rows; r0 += kBlock) {
+        const size_t c1 = std::min(cols, c0 + kBlock), r1 = std::min(rows, r0 + kBlock);
+        float most = 0.f;
+        bool nan = false;
+        for (size_t r = r0; r < r1; ++r)
+          for (size_t c = c0; c < c1; ++c) {
+            most = std::max(most, fabsf(src[r * cols + c]));
+            nan = nan || src[r * cols + c] != src[r * cols + c];
+          }
+        const float scale = nan ? NAN : most == 0.f ? 1.0f : std::max(most / kE4m3Most, kE4m3MinScale);
+        s[c0 / kBlock * blocks_of(rows) + r0 / kBlock] = scale;
+        for (size_t r = r0; r < r1; ++r)
+          for (size_t c = c0; c < c1; ++c) q[c * rows + r] = f32_to_e4m3_bits(src[r * cols + c] / scale);
+      }
+  };
   for (int l = 0; l < d.L; ++l) {
     const float* L0 = hw + hl.layer0 + hl.layer_stride * l;
     // modulation: rows k of [D][6D] into the shared [D][Nmod] matrix
@@ -873,10 +1049,12 @@ int wam_init(const wam_config* cfg, const float* hw, size_t n_hw, void* dev_weig
     }
     h->attn_mref.push_back(mref);
     const size_t lw = wl.lw0 + wl.lw_stride * l;
-    put_T(lw, L0 + hl.qkv_w, D, 3 * D);
-    put_T(lw + 3 * D * D * d.act, L0 + hl.proj_w, D, D);
-    put_T(lw + 4 * D * D * d.act, L0 + hl.fc1_w, D, F);
-    put_T(lw + (4 * D * D + F * D) * d.act, L0 + hl.fc2_w, F, D);
+    const size_t src[4] = {hl.qkv_w, hl.proj_w, hl.fc1_w, hl.fc2_w};
+    const size_t K[4] = {D, D, D, F}, N[4] = {3 * D, D, F, D};
+    for (int i = 0; i < 4; ++i) {
+      if (d.f8) put_blocks(lw + wl.lproj[i], lw + wl.lscale[i], L0 + src[i], K[i], N[i]);
+      else put_T(lw + wl.lproj[i], L0 + src[i], K[i], N[i]);
+    }
   }
   for (size_t r = 0; r < D; ++r)
     for (size_t c = 0; c < 2 * D; ++c)
@@ -959,6 +1137,41 @@ int wam_set_option(wam_t h, int option, int value) {
     default:
       return fail(h, WAM_E_ARG, "unknown option");
   }
+}
+
+int wam_set_rotary(wam_t h, const wam_rotary_args* a) {
+  if (!h) return WAM_E_ARG;
+  if (int st_ = check_not_pending(h)) return st_;
+  if (a) {
+    if (!a->pos) return fail(h, WAM_E_ARG, "null rotary positions");
+    if (a->layout != WAM_ROPE_HALVES && a->layout != WAM_ROPE_PAIRS) return fail(h, WAM_E_ARG, "unknown rotary layout");
+    int64_t pairs = 0;
+    for (int i = 0; i < 3; ++i) {
+      if (a->sections[i] < 0) return fail(h, WAM_E_ARG, "rotary sections must be >= 0");
+      pairs += a->sections[i];
+    }
+    if (pairs < 1 || 2 * pairs > h->d.dh)
+      return fail(h, WAM_E_SHAPE, "rotary sections need 1 <= pairs <= head size / 2");
+    if (!a->freq) return fail(h, WAM_E_ARG, "null rotary frequencies");
+    for (int i = 0; i < pairs; ++i) h->rotary_freq[i] = a->freq[i];
+    h->rotary = *a;
+    h->rotary.freq = nullptr;  // copied
+  } else {
+    h->rotary = wam_rotary_args{};
+  }
+  h->layer_valid = false;  // a retained layer state belongs to the layers as they were
+  drop_graphs(h);
+  return WAM_OK;
+}
+
+int wam_set_post_norm(wam_t h, const float* gains) {
+  if (!h) return WAM_E_ARG;
+  if (int st_ = check_not_pending(h)) return st_;
+  if (reinterpret_cast<uintptr_t>(gains) % 4) return fail(h, WAM_E_ARG, "post-norm gains must be aligned to floats");
+  h->post_gains = gains;
+  h->layer_valid = false;
+  drop_graphs(h);
+  return WAM_OK;
 }
 
 int wam_set_schedule(wam_t h, const float* sigmas, int K) {

@@ -126,6 +126,7 @@ int noalloc_fail(int code, const char* msg);
 
 // ---------------------------------------------------------------- GEMM
 enum GemmEpilogue : int {
+  EPI_BIAS = 0,       // out[m,n] = acc + bias[n]                       (act type)
   EPI_BIAS_GELU = 1,  // out[m,n] = gelu(acc + bias[n])                 (act type)
   EPI_GATED_RES = 2,  // out[m,n] = res[m,n] + gate[n] * (acc + bias[n]) (float32)
   EPI_QKV = 3,        // q,k RMS-normalised per head -> [B*H][Tpad][dh], v -> [B*H][dh][Tpad]
@@ -158,6 +159,9 @@ struct GemmArgs {
 };
 
 hipError_t launch_gemm(const GemmArgs& a, bool bf16_mode, hipStream_t s);
+// The same projections of e4m3 operands (rows contiguous) with float32 scales
+// [M][ceil(K/128)] and [ceil(N/128)][ceil(K/128)]; act type bf16
+hipError_t launch_gemm_fp8(const GemmArgs& a, const float* a_scale, const float* w_scale, hipStream_t s);
 
 // ---------------------------------------------------------------- attention
 struct AttnArgs {
@@ -199,7 +203,7 @@ struct EmbedArgs {
   const float* wv; const float* bv;  // [Cv][D], [D]
   const float* wa; const float* ba;  // [A][D], [D]
   const float* wo; const float* bo;  // [Co][D], [D]
-  const float* pe;    // [T][D] position embedding
+  const float* pe;    // [T][D] position embedding, or null
   float* h;           // [B][T][D]
   int B, T, D, Nv, Cv, Na, A, No, Co;
 };
@@ -210,6 +214,12 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t s);
 hipError_t launch_ln_modulate(const float* h, const float* shift, const float* scale, void* u,
                               int rows, int D, float eps, bool bf16_out, hipStream_t s,
                               const int* skip = nullptr);
+
+// The layer operators of wam.h without their checks.  skip: device flag; when
+// non-null and set the launch does nothing
+hipError_t launch_rope(const wam_rope_args& a, hipStream_t s, const int* skip = nullptr);
+hipError_t launch_norm_residual(const wam_norm_args& a, hipStream_t s, const int* skip = nullptr);
+hipError_t launch_quantize(const wam_quantize_args& a, hipStream_t s, const int* skip = nullptr);
 
 struct FinalArgs {
   const float* h;      // [B][T][D]

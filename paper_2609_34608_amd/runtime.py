@@ -44,7 +44,7 @@ def host_weight_order(n_layers: int) -> list[str]:
 
 def make_config(B, L, D, H, F, Nv, Cv, Na, A, No, Co, dtype="bf16", qk_norm=True, ln_eps=1e-6) -> abi.WamConfig:
     return abi.WamConfig(B=B, L=L, D=D, H=H, F=F, Nv=Nv, Cv=Cv, Na=Na, A=A, No=No, Co=Co,
-                       dtype=abi.WAM_BF16 if dtype == "bf16" else abi.WAM_FP32, qk_norm=int(bool(qk_norm)),
+                       dtype={"bf16": abi.WAM_BF16, "fp8": abi.WAM_FP8}.get(dtype, abi.WAM_FP32), qk_norm=int(bool(qk_norm)),
                        ln_eps=ln_eps)
 
 
@@ -153,6 +153,35 @@ class WamModel:
         self._check(self.lib.wam_set_schedule(self.h, s.ctypes.data_as(C.POINTER(C.c_float)), s.size - 1),
                     "wam_set_schedule")
         self.K = s.size - 1
+
+    def set_rotary(self, pos, sections=None, freq=None, layout="halves", keep_table=False):
+        """Rotary positions of the rows (wam_set_rotary): pos float32 [T, 3] on the
+        device, one frequency per pair; pos None: back to the additive table alone."""
+        if pos is None:
+            self._check(self.lib.wam_set_rotary(self.h, None), "wam_set_rotary")
+            self._pos = None
+            return
+        T = self.cfg.Nv + self.cfg.Na + self.cfg.No
+        if tuple(pos.shape) != (T, 3):
+            raise WamError(f"set_rotary: pos must be [{T}, 3]")
+        ladder = np.ascontiguousarray(freq, np.float64)
+        if len(sections) != 3 or ladder.shape != (sum(sections),):
+            raise WamError("set_rotary: needs three sections and one frequency per pair")
+        self._enter()
+        a = abi.WamRotaryArgs(pos=_ptr(pos), sections=(C.c_int32 * 3)(*sections),
+                              layout=_choice(_LAYOUTS, layout, "set_rotary: layout"), freq=ladder.ctypes.data,
+                              keep_table=int(bool(keep_table)))
+        self._check(self.lib.wam_set_rotary(self.h, C.byref(a)), "wam_set_rotary")
+        self._pos = pos  # read by every step
+
+    def set_post_norm(self, gains):
+        """RMS post-norms of both blocks of every layer (wam_set_post_norm): gains
+        float32 [L, 2, D] on the device, or None."""
+        if gains is not None and tuple(gains.shape) != (self.cfg.L, 2, self.cfg.D):
+            raise WamError(f"set_post_norm: gains must be {(self.cfg.L, 2, self.cfg.D)}")
+        self._enter()
+        self._check(self.lib.wam_set_post_norm(self.h, _ptr(gains)), "wam_set_post_norm")
+        self._gains = gains  # read by every step
 
     def velocity(self, k, x, cond, v_out=None, rr=None):
         self._enter()

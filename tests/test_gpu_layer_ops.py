@@ -343,8 +343,9 @@ TILES = [
     (0, 9864, 1071, 200), (0, 5522, 2075, 512), (0, 9798, 1093, 1216),    # 256x256
     (0, 599, 4880, 200), (0, 8388, 335, 333), (0, 4942, 597, 640),        # 64x128
     (0, 8302, 38, 333), (0, 8577, 40, 200), (0, 9141, 33, 512),           # 64x64
-    (0, 6818, 129, 333), (0, 8617, 99, 512), (0, 6740, 131, 1216),        # 96x64
+    (0, 8739, 129, 200), (0, 8858, 130, 512), (0, 8347, 134, 333),        # 96x64
     (0, 36, 31, 333), (0, 33, 32, 1216),                                  # 32x32
+    (0, 6649, 142, 333), (0, 6708, 129, 512), (0, 290, 4111, 2000),       # 32x64
     (1, 8949, 651, 200), (1, 8209, 687, 333), (1, 4042, 1432, 512),       # 128x128
     (1, 9513, 390, 200), (1, 8321, 449, 512), (1, 6139, 654, 640),        # 160x128
     (1, 6218, 769, 200), (1, 8250, 521, 512), (1, 962, 4623, 1216),       # 96x128

@@ -118,7 +118,8 @@ class WamMatmulArgs(C.Structure):
     _fields_ = [("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("out_dtype", C.c_int32), ("act", C.c_int32),
                 ("a", C.c_void_p), ("a_stride", C.c_int64), ("a_scale", C.c_void_p), ("a_scale_stride", C.c_int64),
                 ("w", C.c_void_p), ("w_stride", C.c_int64), ("w_scale", C.c_void_p), ("w_scale_stride", C.c_int64),
-                ("bias", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64)]
+                ("bias", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64), ("out_scale", C.c_void_p),
+                ("out_scale_stride", C.c_int64)]
 
 
 EXPORTS = {

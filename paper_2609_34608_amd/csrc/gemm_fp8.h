@@ -56,8 +56,10 @@ struct Fp8Operands {
 
 struct Fp8Out {
   const float* bias;  // or null
-  void* out;          // bf16, or float32 of an EXACT product
+  void* out;          // bf16, float32 of an EXACT product, or e4m3 with
   int64_t ld;
+  float* scale;       // a scale per row and 128 columns
+  int64_t ldscale;
 };
 
 // bf16 values of the bytes 8 t .. 8 t + 7 of a lane's operand
@@ -73,8 +75,9 @@ __device__ __forceinline__ bf16x8 to_bf16(const i32x8& v, int t) {
   return r;
 }
 
-// The product of one block's tile; epilogue(acc, m, n, lane) takes a wave's
-// accumulators, whose rows start at m and columns at n.  WIDE: rows further apart
+// The product of one block's tile; epilogue(acc, m, n, lane, lds) takes a wave's
+// accumulators, whose rows start at m and columns at n (lds: the stages, which no
+// load writes any more but other waves may still read).  WIDE: rows further apart
 // than 32-bit offsets inside a tile reach.
 template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool WIDE, typename EPILOGUE>
 __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epilogue) {
@@ -109,7 +112,7 @@ __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epi
   // Load j of this wave fills LDS rows 8 (wid + NW j) .. + 7 of the stage, lane l
   // the chunk l % 8 of row l / 8, i.e. global chunk (l % 8) ^ swizzle (the same
   // for every j).  Rows past M or N read the last one (never stored); chunks past
-  // K read the row's last one and are cleared in LDS before use.
+  // K read the row's last one and are cleared on their way into the MFMAs.
   const uint8_t* abase = p.a + (int64_t)m0 * p.lda;
   const uint8_t* wbase = p.w + (int64_t)n0 * p.ldw;
   const uint32_t col = ((lane % 8) ^ chunk_swizzle(lane / 8)) * 16;
@@ -162,15 +165,36 @@ __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epi
   const int lr = lane % 16, lg = lane / 16;
   const int ch0 = (lg ^ chunk_swizzle(lr)) * 16, ch1 = ((lg + 4) ^ chunk_swizzle(lr)) * 16;
   const int arow = (wm * WM + lr) * BK, wrow = (BM + wn * WN + tile_row<kPaired<TN>>(0, lr)) * BK;
-  auto operand = [&](const uint8_t* row) __attribute__((always_inline)) {
-    const i32x4 x = *reinterpret_cast<const i32x4*>(row + ch0), y = *reinterpret_cast<const i32x4*>(row + ch1);
+  // TAIL: chunks past K of the last stage count as zero, in both operands (either may
+  // hold a NaN there); the bytes past K of a chunk that it ends in are cleared in
+  // LDS (clear_chunk).
+  const int used = p.K - (nk - 1) * BK;
+  auto operand = [&](const uint8_t* row, auto TAIL) __attribute__((always_inline)) {
+    i32x4 x = *reinterpret_cast<const i32x4*>(row + ch0), y = *reinterpret_cast<const i32x4*>(row + ch1);
+    if constexpr (decltype(TAIL)::value) {
+      x &= 16 * lg < used ? -1 : 0;
+      y &= 64 + 16 * lg < used ? -1 : 0;
+    }
     return i32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+  };
+  auto clear_chunk = [&](int s) __attribute__((always_inline)) {
+    for (int row = tid; row < ROWS; row += NW * 64) {
+      const int sw = row < BM ? chunk_swizzle(row) : weight_swizzle<TN>(row - BM);
+      i32x4* q = reinterpret_cast<i32x4*>(&sm[s][row * BK + ((used / 16) ^ sw) * 16]);
+      i32x4 v = *q;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int keep = min(max(used % 16 - 4 * r, 0), 4);  // bytes of this word
+        v[r] &= (int)(0xffffffffull >> (32 - 8 * keep));
+      }
+      *q = v;
+    }
+    __syncthreads();
   };
   // The multiply-adds of row tile i run behind the MFMAs of row tile i + 1, one
   // MFMA and four multiply-adds in turn, so that neither unit waits for the other.
   // load(i) requests part of a later stage before the MFMAs of row tile i.
-  auto compute = [&](auto S, auto load) __attribute__((always_inline)) {
-    constexpr int s = decltype(S)::value;
+  auto compute = [&](int s, auto TAIL, auto load) __attribute__((always_inline)) {
     const float* sc = reinterpret_cast<const float*>(&sm[s][SCALES]);
     const float sw = sc[BM + wn * WN];
     float f[TM];
@@ -178,7 +202,7 @@ __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epi
     for (int i = 0; i < TM; ++i) f[i] = sc[wm * WM + i * 16 + lr] * sw;
     i32x8 wf[TN];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) wf[j] = operand(&sm[s][wrow + tile_row<kPaired<TN>>(j, 0) * BK]);
+    for (int j = 0; j < TN; ++j) wf[j] = operand(&sm[s][wrow + tile_row<kPaired<TN>>(j, 0) * BK], TAIL);
     if constexpr (EXACT) {
       bf16x8 wb[TN][4];
 #pragma unroll
@@ -188,7 +212,7 @@ __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epi
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         load(i);
-        const i32x8 af = operand(&sm[s][arow + i * 16 * BK]);
+        const i32x8 af = operand(&sm[s][arow + i * 16 * BK], TAIL);
         bf16x8 ab[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) ab[t] = to_bf16(af, t);
@@ -205,10 +229,10 @@ __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epi
       const f32x4 z = {0.f, 0.f, 0.f, 0.f};
       f32x4 v[2][TN];
       i32x8 af[2];
-      af[0] = operand(&sm[s][arow]);
+      af[0] = operand(&sm[s][arow], TAIL);
 #pragma unroll
       for (int i = 0; i <= TM; ++i) {
-        if (i + 1 < TM) af[(i + 1) & 1] = operand(&sm[s][arow + (i + 1) * 16 * BK]);
+        if (i + 1 < TM) af[(i + 1) & 1] = operand(&sm[s][arow + (i + 1) * 16 * BK], TAIL);
         if (i < TM) load(i);
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -226,26 +250,6 @@ __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epi
       }
     }
   };
-  // clears the bytes past K of the last stage, in both operands (either may hold
-  // a NaN there)
-  auto clear_tail = [&](auto S) __attribute__((always_inline)) {
-    constexpr int s = decltype(S)::value;
-    const int used = p.K - (nk - 1) * BK;
-    for (int c = tid; c < ROWS * 8; c += NW * 64) {
-      const int row = c / 8;
-      const int at = ((c % 8) ^ (row < BM ? chunk_swizzle(row) : weight_swizzle<TN>(row - BM))) * 16;  // first of K
-      if (at + 16 <= used) continue;
-      i32x4* q = reinterpret_cast<i32x4*>(&sm[s][row * BK + (c % 8) * 16]);
-      i32x4 v = *q;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int keep = min(max(used - at - 4 * r, 0), 4);  // bytes of this word
-        v[r] = keep == 4 ? v[r] : keep == 0 ? 0 : v[r] & ((1 << (8 * keep)) - 1);
-      }
-      *q = v;
-    }
-    __syncthreads();
-  };
   // One K step on stage slot J: this wave's loads of stage kt have landed (the ST - 2
   // newer stages may still be in flight) and its LDS reads are done; after the
   // barrier everyone's are, and the slot read in the previous step is free for
@@ -254,36 +258,137 @@ __device__ __forceinline__ void gemm_fp8_body(const Fp8Operands& p, EPILOGUE epi
   // its turn before its first MFMA (M = 10176, N = 1536, K = 6144: 100 -> 90 us).
   // Waves that have passed the barrier go before those that have not (90 -> 87 us).
   // Past the last stage the loads repeat it into slots nobody reads again.
-  auto step = [&](auto J, int kt, bool tail) __attribute__((always_inline)) {
-    constexpr int j = decltype(J)::value;
+  auto enter = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_s_waitcnt(waitcnt_vm_lgkm0((ST - 2) * LPS));
     compiler_fence();
     __builtin_amdgcn_s_barrier();
     compiler_fence();
     __builtin_amdgcn_s_setprio(1);
-    if (tail) clear_tail(J);
-    compute(J, [&](int i) __attribute__((always_inline)) {
+  };
+  auto step = [&](auto J, int kt) __attribute__((always_inline)) {
+    constexpr int j = decltype(J)::value;
+    enter();
+    compute(j, std::false_type{}, [&](int i) __attribute__((always_inline)) {
       issue(std::integral_constant<int, (j + ST - 1) % ST>{}, min(kt + ST - 1, nk - 1), i * LPT,
             i < TM - 1 ? (i + 1) * LPT : LPS);
     });
   };
 
   static_for<ST - 1>([&](auto P) __attribute__((always_inline)) { issue(P, min((int)decltype(P)::value, nk - 1), 0, LPS); });
-  // whole rounds of the slots, then what is left; a ragged last stage is among the
-  // latter, out of the main loop
-  const bool ragged = p.K % BK != 0;
-  const int nfull = (nk - ragged) / ST * ST;
-  for (int kt0 = 0; kt0 < nfull; kt0 += ST)
-    static_for<ST>([&](auto J) __attribute__((always_inline)) { step(J, kt0 + decltype(J)::value, false); });
-  static_for<ST>([&](auto J) __attribute__((always_inline)) {
-    const int kt = nfull + decltype(J)::value;
-    if (kt < nk) step(J, kt, ragged && kt == nk - 1);
+  // whole rounds of the slots, what is left, and a last stage that K cuts off
+  const int whole = nk - (p.K % BK != 0);
+  const int rounds = whole / ST * ST;
+  for (int kt0 = 0; kt0 < rounds; kt0 += ST)
+    static_for<ST>([&](auto J) __attribute__((always_inline)) { step(J, kt0 + decltype(J)::value); });
+  static_for<ST - 1>([&](auto J) __attribute__((always_inline)) {
+    const int kt = rounds + decltype(J)::value;
+    if (kt < whole) step(J, kt);
   });
+  if (whole < nk) {
+    enter();
+    const int s = whole % ST;
+    if (used % 16) clear_chunk(s);
+    compute(s, std::true_type{}, [](int) {});
+  }
   // no load may still be writing this block's LDS when the block retires
   __builtin_amdgcn_s_waitcnt(0);
 
-  epilogue(acc, m0 + wm * WM, n0 + wn * WN, lane);
+  epilogue(acc, m0 + wm * WM, n0 + wn * WN, lane, &sm[0][0]);
+}
+
+// bias of a lane's columns (zeros without one; columns past N take the last)
+template <int TN, int J, int W>
+__device__ __forceinline__ void load_bias(float (&bias)[J][W], const float* from, int nb, int lg, int N) {
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int r = 0; r < W; ++r) bias[j][r] = 0.f;
+  if (from)
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int r = 0; r < W; ++r) bias[j][r] = from[min(nb + tile_col<kPaired<TN>>(j * (TN / J), lg) + r, N - 1)];
+}
+
+// Bias, activation and 8-bit blocks of the result.  A block's 128 columns are those
+// of two neighbouring waves (64 each), which meet in LDS: the largest magnitude of
+// a row's columns over the lane's values, the row's four lanes, the two waves.  The
+// values themselves never leave the registers unrounded.
+template <int TN, int TM, int NW, bool GELU>
+__device__ __forceinline__ void store_blocks(const Fp8Operands& p, const Fp8Out& o, f32x4 (&acc)[TN][TM], int mb,
+                                             int nb, int lane, uint8_t* lds) {
+  static_assert(TN == 4, "two waves to a block");
+  const int lr = lane % 16, lg = lane / 16, wid = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  uint32_t(*top)[TM * 16] = reinterpret_cast<uint32_t(*)[TM * 16]>(lds);
+  constexpr int W = 8;
+  const bool ragged = nb + TN * 16 > p.N;
+  float bias[TN / 2][W];
+  load_bias<TN>(bias, o.bias, nb, lg, p.N);
+  __syncthreads();  // the stages have been read
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float v = acc[j][i][r] + bias[j / 2][j % 2 * 4 + r];
+        if (GELU) v = gelu_tanh_f(v);
+        acc[j][i][r] = v;
+        most = max(most, abs_bits(v));
+      }
+    if (ragged) {  // columns past N are no part of their block
+      most = 0;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (nb + tile_col<true>(j, lg) + r < p.N) most = max(most, abs_bits(acc[j][i][r]));
+    }
+    most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32, 64));
+    if (lg == 0) top[wid][i * 16 + lr] = most;
+  }
+  __syncthreads();
+  struct __attribute__((packed, aligned(1))) Row {
+    uint32_t v[2];
+  };
+  uint8_t* out = static_cast<uint8_t*>(o.out);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = mb + i * 16 + lr;
+    const float s = block_scale(max(top[wid][i * 16 + lr], top[wid ^ 1][i * 16 + lr])), rs = 1.0f / s;
+    if (m >= p.M) continue;
+    if (lg == 0 && wid % 2 == 0 && nb < p.N) o.scale[m * o.ldscale + nb / kScaleBlock] = s;
+    uint8_t* row = out + m * o.ld + nb;
+#pragma unroll
+    for (int j = 0; j < TN; j += 2) {
+      const int c = tile_col<true>(j, lg);
+      Row x;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const f32x4 v = acc[j + w][i];
+        x.v[w] = pack_e4m3(divide_by(v[0], s, rs), divide_by(v[1], s, rs), divide_by(v[2], s, rs),
+                           divide_by(v[3], s, rs));
+      }
+      if (nb + c + W <= p.N) *reinterpret_cast<Row*>(row + c) = x;
+    }
+  }
+  if (!ragged || p.N % W == 0) return;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = mb + i * 16 + lr;
+    const float s = block_scale(max(top[wid][i * 16 + lr], top[wid ^ 1][i * 16 + lr]));
+#pragma unroll
+    for (int j = 0; j < TN; j += 2) {
+      const int n = nb + tile_col<true>(j, lg);
+      if (m >= p.M || n >= p.N || n + W <= p.N) continue;
+#pragma unroll
+      for (int c = 0; c < W; ++c)
+        if (n + c < p.N) out[m * o.ld + n + c] = to_e4m3(acc[j + c / 4][i][c % 4] / s);
+    }
+  }
 }
 
 // Bias, activation and rounding of a wave's accumulators into a result of any row
@@ -301,15 +406,7 @@ __device__ __forceinline__ void store_product(const Fp8Operands& p, const Fp8Out
     T v[W];
   };
   float bias[TN / G][W];
-#pragma unroll
-  for (int j = 0; j < TN / G; ++j)
-#pragma unroll
-    for (int r = 0; r < W; ++r) bias[j][r] = 0.f;
-  if (o.bias)
-#pragma unroll
-    for (int j = 0; j < TN / G; ++j)
-#pragma unroll
-      for (int r = 0; r < W; ++r) bias[j][r] = o.bias[min(nb + tile_col<kPaired<TN>>(j * G, lg) + r, p.N - 1)];
+  load_bias<TN>(bias, o.bias, nb, lg, p.N);
   auto value = [&](int j, int i, int r) __attribute__((always_inline)) {
     const float v = acc[j * G + r / 4][i][r % 4] + bias[j][r];
     return static_cast<T>(GELU ? gelu_tanh_f(v) : v);
@@ -348,8 +445,18 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool GELU, bool 
 __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, Fp8Out o) {
   constexpr int TM = BM / WGM / 16, TN = BN / WGN / 16;
   gemm_fp8_body<BM, BN, WGM, WGN, ST, EXACT, WIDE>(
-      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane) __attribute__((always_inline)) {
+      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane, uint8_t*) __attribute__((always_inline)) {
         store_product<TN, TM, EXACT, GELU>(p, o, acc, m, n, lane);
+      });
+}
+
+template <int BM, int BN, int WGM, int WGN, int ST, bool GELU>
+__global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_blocks_kernel(Fp8Operands p, Fp8Out o, const int* skip) {
+  constexpr int TM = BM / WGM / 16, TN = BN / WGN / 16;
+  if (skip && *skip) return;
+  gemm_fp8_body<BM, BN, WGM, WGN, ST, false, false>(
+      p, [&](f32x4(&acc)[TN][TM], int m, int n, int lane, uint8_t* lds) __attribute__((always_inline)) {
+        store_blocks<TN, TM, WGM * WGN, GELU>(p, o, acc, m, n, lane, lds);
       });
 }
 
@@ -360,7 +467,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_layer_kernel(Fp8Operan
   static_assert(EPI != EPI_QKV || TN == 4, "QKV epilogue needs whole heads per wave");
   if (g.skip && *g.skip) return;
   gemm_fp8_body<BM, BN, WGM, WGN, ST, false, false>(
-      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane) __attribute__((always_inline)) {
+      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane, uint8_t*) __attribute__((always_inline)) {
         if (n < p.N) store_tile<bf16, EPI, 64, TN, TM, kPaired<TN>>(g, acc, m, n, lane);
       });
 }

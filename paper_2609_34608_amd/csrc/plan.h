@@ -110,14 +110,16 @@ constexpr TileCfg kFp8ExactCfgs[] = {
     {32, 32, 2, 2, 4, 128, 4, {0.21f, 0.27f, 0.36f, 0.43f}, {2.59f, 2.97f, 3.37f, 1.56f}},
 };
 
-// qkv: only tiles whose waves take whole heads of 64 columns
+// qkv: only tiles whose waves take whole heads of 64 columns; blocks: 8-bit results,
+// only tiles of whole scale blocks
+enum Fp8Result : int { FP8_PLAIN = 0, FP8_QKV = 1, FP8_BLOCKS = 2 };
 template <int NC>
-int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K, bool qkv = false) {
+int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K, Fp8Result result = FP8_PLAIN) {
   int best = -1;
   double bc = 0.0;
   for (int c = 0; c < NC; ++c) {
     const TileCfg& t = cfgs[c];
-    if (qkv && t.bn / t.wgn != 64) continue;
+    if ((result == FP8_QKV && t.bn / t.wgn != 64) || (result == FP8_BLOCKS && t.bn % 128)) continue;
     const double v = tile_cost(t, M, N, (K + 127) / 128 * 64);  // tile_cost counts stages of 64
     if (best < 0 || v < bc) best = c, bc = v;
   }

@@ -206,7 +206,7 @@ struct WsLayout {
   size_t x_bar, x_r, x_init, x_work, rr_rows, rr_res, tr_rms, total;
   size_t rr_flag, hist_stats, hist_flag, cond_buf;
   size_t gpart_floats;
-  size_t u_s, mlp8, mlp_s;  // WAM_FP8: scales of u (e4m3), blocks of the MLP hidden layer
+  size_t u_s, mlp_s;  // WAM_FP8: scales of u and of the MLP hidden layer, both e4m3
 };
 
 WsLayout ws_layout(const Dims& d) {
@@ -223,7 +223,7 @@ WsLayout ws_layout(const Dims& d) {
   const size_t head = (size_t)d.B * d.H * d.Tpad * d.dh;
   w.q = take(head * d.act); w.k = take(head * d.act); w.vt = take(head * d.act);
   w.attn = take(MD * d.act);
-  w.mlp = take((size_t)d.M * d.F * d.act);
+  w.mlp = take((size_t)d.M * d.F * (d.f8 ? 1 : d.act));
   w.e = take(kTimeDim * 4); w.a1 = take(d.D * 4); w.sc = take(d.D * 4);
   // modulation table of every schedule step (a pure function of sigma_k)
   w.mod = take((size_t)WAM_MAX_STEPS * d.Nmod * 4);
@@ -244,7 +244,6 @@ WsLayout ws_layout(const Dims& d) {
   w.cond_buf = take((size_t)d.B * d.No * d.Co * 4 + 4);
   if (d.f8) {
     w.u_s = take((size_t)d.M * blocks_of(d.D) * 4);
-    w.mlp8 = take((size_t)d.M * d.F);
     w.mlp_s = take((size_t)d.M * blocks_of(d.F) * 4);
   }
   w.total = o;
@@ -403,14 +402,15 @@ int embed(wam_t h, const float* x, const float* cond) {
 
 // One projection of layer l: i 0 QKV, 1 attention output, 2 MLP-up, 3 MLP-down.  g
 // has everything but its operands' places: A is the activation, bf16 or float32
-// as the mode has it, or (WAM_FP8) e4m3 with its scales.
-int project(wam_t h, int l, int i, GemmArgs g, const void* A, const float* a_scale) {
+// as the mode has it, or (WAM_FP8) e4m3 with its scales; there the MLP-up's result is
+// e4m3 too, with its scales in out_scale.
+int project(wam_t h, int l, int i, GemmArgs g, const void* A, const float* a_scale, float* out_scale = nullptr) {
   const DevLayout& wl = h->wl;
   const size_t lw = wl.lw0 + wl.lw_stride * l;
   g.A = A;
   g.W = h->W<char>(lw + wl.lproj[i]);
   g.role = i;
-  if (h->d.f8) HIPCHK(h, launch_gemm_fp8(g, a_scale, h->W(lw + wl.lscale[i]), h->stream));
+  if (h->d.f8) HIPCHK(h, launch_gemm_fp8(g, a_scale, h->W(lw + wl.lscale[i]), out_scale, h->stream));
   else HIPCHK(h, launch_gemm(g, h->d.bf, h->stream));
   return WAM_OK;
 }
@@ -559,15 +559,14 @@ int run_layer(wam_t h, int l, const int* skip = nullptr, float* copy = nullptr, 
   {
     ProfScope ps(h, WAM_KC_GEMM_FC1, 2.0 * M * D * d.F);
     GemmArgs g{nullptr, nullptr, fc1_b, nullptr, h->S<char>(ws.mlp), d.M, d.F, (int)D, EPI_BIAS_GELU, 2, {}, skip};
-    if ((st = project(h, l, 2, g, u, u_s))) return st;
+    if ((st = project(h, l, 2, g, u, u_s, h->S(ws.mlp_s)))) return st;
   }
-  if (d.f8 && (st = quantize_rows(h, h->S<char>(ws.mlp), d.F, h->S<char>(ws.mlp8), h->S(ws.mlp_s), skip))) return st;
   {
     ProfScope ps(h, WAM_KC_GEMM_FC2, 2.0 * M * D * d.F);
     GemmArgs g{nullptr, nullptr, fc2_b, mod + 5 * D, out ? out : hh, d.M, (int)D, d.F, EPI_GATED_RES, 3, {}, skip,
                hh, copy};
     if (post) g.epi = EPI_BIAS, g.out = y_mlp;
-    if ((st = project(h, l, 3, g, h->S<char>(d.f8 ? ws.mlp8 : ws.mlp), h->S(ws.mlp_s)))) return st;
+    if ((st = project(h, l, 3, g, h->S<char>(ws.mlp), h->S(ws.mlp_s)))) return st;
   }
   if (post) {
     if ((st = norm_rows(h, nullptr, nullptr, y_mlp, post + D, mod + 5 * D, out ? out : hh, skip))) return st;

@@ -160,8 +160,11 @@ struct GemmArgs {
 
 hipError_t launch_gemm(const GemmArgs& a, bool bf16_mode, hipStream_t s);
 // The same projections of e4m3 operands (rows contiguous) with float32 scales
-// [M][ceil(K/128)] and [ceil(N/128)][ceil(K/128)]; act type bf16
-hipError_t launch_gemm_fp8(const GemmArgs& a, const float* a_scale, const float* w_scale, hipStream_t s);
+// [M][ceil(K/128)] and [ceil(N/128)][ceil(K/128)]; act type bf16, but
+// EPI_BIAS_GELU stores e4m3 blocks with their scales in out_scale
+// [M][ceil(N/128)]
+hipError_t launch_gemm_fp8(const GemmArgs& a, const float* a_scale, const float* w_scale, float* out_scale,
+                           hipStream_t s);
 
 // ---------------------------------------------------------------- attention
 struct AttnArgs {

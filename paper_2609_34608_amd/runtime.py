@@ -394,7 +394,7 @@ _NORMS = {"none": abi.WAM_NORM_NONE, "rms": abi.WAM_NORM_RMS, "layer": abi.WAM_N
 _ROPE_ARGS = struct.Struct("@10i4P12qPqP2Pf")
 _NORM_ARGS = struct.Struct("@8i5P10q3P6q2P2f")
 _QUANTIZE_ARGS = struct.Struct("@4iPqPqPq")
-_MATMUL_ARGS = struct.Struct("@5iPqPqPqPqPPq")
+_MATMUL_ARGS = struct.Struct("@5iPqPqPqPqPPqPq")
 
 
 def _operand(t, what, dtypes, index, shape=None):
@@ -609,12 +609,13 @@ def quantize_fp8(x, *, block_rows=1, q=None, scale=None, stream: torch.cuda.Stre
     return q, scale
 
 
-def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_dtype=None,
+def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_dtype=None, out_scale=None,
                stream: torch.cuda.Stream | None = None):
     """out [M, N] = act((a * a_scale) (w * w_scale)^T + bias) of 8-bit blocks
     (wam_matmul_fp8): a [M, K] with scales per row and 128 columns, w [N, K] with
     scales per 128 x 128, both as quantize_fp8 gives them; bias float32 [N]; gelu:
-    the tanh form.  out float32 or bfloat16 (default: a new bfloat16 one)."""
+    the tanh form.  out float32, bfloat16 (default: a new bfloat16 one) or
+    float8_e4m3fn: then returns (out, out_scale), blocks for the next product."""
     index = _first(a, "matmul_fp8: a", _F8, 2)
     _operand(w, "matmul_fp8: w", _F8, index)
     M, K = a.shape
@@ -626,18 +627,22 @@ def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_d
     if bias is not None:
         _operand(bias, "matmul_fp8: bias", _F32, index, (N,))
     if out is None:
-        out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
-        if out_dtype not in _REAL:
-            raise WamError(f"matmul_fp8: out_dtype {out_dtype} is not supported")
-        out = torch.empty((M, N), dtype=out_dtype, device=a.device)
+        out = _new_rows((M, N), torch.bfloat16 if out_dtype is None else out_dtype, a.device, "matmul_fp8: out_dtype")
     else:
-        _operand(out, "matmul_fp8: out", _REAL if out_dtype is None else (out_dtype,), index, (M, N))
-    args = _pack(_MATMUL_ARGS, "matmul_fp8", M, N, K, _TYPES[out.dtype],
-                 abi.WAM_ACT_GELU if gelu else abi.WAM_ACT_NONE, a.data_ptr(), a.stride(0), a_scale.data_ptr(),
-                 a_scale.stride(0), w.data_ptr(), w.stride(0), w_scale.data_ptr(), w_scale.stride(0), _ptr_or_0(bias),
-                 out.data_ptr(), out.stride(0))
+        _operand(out, "matmul_fp8: out", tuple(_TYPES) if out_dtype is None else (out_dtype,), index, (M, N))
+    kind = _TYPES[out.dtype]
+    scale_at = scale_stride = 0
+    if kind == abi.WAM_FP8:
+        shape = (M, -(-N // 128))
+        out_scale = (torch.empty(shape, dtype=torch.float32, device=a.device) if out_scale is None else
+                     _operand(out_scale, "matmul_fp8: out_scale", _F32, index, shape))
+        scale_at, scale_stride = out_scale.data_ptr(), out_scale.stride(0)
+    args = _pack(_MATMUL_ARGS, "matmul_fp8", M, N, K, kind, abi.WAM_ACT_GELU if gelu else abi.WAM_ACT_NONE,
+                 a.data_ptr(), a.stride(0), a_scale.data_ptr(), a_scale.stride(0), w.data_ptr(), w.stride(0),
+                 w_scale.data_ptr(), w_scale.stride(0), _ptr_or_0(bias), out.data_ptr(), out.stride(0), scale_at,
+                 scale_stride)
     _call(abi.lib().wam_matmul_fp8, args, index, stream, "wam_matmul_fp8")
-    return out
+    return (out, out_scale) if kind == abi.WAM_FP8 else out
 
 
 def probe_mfma_bf16(shape: int = 0, n_blocks: int = 1024, iters: int = 20000, device="cuda:0"):

@@ -1,5 +1,5 @@
-// Answers which tile a product of e4m3 matrices takes: lines "exact M N K" (exact 0
-// or 1) on standard input, "BMxBN" per line on standard output; "tables" lists every
+// Answers which tile a product of e4m3 matrices takes: lines "form M N K" (form 0:
+// bf16 result, 1: float32, 2: QKV, 3: 8-bit blocks) on standard input, "BMxBN" per line on standard output; "tables" lists every
 // tile of both tables.  The library's own planner header, host arithmetic only.
 #include <cstdio>
 #include <cstring>
@@ -9,8 +9,8 @@
 using namespace wam;
 
 template <int NC>
-static const TileCfg& choice(const TileCfg (&c)[NC], int M, int N, int K) {
-  return c[plan_fp8(c, M, N, K)];
+static const TileCfg& choice(const TileCfg (&c)[NC], int M, int N, int K, Fp8Result r) {
+  return c[plan_fp8(c, M, N, K, r)];
 }
 
 int main() {
@@ -22,10 +22,11 @@ int main() {
       std::printf("\n");
       continue;
     }
-    int exact, M, N, K;
-    if (std::sscanf(line, "%d %d %d %d", &exact, &M, &N, &K) != 4) return 1;
-    const TileCfg& t = exact ? choice(kFp8ExactCfgs, M, N, K) : choice(kFp8Cfgs, M, N, K);
-    std::printf("%d:%dx%d\n", exact, t.bm, t.bn);
+    int form, M, N, K;
+    if (std::sscanf(line, "%d %d %d %d", &form, &M, &N, &K) != 4) return 1;
+    const TileCfg& t = form == 1 ? choice(kFp8ExactCfgs, M, N, K, FP8_PLAIN)
+                                 : choice(kFp8Cfgs, M, N, K, form == 2 ? FP8_QKV : form == 3 ? FP8_BLOCKS : FP8_PLAIN);
+    std::printf("%d:%dx%d\n", form, t.bm, t.bn);
   }
   return 0;
 }

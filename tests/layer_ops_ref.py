@@ -123,6 +123,24 @@ def check_blocks(q, s, x, bound, rows=1):
     assert (off <= tol).all(), float((off / tol).max())
 
 
+def check_row_blocks(q, s, x, bound):
+    """check_blocks for blocks of 1 x 128, on the device of x."""
+    q, s = f64_there(q), f64_there(s)
+    M, K = x.shape
+    for j in range(-(-K // 128)):
+        at = slice(j * 128, (j + 1) * 128)
+        most, off = x[:, at].abs().max(1).values, bound[:, at].max(1).values
+        scale = s[:, j]
+        # a block whose bound reaches zero may be a block of zeros, whose scale is 1 (a
+        # GELU of -30 is 0 in float32 and 1e-40 here)
+        zero = (scale == 1) & (most <= off) & (q[:, at] == 0).all(1)
+        assert (((scale * 448 - most).abs() <= off + 2 * D * most + 448 * 2.0 ** -126) | zero).all()
+        tol = bound[:, at] + 2.0 ** -4 * (1 + 4 * D) * (x[:, at].abs() + bound[:, at])
+        tol = tol + scale[:, None] * 2.0 ** -10 * (1 + 4 * D)
+        off = (q[:, at] * scale[:, None] - x[:, at]).abs()
+        assert (off <= tol).all(), float((off / tol).max())
+
+
 def values(q, s, rows, wide=f64):
     """The float64 matrix that blocks of (rows x 128) stand for."""
     q, s = wide(q), wide(s)

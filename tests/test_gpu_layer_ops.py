@@ -366,6 +366,50 @@ def test_matmul_tiles(dev, R, exact, M, N, K):
         F.check(out, *F.matmul(*ops, bias, gelu, dtype, wide=F.f64_there), dtype=dtype, wide=F.f64_there)
 
 
+# sizes that take each tile of 8-bit results (tests/test_plan_fp8.py)
+BLOCK_TILES = [(1, 1, 1), (1, 6144, 1536), (5, 130, 200), (130, 200, 333), (700, 1000, 512), (8222, 648, 512),
+               (5498, 641, 640), (9430, 1566, 512), (8648, 797, 333), (9864, 1071, 200), (5522, 2075, 512)]
+
+
+@pytest.mark.parametrize("M,N,K", BLOCK_TILES)
+def test_matmul_into_blocks(dev, R, M, N, K):
+    """8-bit results: blocks of the product before any other rounding; bytes and
+    scales beyond them stay."""
+    ops = _operands(R, dev, M, N, K)
+    bias = _rand(dev, 9, N)
+    for gelu in (False, True):
+        out = torch.full((M, N + 9), 7.0, device=dev).to(FP8)
+        scale = torch.full((M, -(-N // 128) + 1), -1.0, device=dev)
+        got = R.matmul_fp8(*ops, bias=bias, gelu=gelu, out=out[:, :N], out_scale=scale[:, :-1])
+        assert got[0].data_ptr() == out.data_ptr() and (out[:, N:].float() == 7).all() and (scale[:, -1] == -1).all()
+        c, err = F.matmul(*ops, bias, gelu, BF16, wide=F.f64_there)
+        F.check_row_blocks(out[:, :N], scale[:, :-1], c, err)
+    q, s = R.matmul_fp8(*ops, out_dtype=FP8)
+    assert q.dtype == FP8 and s.shape == (M, -(-N // 128)) and (M == 1 or q.stride(0) % 16 == 0)
+
+
+def test_mlp_in_blocks(dev, R):
+    """Two products in a row, the first one's result in 8-bit blocks."""
+    M, D, H = 300, 192, 640
+    a, sa, w1, s1 = _operands(R, dev, M, H, D)
+    w2, s2 = R.quantize_fp8(0.02 * _rand(dev, 5, D, H), block_rows=128)
+    q, s = R.matmul_fp8(a, sa, w1, s1, gelu=True, out_dtype=FP8)
+    out = R.matmul_fp8(q, s, w2, s2, out_dtype=F32)
+    F.check(out, *F.matmul(q, s, w2, s2), dtype=F32)
+
+
+def test_blocks_of_zero_and_non_finite_rows(dev, R):
+    M, N, K = 40, 300, 256
+    a, sa, w, sw = _operands(R, dev, M, N, K)
+    want = R.matmul_fp8(a, sa, w, sw, out_dtype=FP8)
+    a.view(torch.uint8)[3] = 0
+    a.view(torch.uint8)[7, 9] = 127
+    q, s = R.matmul_fp8(a, sa, w, sw, out_dtype=FP8)
+    assert (s[3] == 1).all() and (q[3].float() == 0).all() and s[7].isnan().all()
+    rest = [r for r in range(M) if r not in (3, 7)]
+    assert torch.equal(q[rest].float(), want[0][rest].float()) and torch.equal(s[rest], want[1][rest])
+
+
 def test_matmul_strides_and_tail_bytes(dev, R):
     """Padded rows whose bytes past K are NaN, strided scales, an odd result row
     stride: none of it enters, the elements between stay."""

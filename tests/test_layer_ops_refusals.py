@@ -116,7 +116,9 @@ def test_quantize_refuses(kw, code, text):
 
 @pytest.mark.parametrize("kw,code,text", [
     (dict(N=-1), L.WAM_E_ARG, "sizes"), (dict(K=0), L.WAM_E_SHAPE, "K must"), (dict(K=2**31 - 1), L.WAM_E_SHAPE, "large"),
-    (dict(out_dtype=L.WAM_FP8), L.WAM_E_ARG, "out must"), (dict(act=2), L.WAM_E_ARG, "activation"),
+    (dict(out_dtype=3), L.WAM_E_ARG, "out must"), (dict(out_dtype=L.WAM_FP8), L.WAM_E_ARG, "out_scale"),
+    (dict(out_dtype=L.WAM_FP8, out_scale=P, out_scale_stride=0), L.WAM_E_ARG, "out_scale"),
+    (dict(out_dtype=L.WAM_FP8, out_scale=P, out_scale_stride=1, a_stride=2**24), L.WAM_E_UNSUPPORTED, "2^23"), (dict(act=2), L.WAM_E_ARG, "activation"),
     (dict(a=None), L.WAM_E_ARG, "null"), (dict(w_scale=None), L.WAM_E_ARG, "null"), (dict(a=P + 8), L.WAM_E_ARG, "16"),
     (dict(w_stride=264), L.WAM_E_ARG, "16"), (dict(a_stride=240), L.WAM_E_ARG, "overlap"),
     (dict(w_stride=0), L.WAM_E_ARG, "overlap"), (dict(a_scale_stride=-2), L.WAM_E_ARG, "scales"),

@@ -48,3 +48,19 @@ def test_every_tile_is_chosen(ask):
     size = lambda lo, hi: round(math.exp(rng.uniform(math.log(lo), math.log(hi))))  # noqa: E731
     lines = [f"{rng.randint(0, 1)} {size(1, 12000)} {size(16, 6200)} {size(16, 6200)}" for _ in range(4000)]
     assert set(ask(lines)) == set(ask(["tables"]))
+
+
+def _sweep(ask, form):
+    rng = random.Random(4)
+    size = lambda lo, hi: round(math.exp(rng.uniform(math.log(lo), math.log(hi))))  # noqa: E731
+    return set(ask([f"{form} {size(1, 12000)} {size(16, 6200)} {size(16, 6200)}" for _ in range(4000)]))
+
+
+def test_every_tile_of_blocks_is_tested(ask):
+    got = ask([f"3 {m} {n} {k}" for m, n, k in ops.BLOCK_TILES])
+    assert set(got) == _sweep(ask, 3)
+
+
+def test_qkv_tiles_hold_whole_heads(ask):
+    tiles = _sweep(ask, 2)
+    assert tiles <= {"2:256x256", "2:192x256", "2:128x256", "2:160x128", "2:64x128", "2:32x64"} and "2:32x64" in tiles

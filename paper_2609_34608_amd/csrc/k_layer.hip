@@ -41,13 +41,35 @@ __device__ __forceinline__ void load_n(float (&x)[N], const T* p, int n) {
     for (int i = 0; i < N; ++i) x[i] = i < n ? to_f32(p[i]) : 0.f;
   }
 }
+
+// A result larger than the chip's L2s (8 x 4 MB) cannot wait there for its reader:
+// streaming stores leave the caches to what is read (10176 rows of 24 + 24 heads 29.4 ->
+// 25.4 us, norms of 10176 rows of 1536 40.8 -> 36.9, 8-bit blocks of 10176 x 6144 34.2 ->
+// 32.6).  A smaller one is read from there by the next kernel, and streaming it
+// made the layers of the 8-bit mode 2-5 us slower.
+constexpr int64_t kStreamBytes = (int64_t)32 << 20;
+template <typename P>
+__device__ __forceinline__ void put(void* p, const P& w, bool stream) {
+  typedef uint32_t words __attribute__((ext_vector_type(sizeof(P) / 4), aligned(1)));
+  words v;
+  __builtin_memcpy(&v, &w, sizeof(P));
+  if (stream) {
+    // the empty statements keep the compiler from merging the two stores into a plain one
+    asm volatile("");
+    __builtin_nontemporal_store(v, static_cast<words*>(p));
+    asm volatile("");
+  } else {
+    *static_cast<words*>(p) = v;
+  }
+}
+
 template <int N, typename T>
-__device__ __forceinline__ void store_n(T* p, const float (&x)[N], int n) {
+__device__ __forceinline__ void store_n(T* p, const float (&x)[N], int n, bool stream) {
   Pack<T, N> w;
 #pragma unroll
   for (int i = 0; i < N; ++i) w.v[i] = static_cast<T>(x[i]);
   if (n >= N) {
-    *reinterpret_cast<Pack<T, N>*>(p) = w;
+    put(p, w, stream);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -93,6 +115,7 @@ struct RopeTiling {
   int heads_wave;   // head vectors of one row side by side in a wave
   int wave_rows;    // waves side by side along the rows (the others along the heads)
   int heads_block;  // heads of a block
+  int stream;       // streaming stores
 };
 constexpr int kRopeTable = 2048;  // most (row, pair) angles of a block
 
@@ -195,8 +218,8 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams p, RopeTilin
       }
     }
     if (live && h < h_end) {
-      *reinterpret_cast<Pack<T, 8>*>(o + h * so[2] + e1) = o1;
-      *reinterpret_cast<Pack<T, 8>*>(o + h * so[2] + e2) = o2;
+      put(o + h * so[2] + e1, o1, tl.stream);
+      put(o + h * so[2] + e2, o2, tl.stream);
     }
   }
 }
@@ -268,7 +291,7 @@ __device__ __forceinline__ uint32_t most_of(const float (&x)[N]) {
 
 // e4m3 of x / s into the first n bytes at q
 template <int N>
-__device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&x)[N], float s, int n) {
+__device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&x)[N], float s, int n, bool stream) {
   struct __attribute__((packed, aligned(1))) Bytes {
     uint32_t v[N / 4];
   };
@@ -279,7 +302,7 @@ __device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&x)[N], floa
     w.v[i] = pack_e4m3(divide_by(x[4 * i], s, r), divide_by(x[4 * i + 1], s, r), divide_by(x[4 * i + 2], s, r),
                        divide_by(x[4 * i + 3], s, r));
   if (n >= N) {
-    *reinterpret_cast<Bytes*>(q) = w;
+    put(q, w, stream);
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i)
@@ -309,7 +332,7 @@ constexpr int kNormCols = 4;  // columns of a lane and chunk
 // over buffers larger than the last-level cache, 5.1 with modulation per row;
 // requesting gate and modulation ahead of the sums was 3-5% slower (registers).
 template <int CH, int W, typename TH, typename TY>
-__global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, const int* skip) {
+__global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, bool stream_h, bool stream_u, const int* skip) {
   __shared__ float part[2][4];
   if (skip && *skip) return;
   const int lane = threadIdx.x % kWave, wid = threadIdx.x / kWave;
@@ -391,7 +414,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, con
   if (a.h_out) {
     TH* o = static_cast<TH*>(a.h_out) + b * a.h_out_stride[0] + t * a.h_out_stride[1];
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store_n(o + col(c), x[c], have(c));
+    for (int c = 0; c < CH; ++c) store_n(o + col(c), x[c], have(c), stream_h);
   }
   if (!a.u) return;
   standardise(x, a.pre);
@@ -410,10 +433,10 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, con
   const int64_t u0 = b * a.u_stride[0] + t * a.u_stride[1];
   if (a.u_dtype == WAM_BF16) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store_n(static_cast<bf16*>(a.u) + u0 + col(c), x[c], have(c));
+    for (int c = 0; c < CH; ++c) store_n(static_cast<bf16*>(a.u) + u0 + col(c), x[c], have(c), stream_u);
   } else if (a.u_dtype == WAM_FP32) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) store_n(static_cast<float*>(a.u) + u0 + col(c), x[c], have(c));
+    for (int c = 0; c < CH; ++c) store_n(static_cast<float*>(a.u) + u0 + col(c), x[c], have(c), stream_u);
   } else {
     float* us = a.u_scale + b * a.u_scale_stride[0] + t * a.u_scale_stride[1];
 #pragma unroll
@@ -422,7 +445,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, con
       uint32_t most = group_max<16>(most_of(x[c]));
       most = max(most, (uint32_t)__shfl_xor((int)most, 16, 64));
       const float s = block_scale(most);
-      store_e4m3(static_cast<uint8_t*>(a.u) + u0 + col(c), x[c], s, n);
+      store_e4m3(static_cast<uint8_t*>(a.u) + u0 + col(c), x[c], s, n, stream_u);
       if (lane % 32 == 0 && n > 0) us[col(c) / kScaleBlock] = s;
     }
   }
@@ -434,11 +457,13 @@ hipError_t launch_norm_rows(const wam_norm_args& a, hipStream_t s, const int* sk
   // one wave per row: blocks of four rows, or of one while the chip has room
   const int block = W > 1 || rows >= 1024 ? 256 : kWave;
   const dim3 grid((unsigned)(W > 1 ? rows : (rows + block / kWave - 1) / (block / kWave)));
+  const bool stream_h = rows * a.D * (int64_t)sizeof(TH) > kStreamBytes;
+  const bool stream_u = rows * a.D * (a.u_dtype == WAM_FP32 ? 4 : a.u_dtype == WAM_BF16 ? 2 : 1) > kStreamBytes;
   const int chunks = (a.D + kNormCols * kWave * W - 1) / (kNormCols * kWave * W);
   auto launch = [&](auto CH) {
     constexpr int c = decltype(CH)::value;
     if constexpr (W == 1 || c > 2) {  // four waves: past 2048 columns
-      if (chunks == c) launch_k(norm_residual_kernel<c, W, TH, TY>, grid, block, 0, s, a, skip);
+      if (chunks == c) launch_k(norm_residual_kernel<c, W, TH, TY>, grid, block, 0, s, a, stream_h, stream_u, skip);
     }
   };
   launch(std::integral_constant<int, 1>{});
@@ -464,7 +489,7 @@ constexpr int kQuantCols = 16, kQuantGroup = kScaleBlock / kQuantCols;
 
 // blocks of 1 x 128
 template <typename T>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(wam_quantize_args a, int kb, const int* skip) {
+__global__ __launch_bounds__(256) void quantize_rows_kernel(wam_quantize_args a, int kb, bool stream, const int* skip) {
   if (skip && *skip) return;
   const uint32_t i = blockIdx.x * 32u + threadIdx.x / kQuantGroup;  // scale block
   const int m = (int)(i / (uint32_t)kb), bk = (int)(i % (uint32_t)kb);
@@ -474,7 +499,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(wam_quantize_args a,
   load_n(x, static_cast<const T*>(a.x) + m * a.x_stride + col, a.K - col);
   const float s = block_scale(group_max<kQuantGroup>(most_of(x)));
   if (threadIdx.x % kQuantGroup == 0) a.scale[m * a.scale_stride + bk] = s;
-  store_e4m3(static_cast<uint8_t*>(a.q) + m * a.q_stride + col, x, s, a.K - col);
+  store_e4m3(static_cast<uint8_t*>(a.q) + m * a.q_stride + col, x, s, a.K - col, stream);
 }
 
 // blocks of 128 x 128: one per thread block, four rows per thread in registers
@@ -501,7 +526,7 @@ __global__ __launch_bounds__(256) void quantize_tiles_kernel(wam_quantize_args a
 #pragma unroll
   for (int j = 0; j < kRows; ++j) {
     const int64_t m = m0 + j * (256 / kQuantGroup);
-    if (m < a.M) store_e4m3(static_cast<uint8_t*>(a.q) + m * a.q_stride + col, x[j], s, a.K - col);
+    if (m < a.M) store_e4m3(static_cast<uint8_t*>(a.q) + m * a.q_stride + col, x[j], s, a.K - col, false);
   }
 }
 
@@ -509,7 +534,8 @@ template <typename T>
 hipError_t launch_blocks(const wam_quantize_args& a, hipStream_t s, const int* skip) {
   const int kb = (a.K + kScaleBlock - 1) / kScaleBlock;
   const int64_t n = (int64_t)kb * ((a.M + a.block_rows - 1) / a.block_rows);
-  if (a.block_rows == 1) launch_k(quantize_rows_kernel<T>, dim3((unsigned)((n + 31) / 32)), 256, 0, s, a, kb, skip);
+  if (a.block_rows == 1) launch_k(quantize_rows_kernel<T>, dim3((unsigned)((n + 31) / 32)), 256, 0, s, a, kb,
+                                    (int64_t)a.M * a.K > kStreamBytes, skip);
   else launch_k(quantize_tiles_kernel<T>, dim3((unsigned)n), 256, 0, s, a, kb);
   return hipGetLastError();
 }
@@ -598,6 +624,9 @@ hipError_t launch_rope_params(const RopeParams& p, hipStream_t s) {
   const int64_t row_blocks = (rows + rows_block - 1) / rows_block;
   const int steps = row_blocks < 256 ? 1 : std::min(3, (H + head_step - 1) / head_step);
   tl.heads_block = head_step * steps;
+  // in place the lines have just been read (a layer of 10176 rows of 1536: 2-6 us slower)
+  tl.stream = (a.Hq == 0 || a.q != a.q_out) && (a.Hk == 0 || a.k != a.k_out) &&
+              rows * ((int64_t)a.Hq + a.Hk) * a.dh * (a.dtype == WAM_BF16 ? 2 : 4) > kStreamBytes;
   const int64_t head_blocks = (H + tl.heads_block - 1) / tl.heads_block;
   if (row_blocks > 0x7fffffff || head_blocks > 65535) return hipErrorInvalidValue;
   const dim3 grid((unsigned)row_blocks, (unsigned)head_blocks, a.Hq > 0 && a.Hk > 0 ? 2 : 1);

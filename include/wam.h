@@ -126,6 +126,7 @@ extern "C" {
 #define WAM_ROPE_HALVES 0 /* elements i and i + P      */
 #define WAM_ROPE_PAIRS 1  /* elements 2 i and 2 i + 1  */
 #define WAM_MAX_HEAD 256
+#define WAM_MAX_ROWS 16777215 /* of wam_rope and wam_norm_residual: B * T */
 
 #define WAM_MAX_BATCH 16
 #define WAM_MAX_COMPONENTS 8
@@ -444,7 +445,8 @@ const char *wam_noalloc_last_error(void);
  * q_gain / k_gain (float32 [dh]) each head vector x is first divided by its
  * root mean square and multiplied by the gain: x gain / sqrt(mean(x^2) + eps);
  * NULL leaves it out.  Results are rounded once.  q_out may be q and k_out may be k
- * (with the same strides).  Hk = 0 leaves k out (Hq = 0: q).  dh <= 256. */
+ * (with the same strides).  Hk = 0 leaves k out (Hq = 0: q).  dh <= 256,
+ * B * T <= WAM_MAX_ROWS, Hq + Hk <= WAM_MAX_ROWS. */
 typedef struct {
   int32_t B, T, Hq, Hk, dh;
   int32_t dtype;              /* of q, k and the results: WAM_FP32 | WAM_BF16  */
@@ -477,7 +479,8 @@ int wam_rope_frequencies(const int32_t *sections, double theta, int32_t shared, 
  * h_out NULL: not stored (u must be asked for).  Sums are float32.  u of type
  * WAM_FP8 is stored as blocks of 128 columns of a row, as wam_quantize_fp8
  * does, with its float32 scales in u_scale [B][T][ceil(D / 128)].  h_out may
- * be h and u may be y (with the same type and strides).  1 <= D <= 8192. */
+ * be h and u may be y (with the same type and strides).  1 <= D <= 8192,
+ * B * T <= WAM_MAX_ROWS. */
 #define WAM_NORM_NONE 0
 #define WAM_NORM_RMS 1
 #define WAM_NORM_LAYER 2
@@ -502,7 +505,8 @@ int wam_norm_residual(const wam_norm_args *args, void *hip_stream);
  * float32, at least 2^-126 (1 where the block is zero), and q = x / scale rounded
  * to e4m3, to nearest, ties to even.  A block with a NaN or an infinity has that
  * as its scale, and stands for NaN.  scale: [ceil(M / block_rows)][ceil(K / 128)].
- * Bytes of a row of q past K are left as they are. */
+ * Bytes of a row of q past K are left as they are.  At most 2^29 - 32 blocks of
+ * one row or 2^24 - 1 of 128 rows. */
 typedef struct {
   int32_t M, K;
   int32_t dtype;       /* of x: WAM_FP32 | WAM_BF16 */
@@ -521,10 +525,12 @@ int wam_quantize_fp8(const wam_quantize_args *args, void *hip_stream);
  *                   sum_{k in block j} a[m][k] w[n][k] + bias[n])
  * a [M][K] with scales per row (blocks of 1 x 128), w [N][K] with scales per
  * block of 128 x 128, as wam_quantize_fp8 makes them.  Block products and their
- * scaled sum are float32; with a bf16 result the products of 8 consecutive k are
- * cut below 2^-13 of the power of two of the largest of them (the 8-bit matrix
- * instruction), with a float32 result they are not.  a and w must start on 16 bytes and their row strides
- * be multiples of 16; the bytes of a row past K may hold anything.  act:
+ * scaled sum are float32; with a bf16 or e4m3 result the products of 8
+ * consecutive k are cut below 2^-13 of the power of two of the largest of them
+ * (the 8-bit matrix instruction), with a float32 result they are not.  a and w
+ * must start on 16 bytes and their row strides be multiples of 16; the bytes of a
+ * row past K may hold anything.  WAM_E_SHAPE where the tiles pass a grid
+ * (from 2^24 of 32 x 32 on).  act:
  * WAM_ACT_NONE or WAM_ACT_GELU (tanh form).  out: WAM_FP32, WAM_BF16, or WAM_FP8:
  * blocks of 1 x 128 of the result before any rounding, with their scales in out_scale
  * [M][ceil(N / 128)], as wam_quantize_fp8 makes them, for the next product (rows

@@ -24,7 +24,7 @@ WAM_ATTN_AUTO, WAM_ATTN_RUNNING_MAX, WAM_ATTN_BOUNDED, WAM_ATTN_PINGPONG, WAM_AT
 (WAM_KC_GEMM_QKV, WAM_KC_GEMM_PROJ, WAM_KC_GEMM_FC1, WAM_KC_GEMM_FC2, WAM_KC_ATTENTION,
  WAM_KC_RR_GATE, WAM_KC_RR_INJECT, WAM_KC_RR_REFRESH, WAM_KC_COUNT) = range(9)
 
-WAM_ROPE_HALVES, WAM_ROPE_PAIRS, WAM_MAX_HEAD = 0, 1, 256
+WAM_ROPE_HALVES, WAM_ROPE_PAIRS, WAM_MAX_HEAD, WAM_MAX_ROWS = 0, 1, 256, 16777215
 WAM_NORM_NONE, WAM_NORM_RMS, WAM_NORM_LAYER, WAM_MAX_NORM_D = 0, 1, 2, 8192
 WAM_ACT_NONE, WAM_ACT_GELU = 0, 1
 

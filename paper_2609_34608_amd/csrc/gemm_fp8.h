@@ -315,7 +315,7 @@ __device__ __forceinline__ void load_bias(float (&bias)[J][W], const float* from
 // of two neighbouring waves (64 each), which meet in LDS: the largest magnitude of
 // a row's columns over the lane's values, the row's four lanes, the two waves.  The
 // values themselves never leave the registers unrounded.
-template <int TN, int TM, int NW, bool GELU>
+template <int TN, int TM, bool GELU>
 __device__ __forceinline__ void store_blocks(const Fp8Operands& p, const Fp8Out& o, f32x4 (&acc)[TN][TM], int mb,
                                              int nb, int lane, uint8_t* lds) {
   static_assert(TN == 4, "two waves to a block");
@@ -456,7 +456,7 @@ __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_blocks_kernel(Fp8Opera
   if (skip && *skip) return;
   gemm_fp8_body<BM, BN, WGM, WGN, ST, false, false>(
       p, [&](f32x4(&acc)[TN][TM], int m, int n, int lane, uint8_t* lds) __attribute__((always_inline)) {
-        store_blocks<TN, TM, WGM * WGN, GELU>(p, o, acc, m, n, lane, lds);
+        store_blocks<TN, TM, GELU>(p, o, acc, m, n, lane, lds);
       });
 }
 

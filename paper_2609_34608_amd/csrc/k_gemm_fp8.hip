@@ -12,11 +12,17 @@ namespace {
 using gemm::Fp8Operands;
 using gemm::Fp8Out;
 
+// Blocks of `threads` for the tiles of an M x N result, 0 where a grid, whose
+// threads count in 32 bits, ends before them.
+unsigned tile_grid(const Fp8Operands& p, int bm, int bn, int threads) {
+  const int64_t blocks = (int64_t)((p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn);
+  return blocks * threads > 0xffffffffll ? 0 : (unsigned)blocks;
+}
+
 template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool WIDE>
 hipError_t launch_tile(const Fp8Operands& p, const Fp8Out& o, bool gelu, hipStream_t s) {
-  const int64_t blocks = (int64_t)((p.M + BM - 1) / BM) * ((p.N + BN - 1) / BN);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks), block(WGM * WGN * 64);
+  const dim3 block(WGM * WGN * 64), grid(tile_grid(p, BM, BN, block.x));
+  if (!grid.x) return hipErrorInvalidConfiguration;
   if (gelu) launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, EXACT, true, WIDE>, grid, block, 0, s, p, o);
   else launch_k(gemm::gemm_fp8_kernel<BM, BN, WGM, WGN, ST, EXACT, false, WIDE>, grid, block, 0, s, p, o);
   return hipGetLastError();
@@ -46,9 +52,8 @@ template <int C>
 hipError_t launch_blocks_cfg(const Fp8Operands& p, const Fp8Out& o, bool gelu, hipStream_t s, const int* skip) {
   constexpr TileCfg t = kFp8Cfgs[C];
   if constexpr (t.bn % 128 == 0) {
-    const int64_t blocks = (int64_t)((p.M + t.bm - 1) / t.bm) * ((p.N + t.bn - 1) / t.bn);
-    if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)blocks), block(t.wgm * t.wgn * 64);
+    const dim3 block(t.wgm * t.wgn * 64), grid(tile_grid(p, t.bm, t.bn, block.x));
+    if (!grid.x) return hipErrorInvalidConfiguration;
     if (gelu) launch_k(gemm::gemm_fp8_blocks_kernel<t.bm, t.bn, t.wgm, t.wgn, t.st, true>, grid, block, 0, s, p, o, skip);
     else launch_k(gemm::gemm_fp8_blocks_kernel<t.bm, t.bn, t.wgm, t.wgn, t.st, false>, grid, block, 0, s, p, o, skip);
     return hipGetLastError();
@@ -86,9 +91,8 @@ hipError_t launch_fp8(const Fp8Operands& p, const Fp8Out& o, int out_dtype, bool
 template <int C>
 hipError_t launch_layer_cfg(const Fp8Operands& p, const GemmArgs& g, hipStream_t s) {
   constexpr TileCfg t = kFp8Cfgs[C];
-  const int64_t blocks = (int64_t)((p.M + t.bm - 1) / t.bm) * ((p.N + t.bn - 1) / t.bn);
-  if (blocks > 0x7fffffff) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks), block(t.wgm * t.wgn * 64);
+  const dim3 block(t.wgm * t.wgn * 64), grid(tile_grid(p, t.bm, t.bn, block.x));
+  if (!grid.x) return hipErrorInvalidConfiguration;
   auto go = [&](auto EPI) {
     launch_k(gemm::gemm_fp8_layer_kernel<t.bm, t.bn, t.wgm, t.wgn, t.st, decltype(EPI)::value>, grid, block, 0, s, p, g);
     return hipGetLastError();
@@ -160,16 +164,18 @@ extern "C" int wam_matmul_fp8(const wam_matmul_args* a, void* hip_stream) {
     const int64_t nb = ((int64_t)a->N + kScaleBlock - 1) / kScaleBlock;
     if (!a->out_scale || !aligned_to(a->out_scale, 4) || (a->M > 1 && a->out_scale_stride < nb))
       return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: out of WAM_FP8 needs out_scale with distinct rows");
-    if (a->a_stride > kNear || a->w_stride > kNear || a->K > kNear)
+    if ((a->M > 1 && a->a_stride > kNear) || (a->N > 1 && a->w_stride > kNear) || a->K > kNear)
       return noalloc_fail(WAM_E_UNSUPPORTED, "wam_matmul_fp8: out of WAM_FP8 needs rows of at most 2^23 bytes");
   }
   if ((a->M > 1 && a->out_stride < a->N) || !aligned_to(a->out, esize))
     return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: rows of out must be distinct and aligned to their elements");
   if (a->out == a->a || a->out == a->w) return noalloc_fail(WAM_E_ARG, "wam_matmul_fp8: out must not be a or w");
   gemm::Fp8Operands p{static_cast<const uint8_t*>(a->a), static_cast<const uint8_t*>(a->w), a->a_scale, a->w_scale,
-                      a->a_stride, a->w_stride, a->a_scale_stride, a->w_scale_stride, a->M, a->N, a->K};
+                      a->M > 1 ? a->a_stride : 0, a->N > 1 ? a->w_stride : 0, a->a_scale_stride, a->w_scale_stride,
+                      a->M, a->N, a->K};
   gemm::Fp8Out o{a->bias, a->out, a->out_stride, a->out_scale, a->out_scale_stride};
-  if (launch_fp8(p, o, a->out_dtype, a->act == WAM_ACT_GELU, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
-    return noalloc_fail(WAM_E_HIP, "wam_matmul_fp8: kernel launch failed");
+  const hipError_t e = launch_fp8(p, o, a->out_dtype, a->act == WAM_ACT_GELU, static_cast<hipStream_t>(hip_stream));
+  if (e == hipErrorInvalidConfiguration) return noalloc_fail(WAM_E_SHAPE, "wam_matmul_fp8: too many tiles for one launch");
+  if (e != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_matmul_fp8: kernel launch failed");
   return WAM_OK;
 }

@@ -225,58 +225,60 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams p, RopeTilin
 }
 
 // Any other head size or sections: one wave per head vector, element e = lane +
-// 64 j.
+// 64 j; blocks of four vectors, each taking several where a grid ends.
 __global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
   if (p.skip && *p.skip) return;
   const wam_rope_args& a = p.a;
   const int heads = a.Hq + a.Hk;
-  const int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
-  if (item >= (int64_t)a.B * a.T * heads) return;
+  const int64_t items = (int64_t)a.B * a.T * heads;
   const int lane = threadIdx.x % kWave;
-  const int hd = (int)(item % heads);
-  const int64_t row = item / heads;
-  const int t = (int)(row % a.T), b = (int)(row / a.T);
-  const bool isq = hd < a.Hq;
-  const int h = isq ? hd : hd - a.Hq;
-  const int64_t* si = isq ? a.q_stride : a.k_stride;
-  const int64_t* so = isq ? a.q_out_stride : a.k_out_stride;
-  const int64_t in = b * si[0] + t * si[1] + h * si[2], out = b * so[0] + t * so[1] + h * so[2];
-  const void* x = isq ? a.q : a.k;
-  void* o = isq ? a.q_out : a.k_out;
-  const float* gain = isq ? a.q_gain : a.k_gain;
-  const float* pos = a.pos + b * a.pos_stride + (int64_t)t * 3;
+  for (int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; item < items; item += (int64_t)gridDim.x * 4) {
+    const int hd = (int)(item % heads);
+    const int64_t row = item / heads;
+    const int t = (int)(row % a.T), b = (int)(row / a.T);
+    const bool isq = hd < a.Hq;
+    const int h = isq ? hd : hd - a.Hq;
+    const int64_t* si = isq ? a.q_stride : a.k_stride;
+    const int64_t* so = isq ? a.q_out_stride : a.k_out_stride;
+    const int64_t in = b * si[0] + t * si[1] + h * si[2], out = b * so[0] + t * so[1] + h * so[2];
+    const void* x = isq ? a.q : a.k;
+    void* o = isq ? a.q_out : a.k_out;
+    const float* gain = isq ? a.q_gain : a.k_gain;
+    const float* pos = a.pos + b * a.pos_stride + (int64_t)t * 3;
 
-  constexpr int J = WAM_MAX_HEAD / kWave;
-  float own[J], other[J];
-  float ss = 0.f;
+    constexpr int J = WAM_MAX_HEAD / kWave;
+    float own[J], other[J];
+    float ss = 0.f;
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int e = lane + kWave * j;
-    own[j] = other[j] = 0.f;
-    if (e >= a.dh) continue;
-    own[j] = load1(x, in + e, a.dtype);
-    ss += own[j] * own[j];
-    if (e < 2 * p.pairs) {
-      const int partner = a.layout == WAM_ROPE_PAIRS ? e ^ 1 : e < p.pairs ? e + p.pairs : e - p.pairs;
-      other[j] = load1(x, in + partner, a.dtype);
-      if (gain) other[j] *= gain[partner];
+    for (int j = 0; j < J; ++j) {
+      const int e = lane + kWave * j;
+      own[j] = other[j] = 0.f;
+      if (e >= a.dh) continue;
+      own[j] = load1(x, in + e, a.dtype);
+      ss += own[j] * own[j];
+      if (e < 2 * p.pairs) {
+        const int partner = a.layout == WAM_ROPE_PAIRS ? e ^ 1 : e < p.pairs ? e + p.pairs : e - p.pairs;
+        other[j] = load1(x, in + partner, a.dtype);
+        if (gain) other[j] *= gain[partner];
+      }
+      if (gain) own[j] *= gain[e];
     }
-    if (gain) own[j] *= gain[e];
-  }
-  const float rs = gain ? rsqrt_newton(wave_sum(ss) / (float)a.dh + a.eps) : 1.0f;
+    __builtin_amdgcn_wave_barrier();  // in place: every lane has read its partner before any lane stores
+    const float rs = gain ? rsqrt_newton(wave_sum(ss) / (float)a.dh + a.eps) : 1.0f;
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int e = lane + kWave * j;
-    if (e >= a.dh) continue;
-    float v = own[j] * rs;
-    if (e < 2 * p.pairs) {
-      const bool first = a.layout == WAM_ROPE_PAIRS ? e % 2 == 0 : e < p.pairs;
-      const int i = a.layout == WAM_ROPE_PAIRS ? e / 2 : first ? e : e - p.pairs;
-      float c, s;
-      axis_turn(p, pos, i, c, s);
-      v = v * c + other[j] * rs * (first ? -s : s);
+    for (int j = 0; j < J; ++j) {
+      const int e = lane + kWave * j;
+      if (e >= a.dh) continue;
+      float v = own[j] * rs;
+      if (e < 2 * p.pairs) {
+        const bool first = a.layout == WAM_ROPE_PAIRS ? e % 2 == 0 : e < p.pairs;
+        const int i = a.layout == WAM_ROPE_PAIRS ? e / 2 : first ? e : e - p.pairs;
+        float c, s;
+        axis_turn(p, pos, i, c, s);
+        v = v * c + other[j] * rs * (first ? -s : s);
+      }
+      store1(o, out + e, a.dtype, v);
     }
-    store1(o, out + e, a.dtype, v);
   }
 }
 
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, boo
   const int b = __builtin_amdgcn_readfirstlane((int)(row / a.T)), t = __builtin_amdgcn_readfirstlane((int)(row % a.T));
   const int D = a.D;
   auto col = [&](int c) { return kNormCols * ((W == 1 ? lane : (int)threadIdx.x) + kWave * W * c); };
-  // columns of chunk c that the row has (all eight but in the last chunk)
+  // columns of chunk c that the row has (all four but in the last chunk)
   auto have = [&](int c) { return c < CH - 1 ? kNormCols : D - col(c); };
   int turn = 0;
   auto row_sum = [&](float v) __attribute__((always_inline)) {
@@ -575,8 +577,8 @@ bool float_type(int t) { return t == WAM_FP32 || t == WAM_BF16; }
 int64_t type_size(int t) { return t == WAM_FP32 ? 4 : t == WAM_BF16 ? 2 : 1; }
 bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)n == 0; }
 
-// blocks of a one-dimensional grid
-constexpr int64_t kMaxGrid = 0x7fffffff;
+// blocks of 256 threads along one dimension of a grid, whose threads count in 32 bits
+constexpr int64_t kMaxGrid = (1 << 24) - 1;
 
 int check_heads(int H, const wam_rope_args* a, const void* x, const void* out, const int64_t* si,
                 const int64_t* so) {
@@ -604,8 +606,8 @@ hipError_t launch_rope_params(const RopeParams& p, hipStream_t s) {
   const int64_t rows = (int64_t)a.B * a.T;
   const int H = a.Hq > a.Hk ? a.Hq : a.Hk;
   if (a.dh % 16 || p.pairs % 8) {
-    const int64_t items = rows * (a.Hq + a.Hk);
-    launch_k(rope_kernel, dim3((unsigned)((items + 3) / 4)), 256, 0, s, p);
+    const int64_t blocks = (rows * (a.Hq + a.Hk) + 3) / 4;
+    launch_k(rope_kernel, dim3((unsigned)std::min(blocks, kMaxGrid)), 256, 0, s, p);
     return hipGetLastError();
   }
   RopeTiling tl{};
@@ -622,13 +624,14 @@ hipError_t launch_rope_params(const RopeParams& p, hipStream_t s) {
   tl.wave_rows = 2;
   const int rows_block = slots / tl.heads_wave * tl.wave_rows, head_step = tl.heads_wave * 4 / tl.wave_rows;
   const int64_t row_blocks = (rows + rows_block - 1) / rows_block;
-  const int steps = row_blocks < 256 ? 1 : std::min(3, (H + head_step - 1) / head_step);
+  constexpr int kMaxHeadBlocks = 65535;  // of a grid's second dimension
+  const int all_steps = (H + head_step - 1) / head_step;
+  const int steps = std::max(row_blocks < 256 ? 1 : std::min(3, all_steps), all_steps / kMaxHeadBlocks + 1);
   tl.heads_block = head_step * steps;
   // in place the lines have just been read (a layer of 10176 rows of 1536: 2-6 us slower)
   tl.stream = (a.Hq == 0 || a.q != a.q_out) && (a.Hk == 0 || a.k != a.k_out) &&
               rows * ((int64_t)a.Hq + a.Hk) * a.dh * (a.dtype == WAM_BF16 ? 2 : 4) > kStreamBytes;
-  const int64_t head_blocks = (H + tl.heads_block - 1) / tl.heads_block;
-  if (row_blocks > 0x7fffffff || head_blocks > 65535) return hipErrorInvalidValue;
+  const int head_blocks = (all_steps + steps - 1) / steps;
   const dim3 grid((unsigned)row_blocks, (unsigned)head_blocks, a.Hq > 0 && a.Hk > 0 ? 2 : 1);
   if (a.dtype == WAM_BF16) {
     if (a.layout == WAM_ROPE_PAIRS) launch_rope_units<bf16, true>(p, tl, grid, s);
@@ -701,15 +704,16 @@ int wam_rope(const wam_rope_args* a, void* hip_stream) {
   if (2 * pairs > a->dh) return noalloc_fail(WAM_E_SHAPE, "wam_rope: the sections' pairs must fit the head (2 P <= dh)");
   if (pairs > 0 && !a->freq) return noalloc_fail(WAM_E_ARG, "wam_rope: null freq");
   if ((a->q_gain || a->k_gain) && !(a->eps >= 0.f)) return noalloc_fail(WAM_E_ARG, "wam_rope: eps must be >= 0");
-  if ((int64_t)a->Hq + a->Hk > INT32_MAX) return noalloc_fail(WAM_E_SHAPE, "wam_rope: too many heads");
+  if ((int64_t)a->Hq + a->Hk > WAM_MAX_ROWS) return noalloc_fail(WAM_E_SHAPE, "wam_rope: too many heads");
   if (a->B == 0 || a->T == 0 || a->Hq + a->Hk == 0) return WAM_OK;
   if (!a->pos || !aligned_to(a->pos, 4)) return noalloc_fail(WAM_E_ARG, "wam_rope: null or unaligned pos");
   if (!strides_ok(&a->pos_stride, 1)) return noalloc_fail(WAM_E_ARG, "wam_rope: strides must be >= 0");
   int st = check_heads(a->Hq, a, a->q, a->q_out, a->q_stride, a->q_out_stride);
   if (!st) st = check_heads(a->Hk, a, a->k, a->k_out, a->k_stride, a->k_out_stride);
   if (st) return st;
-  if ((double)a->B * a->T * ((double)a->Hq + a->Hk) / 4 >= (double)kMaxGrid)
-    return noalloc_fail(WAM_E_SHAPE, "wam_rope: too many head vectors for one launch");
+  if ((int64_t)a->B * a->T > WAM_MAX_ROWS) return noalloc_fail(WAM_E_SHAPE, "wam_rope: too many rows");
+  if (a->Hq > 0 && a->Hk > 0 && (a->q_out == a->k_out || a->q_out == a->k || a->k_out == a->q))
+    return noalloc_fail(WAM_E_ARG, "wam_rope: a result must not be the other one or its input");
   if (launch_rope(*a, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
     return noalloc_fail(WAM_E_HIP, "wam_rope: kernel launch failed");
   return WAM_OK;
@@ -724,7 +728,7 @@ int wam_norm_residual(const wam_norm_args* a, void* hip_stream) {
   if (!(a->eps >= 0.f)) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: eps must be >= 0");
   auto kind = [](int k) { return k == WAM_NORM_NONE || k == WAM_NORM_RMS || k == WAM_NORM_LAYER; };
   if (!kind(a->post) || !kind(a->pre)) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: unknown norm");
-  if ((int64_t)a->B * a->T > kMaxGrid) return noalloc_fail(WAM_E_SHAPE, "wam_norm_residual: too many rows");
+  if ((int64_t)a->B * a->T > WAM_MAX_ROWS) return noalloc_fail(WAM_E_SHAPE, "wam_norm_residual: too many rows");
   if (a->B == 0 || a->T == 0) return WAM_OK;
   const int64_t size[2] = {a->B, a->T};
   if (!a->h) return noalloc_fail(WAM_E_ARG, "wam_norm_residual: null h");
@@ -772,7 +776,9 @@ int wam_quantize_fp8(const wam_quantize_args* a, void* hip_stream) {
   const int64_t mb = ((int64_t)a->M + a->block_rows - 1) / a->block_rows;
   if (!strides_ok(&a->x_stride, 1) || (a->M > 1 && a->q_stride < a->K) || (mb > 1 && a->scale_stride < kb))
     return noalloc_fail(WAM_E_ARG, "wam_quantize_fp8: x_stride must be >= 0, and rows of the results distinct");
-  if (mb * kb > kMaxGrid) return noalloc_fail(WAM_E_SHAPE, "wam_quantize_fp8: too many blocks for one launch");
+  // 32 blocks of one row to a thread block; columns of the last scale block stay in 31 bits
+  if (mb * kb > (a->block_rows == 1 ? 32 * kMaxGrid : kMaxGrid) || a->K > INT32_MAX - kScaleBlock)
+    return noalloc_fail(WAM_E_SHAPE, "wam_quantize_fp8: too many blocks for one launch");
   if (launch_quantize(*a, static_cast<hipStream_t>(hip_stream)) != hipSuccess)
     return noalloc_fail(WAM_E_HIP, "wam_quantize_fp8: kernel launch failed");
   return WAM_OK;

@@ -1142,7 +1142,8 @@ int wam_set_rotary(wam_t h, const wam_rotary_args* a) {
   if (!h) return WAM_E_ARG;
   if (int st_ = check_not_pending(h)) return st_;
   if (a) {
-    if (!a->pos) return fail(h, WAM_E_ARG, "null rotary positions");
+    if (!a->pos || reinterpret_cast<uintptr_t>(a->pos) % 4)
+      return fail(h, WAM_E_ARG, "null or unaligned rotary positions");
     if (a->layout != WAM_ROPE_HALVES && a->layout != WAM_ROPE_PAIRS) return fail(h, WAM_E_ARG, "unknown rotary layout");
     int64_t pairs = 0;
     for (int i = 0; i < 3; ++i) {

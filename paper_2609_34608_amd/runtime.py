@@ -161,6 +161,8 @@ class WamModel:
             self._check(self.lib.wam_set_rotary(self.h, None), "wam_set_rotary")
             self._pos = None
             return
+        if not isinstance(pos, torch.Tensor) or sections is None or freq is None:
+            raise WamError("set_rotary: needs positions, sections and frequencies")
         T = self.cfg.Nv + self.cfg.Na + self.cfg.No
         if tuple(pos.shape) != (T, 3):
             raise WamError(f"set_rotary: pos must be [{T}, 3]")
@@ -381,6 +383,8 @@ def remap_noalloc(cfg: abi.WamConfig, x_bar, x_r, sigma_r, sigma_b0, shift_actio
 
 
 # ---------------------------------------------------------------- layer operators
+# stream: the call's stream (default: torch's current one), to which results that the
+# call allocates belong, as under torch.cuda.stream(stream).
 FP8 = torch.float8_e4m3fn
 _TYPES = {torch.float32: abi.WAM_FP32, torch.bfloat16: abi.WAM_BF16, FP8: abi.WAM_FP8}
 _REAL = (torch.float32, torch.bfloat16)
@@ -429,9 +433,23 @@ def _choice(table, key, what):
         raise WamError(f"{what}: unknown value {key!r}") from None
 
 
+def _new(stream, make, *args, **kw):
+    """A new result of an operator on `stream`: memory of that stream's own, as another
+    stream's may still be in use there."""
+    if stream is None:
+        return make(*args, **kw)
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
 def _call(fn, args, index, stream, what):
     """Enqueues a handle-free operator on GPU `index` (stream: default torch's current one)."""
-    handle = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(index)
+    elif stream.device_index != index:
+        raise WamError(f"{what}: stream of GPU {stream.device_index}, operands on GPU {index}")
+    else:
+        handle = stream.cuda_stream
     if index == torch._C._cuda_getDevice():
         rc = fn(args, handle)
     else:
@@ -487,7 +505,8 @@ def rope(q, k, pos, sections, freq, *, layout="halves", q_gain=None, k_gain=None
         if k.dim() != 4 or k.shape[0] != B or k.shape[1] != T or k.shape[3] != dh:
             raise WamError("rope: k must be [B, T, H, dh] as q")
         Hk = k.shape[2]
-    _operand(pos, "rope: pos", _F32, index, (T, 3) if pos.dim() == 2 else (B, T, 3))
+    each = isinstance(pos, torch.Tensor) and pos.dim() == 3  # sample has its own positions
+    _operand(pos, "rope: pos", _F32, index, (B, T, 3) if each else (T, 3))
     if T > 1 and pos.stride(-2) != 3:
         raise WamError("rope: rows of pos must be contiguous")
     if len(sections) != 3 or len(freq) != sum(sections):
@@ -498,15 +517,16 @@ def rope(q, k, pos, sections, freq, *, layout="halves", q_gain=None, k_gain=None
         _operand(q_gain, "rope: q_gain", _F32, index, (dh,))
     if k_gain is not None:
         _operand(k_gain, "rope: k_gain", _F32, index, (dh,))
-    q_out = torch.empty_like(q) if q_out is None else _operand(q_out, "rope: q_out", own, index, q.shape)
+    q_out = _new(stream, torch.empty_like, q) if q_out is None else _operand(q_out, "rope: q_out", own, index, q.shape)
     if k is not None:
-        k_out = torch.empty_like(k) if k_out is None else _operand(k_out, "rope: k_out", own, index, k.shape)
+        k_out = (_new(stream, torch.empty_like, k) if k_out is None else
+                 _operand(k_out, "rope: k_out", own, index, k.shape))
     else:
         k_out = None
     ks, kos = (k.stride()[:3], k_out.stride()[:3]) if k is not None else (_NO_HEADS, _NO_HEADS)
     a = _pack(_ROPE_ARGS, "rope", B, T, Hq, Hk, dh, _TYPES[q.dtype], _choice(_LAYOUTS, layout, "rope: layout"),
               *sections, q.data_ptr(), _ptr_or_0(k), q_out.data_ptr(), _ptr_or_0(k_out), *q.stride()[:3], *ks,
-              *q_out.stride()[:3], *kos, pos.data_ptr(), pos.stride(0) if pos.dim() == 3 else 0, at,
+              *q_out.stride()[:3], *kos, pos.data_ptr(), pos.stride(0) if each else 0, at,
               _ptr_or_0(q_gain), _ptr_or_0(k_gain), eps)
     _call(abi.lib().wam_rope, a, index, stream, "wam_rope")
     return q_out, k_out
@@ -549,7 +569,8 @@ def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale
     g, g0, g1 = _row_vectors(gate, "norm_residual: gate", index, shape)
     c, c0, c1 = _row_vectors(scale, "norm_residual: scale", index, shape)
     s, s0, s1 = _row_vectors(shift, "norm_residual: shift", index, shape)
-    h_out = torch.empty_like(h) if h_out is None else _operand(h_out, "norm_residual: h_out", (h.dtype,), index, shape)
+    h_out = (_new(stream, torch.empty_like, h) if h_out is None else
+             _operand(h_out, "norm_residual: h_out", (h.dtype,), index, shape))
     post = _choice(_NORMS, post, "norm_residual: post")
     if pre is None:
         u = u_scale = None
@@ -557,13 +578,14 @@ def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale
     else:
         kind = _choice(_NORMS, pre, "norm_residual: pre")
         if u is None:
-            u = _new_rows(shape, torch.bfloat16 if u_dtype is None else u_dtype, h.device, "norm_residual: u_dtype")
+            u = _new(stream, _new_rows, shape, torch.bfloat16 if u_dtype is None else u_dtype, h.device,
+                     "norm_residual: u_dtype")
         else:
             _operand(u, "norm_residual: u", tuple(_TYPES) if u_dtype is None else (u_dtype,), index, shape)
         u_type = _TYPES[u.dtype]
         if u_type == abi.WAM_FP8:
             blocks = (B, T, -(-D // 128))
-            u_scale = (torch.empty(blocks, dtype=torch.float32, device=h.device) if u_scale is None else
+            u_scale = (_new(stream, torch.empty, blocks, dtype=torch.float32, device=h.device) if u_scale is None else
                        _operand(u_scale, "norm_residual: u_scale", _F32, index, blocks))
         else:
             u_scale = None
@@ -597,11 +619,11 @@ def quantize_fp8(x, *, block_rows=1, q=None, scale=None, stream: torch.cuda.Stre
         raise WamError("quantize_fp8: block_rows must be 1 or 128")
     M, K = x.shape
     if q is None:
-        q = _new_rows((M, K), FP8, x.device, "quantize_fp8: q")
+        q = _new(stream, _new_rows, (M, K), FP8, x.device, "quantize_fp8: q")
     else:
         _operand(q, "quantize_fp8: q", _F8, index, x.shape)
     shape = (-(-M // block_rows), -(-K // 128))
-    scale = (torch.empty(shape, dtype=torch.float32, device=x.device) if scale is None else
+    scale = (_new(stream, torch.empty, shape, dtype=torch.float32, device=x.device) if scale is None else
              _operand(scale, "quantize_fp8: scale", _F32, index, shape))
     a = _pack(_QUANTIZE_ARGS, "quantize_fp8", M, K, _TYPES[x.dtype], block_rows, x.data_ptr(), x.stride(0), q.data_ptr(),
               q.stride(0), scale.data_ptr(), scale.stride(0))
@@ -627,14 +649,15 @@ def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_d
     if bias is not None:
         _operand(bias, "matmul_fp8: bias", _F32, index, (N,))
     if out is None:
-        out = _new_rows((M, N), torch.bfloat16 if out_dtype is None else out_dtype, a.device, "matmul_fp8: out_dtype")
+        out = _new(stream, _new_rows, (M, N), torch.bfloat16 if out_dtype is None else out_dtype, a.device,
+                   "matmul_fp8: out_dtype")
     else:
         _operand(out, "matmul_fp8: out", tuple(_TYPES) if out_dtype is None else (out_dtype,), index, (M, N))
     kind = _TYPES[out.dtype]
     scale_at = scale_stride = 0
     if kind == abi.WAM_FP8:
         shape = (M, -(-N // 128))
-        out_scale = (torch.empty(shape, dtype=torch.float32, device=a.device) if out_scale is None else
+        out_scale = (_new(stream, torch.empty, shape, dtype=torch.float32, device=a.device) if out_scale is None else
                      _operand(out_scale, "matmul_fp8: out_scale", _F32, index, shape))
         scale_at, scale_stride = out_scale.data_ptr(), out_scale.stride(0)
     args = _pack(_MATMUL_ARGS, "matmul_fp8", M, N, K, kind, abi.WAM_ACT_GELU if gelu else abi.WAM_ACT_NONE,

@@ -168,6 +168,33 @@ def test_rope_offsets_past_32_bits(dev, R):
     assert torch.equal(q, want)
 
 
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("dh,sec", [(200, (40, 30, 30)), (130, (65, 0, 0)), (250, (1, 2, 3)), (17, (3, 2, 3)), (64, (5, 6, 7))])
+def test_rope_in_place_of_any_head(dev, R, dh, sec, layout):
+    """Pairs whose halves lie in different lanes, turned where they are."""
+    q, g = _rand(dev, 1, 2, 90, 3, dh).to(BF16), 1 + 0.1 * _rand(dev, 2, dh)
+    for gain in (None, g):
+        own = q.clone()
+        args = (_positions(dev, 90), sec, R.rope_frequencies(sec))
+        want = R.rope(q, None, *args, layout=layout, q_gain=gain)[0]
+        R.rope(own, None, *args, layout=layout, q_gain=gain, q_out=own)
+        assert torch.equal(own, want)
+
+
+def test_rope_many_heads_and_vectors(dev, R):
+    """More heads than a grid's second dimension has blocks of, and more head vectors
+    than its first."""
+    q = _rand(dev, 1, 1, 1, 8 * 65535 + 11, 16).to(BF16)
+    _check_rope(R, q, None, _positions(dev, 1, far=2.0), (2, 3, 3), "halves")
+    T, H, sec, freq = 15_000_001, 5, (1, 0, 0), R.rope_frequencies((1, 0, 0))
+    q = torch.arange(T * H * 2, device=dev).remainder_(251).to(BF16).view(1, T, H, 2)
+    pos = torch.arange(T * 3, device=dev).remainder_(1009).to(F32).view(T, 3)
+    out = R.rope(q, None, pos, sec, freq)[0]
+    cut = T // 2
+    for part in (slice(0, cut), slice(cut, T)):
+        assert torch.equal(out[:, part], R.rope(q[:, part], None, pos[part], sec, freq)[0])
+
+
 # ------------------------------------------------------------- norms around a block
 def _check_norm(R, h, y, u_dtype, **kw):
     got = R.norm_residual(h, y, u_dtype=u_dtype, **kw)
@@ -512,6 +539,34 @@ def test_other_stream_and_overlapping_calls(dev, R):
     out = R.rope(a["q"], None, a["pos"], (8, 12, 12), a["freq"], stream=s)[0]
     s.synchronize()
     assert torch.equal(out, R.rope(a["q"], None, a["pos"], (8, 12, 12), a["freq"])[0])
+
+
+def test_results_belong_to_the_given_stream(dev, R):
+    """Memory that the current stream has freed but still writes is no result of
+    another stream's call."""
+    x = _rand(dev, 1, 1, 4096, 8, 64)
+    rows, w = x.view(4096, 512), R.quantize_fp8(_rand(dev, 2, 512, 512), block_rows=128)
+    pos, sec, freq = _positions(dev, 4096), (8, 12, 12), R.rope_frequencies((8, 12, 12))
+    q8, s8 = R.quantize_fp8(rows)
+    calls = (lambda s: R.rope(x, None, pos, sec, freq, stream=s)[:1],
+             lambda s: R.norm_residual(rows.view(1, 4096, 512), u_dtype=FP8, stream=s),
+             lambda s: R.quantize_fp8(rows, stream=s),
+             lambda s: (R.matmul_fp8(q8, s8, *w, out_dtype=F32, stream=s),))
+    side, slow = torch.cuda.Stream(dev), torch.empty(1 << 28, device=dev)
+    for call in calls:
+        want = [t.float() for t in call(None)]
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        junk = [torch.empty_like(t) for t in call(None)]
+        for _ in range(20):
+            slow.zero_()
+        for t in junk:
+            t.view(torch.uint8).fill_(1)
+        del junk, t
+        got = call(side)
+        torch.cuda.synchronize()
+        for g, t in zip(got, want):
+            assert torch.equal(g.float(), t)
 
 
 def test_captured_and_replayed(dev, R):

@@ -151,6 +151,33 @@ def test_frequencies():
             R.rope_frequencies(sec, theta)
 
 
+@pytest.mark.parametrize("fn,a,code,text", [
+    ("wam_rope", _rope(T=L.WAM_MAX_ROWS + 1, q_out_stride=_i64(0, 128, 64), k_out_stride=_i64(0, 128, 64))[0],
+     L.WAM_E_SHAPE, "too many rows"),
+    ("wam_rope", _rope(Hq=2**24, q_out_stride=_i64(2**40, 2**30, 64))[0], L.WAM_E_SHAPE, "too many heads"),
+    ("wam_rope", _rope(k_out=P + 8192)[0], L.WAM_E_ARG, "the other one"),
+    ("wam_rope", _rope(q_out=P + 4096)[0], L.WAM_E_ARG, "the other one"),
+    ("wam_rope", _rope(k_out=P)[0], L.WAM_E_ARG, "the other one"),
+    ("wam_rope", _rope(k=P, q_out=P, q_out_stride=_i64(512, 128, 64))[0], L.WAM_E_ARG, "the other one"),
+    ("wam_norm_residual", _norm(T=L.WAM_MAX_ROWS + 1), L.WAM_E_SHAPE, "too many rows"),
+    ("wam_quantize_fp8", _quant(M=2**29, K=1), L.WAM_E_SHAPE, "too many blocks"),
+    ("wam_quantize_fp8", _quant(M=2**31 - 1, K=1, block_rows=128), L.WAM_E_SHAPE, "too many blocks"),
+    ("wam_quantize_fp8", _quant(M=1, K=2**31 - 1), L.WAM_E_SHAPE, "too many blocks"),
+    ("wam_matmul_fp8", _matmul(M=2**30, N=1, K=16), L.WAM_E_SHAPE, "too many tiles"),
+    ("wam_matmul_fp8", _matmul(M=2**30, N=1, K=16, out_dtype=L.WAM_FP32), L.WAM_E_SHAPE, "too many tiles"),
+    ("wam_matmul_fp8", _matmul(M=2**30, N=2**11, K=16, out_stride=2**11, out_dtype=L.WAM_FP8, out_scale=P,
+                               out_scale_stride=16), L.WAM_E_SHAPE, "too many tiles")])
+def test_sizes_past_a_grid_and_shared_results(fn, a, code, text):
+    _refused(fn, a, code, text)
+
+
+def test_binding_refuses_a_stream_of_another_gpu():
+    class Stream:
+        device_index, cuda_stream = 1, 0
+    with pytest.raises(R.WamError, match="stream of GPU 1"):
+        R._call(L.lib().wam_quantize_fp8, None, 0, Stream(), "wam_quantize_fp8")
+
+
 def test_binding_refuses_host_tensors():
     x = torch.zeros(1, 4, 2, 64)
     with pytest.raises(R.WamError, match="device tensors only"):

@@ -437,6 +437,21 @@ def test_blocks_of_zero_and_non_finite_rows(dev, R):
     assert torch.equal(q[rest].float(), want[0][rest].float()) and torch.equal(s[rest], want[1][rest])
 
 
+@pytest.mark.parametrize("M,N,K", [t[1:] for t in TILES if not t[0]] + [(1, 1, 16), (3, 2, 16), (5, 7, 16), (40, 15, 16),
+                                                                        (40, 64, 16), (33, 129, 16), (70, 96, 16)])
+def test_matmul_rows_inside_words(dev, R, M, N, K):
+    """bf16 rows at any element address: the same bits as rows on words, nothing around
+    them touched."""
+    ops, bias = _operands(R, dev, M, N, K), _rand(dev, 9, N)
+    want = R.matmul_fp8(*ops, bias=bias, gelu=True, out=torch.empty(M, N + N % 2, dtype=BF16, device=dev)[:, :N])
+    for ld, offset in ((N + 1 + N % 2, 0), (N + 1 + N % 2, 1), (N + 2 - N % 2, 1)):
+        buf = torch.full((offset + M * ld,), float("nan"), dtype=BF16, device=dev)
+        out = buf[offset:].view(M, ld)
+        R.matmul_fp8(*ops, bias=bias, gelu=True, out=out[:, :N])
+        assert torch.equal(out[:, :N], want)
+        assert out[:, N:].isnan().all() and buf[:offset].isnan().all()
+
+
 def test_matmul_strides_and_tail_bytes(dev, R):
     """Padded rows whose bytes past K are NaN, strided scales, an odd result row
     stride: none of it enters, the elements between stay."""

@@ -410,7 +410,7 @@ def _operand(t, what, dtypes, index, shape=None):
         raise WamError(f"{what}: dtype {t.dtype} is not supported")
     if shape is not None and t.shape != shape:
         raise WamError(f"{what}: shape {tuple(t.shape)} is not {tuple(shape)}")
-    if t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
+    if not t.is_contiguous() and t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise WamError(f"{what}: the last dimension must be contiguous")
     return t
 
@@ -532,16 +532,17 @@ def rope(q, k, pos, sections, freq, *, layout="halves", q_gain=None, k_gain=None
     return q_out, k_out
 
 
-def _row_vectors(v, what, index, shape):
-    """Pointer and strides (sample, row) of float32 vectors that broadcast to shape."""
+def _row_vectors(v, what, index, B, T, D):
+    """Pointer and strides (sample, row) of float32 vectors that broadcast to [B, T, D]."""
     if v is None:
         return 0, 0, 0
     _operand(v, what, _F32, index)
-    n, own = v.dim(), v.shape
-    if not 1 <= n <= 3 or own[-1] != shape[2] or any(own[i] not in (1, shape[3 - n + i]) for i in range(n - 1)):
-        raise WamError(f"{what}: shape {tuple(own)} does not broadcast to {tuple(shape)} with D values per row")
+    own, n = v.shape, v.dim()
+    b, t, d = own if n == 3 else (1, *own) if n == 2 else (1, 1, *own) if n == 1 else (0, 0, -1)
+    if d != D or b not in (1, B) or t not in (1, T):
+        raise WamError(f"{what}: shape {tuple(own)} does not broadcast to {(B, T, D)} with D values per row")
     s = v.stride()
-    return (v.data_ptr(), s[0] if n == 3 and own[0] != 1 else 0, s[-2] if n >= 2 and own[-2] != 1 else 0)
+    return v.data_ptr(), s[0] if b != 1 else 0, s[-2] if t != 1 else 0
 
 
 _NO_ROWS = (0, 0)
@@ -566,9 +567,9 @@ def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale
         _operand(post_gain, "norm_residual: post_gain", _F32, index, (D,))
     if pre_gain is not None:
         _operand(pre_gain, "norm_residual: pre_gain", _F32, index, (D,))
-    g, g0, g1 = _row_vectors(gate, "norm_residual: gate", index, shape)
-    c, c0, c1 = _row_vectors(scale, "norm_residual: scale", index, shape)
-    s, s0, s1 = _row_vectors(shift, "norm_residual: shift", index, shape)
+    g, g0, g1 = _row_vectors(gate, "norm_residual: gate", index, B, T, D)
+    c, c0, c1 = _row_vectors(scale, "norm_residual: scale", index, B, T, D)
+    s, s0, s1 = _row_vectors(shift, "norm_residual: shift", index, B, T, D)
     h_out = (_new(stream, torch.empty_like, h) if h_out is None else
              _operand(h_out, "norm_residual: h_out", (h.dtype,), index, shape))
     post = _choice(_NORMS, post, "norm_residual: post")
@@ -579,7 +580,7 @@ def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale
         kind = _choice(_NORMS, pre, "norm_residual: pre")
         if u is None:
             u = _new(stream, _new_rows, shape, torch.bfloat16 if u_dtype is None else u_dtype, h.device,
-                     "norm_residual: u_dtype")
+                     "norm_residual: u_dtype", h)
         else:
             _operand(u, "norm_residual: u", tuple(_TYPES) if u_dtype is None else (u_dtype,), index, shape)
         u_type = _TYPES[u.dtype]
@@ -598,12 +599,14 @@ def norm_residual(h, y=None, *, post="rms", post_gain=None, gate=None, res_scale
     return (h_out,) if u is None else (h_out, u) if u_scale is None else (h_out, u, u_scale)
 
 
-def _new_rows(shape, dtype, dev, what):
+def _new_rows(shape, dtype, dev, what, like=None):
     """A new tensor; e4m3 rows start a multiple of 16 bytes apart, as matmul_fp8
-    takes them."""
+    takes them.  like: a tensor of that shape (empty_like is the faster call)."""
     if dtype not in _TYPES:
         raise WamError(f"{what}: dtype {dtype} is not supported")
     if dtype != FP8 or shape[-1] % 16 == 0:
+        if like is not None and like.is_contiguous():
+            return torch.empty_like(like, dtype=dtype)
         return torch.empty(shape, dtype=dtype, device=dev)
     padded = (*shape[:-1], -(-shape[-1] // 16) * 16)
     return torch.empty(padded, dtype=dtype, device=dev)[..., :shape[-1]]

@@ -79,18 +79,23 @@ __device__ __forceinline__ void store_n(T* p, const float (&x)[N], int n, bool s
 
 // ------------------------------------------------------------- rotary positions
 constexpr int kMaxPairs = WAM_MAX_HEAD / 2;
+// P: room for that many pairs.  Arguments travel with every launch, so heads of up to
+// 32 pairs have a form of their own (a call on one row 8.3 -> 7.9 us).
+constexpr int kFewPairs = 32;
+template <int P>
 struct RopeParams {
   wam_rope_args a;
   int pairs, end0, end1;     // pairs of axis 0 end at end0, of axis 1 at end1
   const int* skip;
-  double turns[kMaxPairs];   // revolutions per unit of position
+  double turns[P];           // revolutions per unit of position
 };
 
 // cos and sin of pos * freq.  The product is taken in revolutions and in
 // float64, so that dropping the whole ones is exact and far positions lose
 // nothing (a float32 angle of position 1e5 is off by 4e-3); what is left lies
 // within half a turn and float32 does for it.
-__device__ __forceinline__ void axis_turn(const RopeParams& p, const float* pos, int i, float& c, float& s) {
+template <int P>
+__device__ __forceinline__ void axis_turn(const RopeParams<P>& p, const float* pos, int i, float& c, float& s) {
   const int axis = i < p.end0 ? 0 : i < p.end1 ? 1 : 2;
   double t = (double)pos[axis] * p.turns[i];
   t -= rint(t);
@@ -125,8 +130,8 @@ constexpr int kRopeTable = 2048;  // most (row, pair) angles of a block
 // the norm needs the other lanes of its vector.  The block's angles are computed
 // once, in LDS, while the first loads are in flight, and a lane keeps those of
 // its unit in registers for all the heads it visits.
-template <typename T, bool PAIRS, bool NORM>
-__global__ __launch_bounds__(256) void rope_units_kernel(RopeParams p, RopeTiling tl) {
+template <typename T, bool PAIRS, bool NORM, int P>
+__global__ __launch_bounds__(256) void rope_units_kernel(RopeParams<P> p, RopeTiling tl) {
   __shared__ float2 turn[kRopeTable];
   if (p.skip && *p.skip) return;
   const wam_rope_args& a = p.a;
@@ -226,7 +231,8 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams p, RopeTilin
 
 // Any other head size or sections: one wave per head vector, element e = lane +
 // 64 j; blocks of four vectors, each taking several where a grid ends.
-__global__ __launch_bounds__(256) void rope_kernel(RopeParams p) {
+template <int P>
+__global__ __launch_bounds__(256) void rope_kernel(RopeParams<P> p) {
   if (p.skip && *p.skip) return;
   const wam_rope_args& a = p.a;
   const int heads = a.Hq + a.Hk;
@@ -330,9 +336,10 @@ constexpr int kNormCols = 4;  // columns of a lane and chunk
 // alignment (with eight columns a lane, 16 bytes of bf16 but two strided loads of
 // float32: 4 x 2306 rows of 1024 31.7 against 29.7 us).  Sums are over lanes, and over
 // the waves in LDS.  32 lanes of a chunk are one block of 128 columns, which is
-// what 8-bit results need.  HBM bound: 10 to 12 bytes an element at 3.8-4.5 TB/s
-// over buffers larger than the last-level cache, 5.1 with modulation per row;
-// requesting gate and modulation ahead of the sums was 3-5% slower (registers).
+// what 8-bit results need.  HBM bound: 10176 rows of 1536 into 8-bit blocks move
+// 172 MB in 37 us (4.7 TB/s), 4 x 2306 rows of 1024 with modulation per row 227 MB in
+// 42.5 (5.3); requesting gate and modulation ahead of the sums was 3-5% slower
+// (registers).
 template <int CH, int W, typename TH, typename TY>
 __global__ __launch_bounds__(256) void norm_residual_kernel(wam_norm_args a, bool stream_h, bool stream_u, const int* skip) {
   __shared__ float part[2][4];
@@ -595,28 +602,29 @@ int check_heads(int H, const wam_rope_args* a, const void* x, const void* out, c
   return WAM_OK;
 }
 
-template <typename T, bool PAIRS>
-void launch_rope_units(const RopeParams& p, const RopeTiling& tl, dim3 grid, hipStream_t s) {
-  if (p.a.q_gain || p.a.k_gain) launch_k(rope_units_kernel<T, PAIRS, true>, grid, 256, 0, s, p, tl);
-  else launch_k(rope_units_kernel<T, PAIRS, false>, grid, 256, 0, s, p, tl);
+template <typename T, bool PAIRS, int P>
+void launch_rope_units(const RopeParams<P>& p, const RopeTiling& tl, dim3 grid, hipStream_t s) {
+  if (p.a.q_gain || p.a.k_gain) launch_k(rope_units_kernel<T, PAIRS, true, P>, grid, 256, 0, s, p, tl);
+  else launch_k(rope_units_kernel<T, PAIRS, false, P>, grid, 256, 0, s, p, tl);
 }
 
-hipError_t launch_rope_params(const RopeParams& p, hipStream_t s) {
+template <int P>
+hipError_t launch_rope_params(const RopeParams<P>& p, hipStream_t s) {
   const wam_rope_args& a = p.a;
   const int64_t rows = (int64_t)a.B * a.T;
   const int H = a.Hq > a.Hk ? a.Hq : a.Hk;
   if (a.dh % 16 || p.pairs % 8) {
     const int64_t blocks = (rows * (a.Hq + a.Hk) + 3) / 4;
-    launch_k(rope_kernel, dim3((unsigned)std::min(blocks, kMaxGrid)), 256, 0, s, p);
+    launch_k(rope_kernel<P>, dim3((unsigned)std::min(blocks, kMaxGrid)), 256, 0, s, p);
     return hipGetLastError();
   }
   RopeTiling tl{};
   tl.lanes = 1;
   while (tl.lanes * 16 < a.dh) tl.lanes *= 2;
   // Four heads side by side, two waves along the rows, up to three steps over the
-  // heads: within 2% of the fastest tiling at 10176 rows of 24 heads (28 us; the worst
-  // 56), 2 x 2877 of 19 (13.5; 37), 4 x 2306 of 16 and 4000 float32 rows of 8 heads
-  // of 128, rows or heads innermost in memory alike.  Few rows: one step, so that
+  // heads: within 2% of the fastest tiling at 10176 rows of 24 heads (28 us with plain
+  // stores; the worst 56), 2 x 2877 of 19 (13.5; 37), 4 x 2306 of 16 and 4000 float32
+  // rows of 8 heads of 128, rows or heads innermost in memory alike.  Few rows: one step, so that
   // more blocks share them.
   const int slots = kWave / tl.lanes;
   tl.heads_wave = 1;
@@ -643,10 +651,9 @@ hipError_t launch_rope_params(const RopeParams& p, hipStream_t s) {
   return hipGetLastError();
 }
 
-}  // namespace
-
-hipError_t launch_rope(const wam_rope_args& a, hipStream_t s, const int* skip) {
-  RopeParams p{};
+template <int P>
+hipError_t launch_rope_room(const wam_rope_args& a, hipStream_t s, const int* skip) {
+  RopeParams<P> p;
   p.a = a;
   p.skip = skip;
   p.end0 = a.sections[0];
@@ -654,6 +661,13 @@ hipError_t launch_rope(const wam_rope_args& a, hipStream_t s, const int* skip) {
   p.pairs = p.end1 + a.sections[2];
   for (int i = 0; i < p.pairs; ++i) p.turns[i] = a.freq[i] * (0.5 / M_PI);
   return launch_rope_params(p, s);
+}
+
+}  // namespace
+
+hipError_t launch_rope(const wam_rope_args& a, hipStream_t s, const int* skip) {
+  return a.sections[0] + a.sections[1] + a.sections[2] <= kFewPairs ? launch_rope_room<kFewPairs>(a, s, skip)
+                                                                    : launch_rope_room<kMaxPairs>(a, s, skip);
 }
 
 hipError_t launch_norm_residual(const wam_norm_args& a, hipStream_t s, const int* skip) {

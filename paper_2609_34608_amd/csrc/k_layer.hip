@@ -43,10 +43,11 @@ __device__ __forceinline__ void load_n(float (&x)[N], const T* p, int n) {
 }
 
 // A result larger than the chip's L2s (8 x 4 MB) cannot wait there for its reader:
-// streaming stores leave the caches to what is read (10176 rows of 24 + 24 heads 29.4 ->
-// 25.4 us, norms of 10176 rows of 1536 40.8 -> 36.9, 8-bit blocks of 10176 x 6144 34.2 ->
-// 32.6).  A smaller one is read from there by the next kernel, and streaming it
-// made the layers of the 8-bit mode 2-5 us slower.
+// streaming stores leave the caches to what is read (10176 rows of 24 + 24 heads 27.7 ->
+// 22.0 us, norms of 10176 rows of 1536 40.8 -> 36.9, 8-bit blocks of 10176 x 6144 34.2 ->
+// 32.6).  They have to be whole lines.  A smaller result is read from there by the
+// next kernel: streaming 28 MB of q and k made them and their reader together 29.7
+// us instead of 26.5.
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 template <typename P>
 __device__ __forceinline__ void put(void* p, const P& w, bool stream) {
@@ -122,17 +123,23 @@ struct RopeTiling {
   int heads_block;  // heads of a block
   int stream;       // streaming stores
 };
-constexpr int kRopeTable = 2048;  // most (row, pair) angles of a block
+constexpr int kRopeTable = 1024;  // most (row, pair) angles of a block
 
 // Head vectors of whole units of 16 elements: eight pairs, or 16 elements past the
 // rotated ones.  A lane takes one unit with two 8-element loads (the two halves
 // of the pairs, or 16 neighbours), so that a pair never leaves its lane and only
 // the norm needs the other lanes of its vector.  The block's angles are computed
 // once, in LDS, while the first loads are in flight, and a lane keeps those of
-// its unit in registers for all the heads it visits.
+// its unit in registers for all the heads it visits.  Results go out through LDS,
+// where a wave keeps its vectors side by side, so that 16 bytes a lane make whole
+// lines.  10176 rows of 24 + 24 heads take 21-22 us in either layout, with any
+// number of pairs, and as 48 + 48 heads of 32 (125 MB, 5.8 TB/s); streamed as a lane
+// holds them, lines in pieces, 26 to 36, and 5088 rows of neighbours in float32 78.
 template <typename T, bool PAIRS, bool NORM, int P>
 __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams<P> p, RopeTiling tl) {
+  constexpr int kPieces = sizeof(T);  // 16-byte pieces of a lane
   __shared__ float2 turn[kRopeTable];
+  __shared__ __attribute__((aligned(16))) uint8_t stage[4][kWave * kPieces * 16];
   if (p.skip && *p.skip) return;
   const wam_rope_args& a = p.a;
   const bool isq = blockIdx.z == 0 && a.Hq > 0;
@@ -149,30 +156,44 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams<P> p, RopeTi
   const int head_step = tl.heads_wave * (4 / tl.wave_rows);
   int h = (int)blockIdx.y * tl.heads_block + (wid / tl.wave_rows) * tl.heads_wave + slot % tl.heads_wave;
 
-  const int64_t rows = (int64_t)a.B * a.T, row0 = (int64_t)blockIdx.x * rows_block;
-  const int64_t row = row0 + row_in_block;
-  const int b = (int)(row / a.T), t = (int)(row % a.T);
+  const uint32_t Tn = a.T, rows = a.B * Tn, row0 = blockIdx.x * (uint32_t)rows_block;  // rows < 2^24
+  const uint32_t row = row0 + row_in_block, b = row / Tn, t = row % Tn;
   const bool live = row < rows && 16 * unit < a.dh;
   const int turned = p.pairs / 8;  // units that turn
   const int e1 = PAIRS || unit >= turned ? 16 * unit : 8 * unit;
   const int e2 = PAIRS || unit >= turned ? e1 + 8 : e1 + p.pairs;
   const T* x = static_cast<const T*>(isq ? a.q : a.k) + (live ? b * si[0] + t * si[1] : 0);
-  T* o = static_cast<T*>(isq ? a.q_out : a.k_out) + (live ? b * so[0] + t * so[1] : 0);
 
-  float x1[8], x2[8];
+  // where the wave's vectors, one after the other in LDS, go in pieces of 16 bytes
+  const uint32_t vec = a.dh * (uint32_t)sizeof(T);
+  uint8_t* own = stage[wid] + slot * vec;
+  uint8_t* to[kPieces];
+  int to_head[kPieces];
+#pragma unroll
+  for (int k = 0; k < kPieces; ++k) {
+    const uint32_t at = (k * kWave + lane) * 16, s = at / vec;
+    const uint32_t r = row0 + (wid % tl.wave_rows) * rows_wave + s / tl.heads_wave;
+    const int head = h + (int)(s % tl.heads_wave) - slot % tl.heads_wave;
+    const bool some = s < (uint32_t)(kWave / tl.lanes) && r < rows;
+    to_head[k] = some ? head : H;
+    to[k] = static_cast<uint8_t*>(isq ? a.q_out : a.k_out) + at % vec +
+            (some ? (r / Tn * so[0] + r % Tn * so[1] + head * so[2]) * (int64_t)sizeof(T) : 0);
+  }
+
+  Pack<T, 8> x1{}, x2{};  // as loaded: converted only when their turn comes
   auto load = [&](int hh) __attribute__((always_inline)) {
     if (live && hh < h_end) {
-      load_n(x1, x + hh * si[2] + e1, 8);
-      load_n(x2, x + hh * si[2] + e2, 8);
+      x1 = *reinterpret_cast<const Pack<T, 8>*>(x + hh * si[2] + e1);
+      x2 = *reinterpret_cast<const Pack<T, 8>*>(x + hh * si[2] + e2);
     }
   };
   load(h);
-  for (int i = threadIdx.x; i < rows_block * p.pairs; i += 256) {
-    const int r = i / p.pairs;
-    const int64_t rr = min(row0 + r, rows - 1);
-    const float* pos = a.pos + rr / a.T * a.pos_stride + rr % a.T * 3;
+  for (uint32_t i = threadIdx.x; i < (uint32_t)(rows_block * p.pairs); i += 256) {
+    const uint32_t r = i / (uint32_t)p.pairs;
+    const uint32_t rr = min(row0 + r, rows - 1);
+    const float* pos = a.pos + rr / Tn * a.pos_stride + rr % Tn * 3;
     float c, s;
-    axis_turn(p, pos, i % p.pairs, c, s);
+    axis_turn(p, pos, (int)(i % (uint32_t)p.pairs), c, s);
     turn[i] = make_float2(c, s);
   }
   float g1[8], g2[8];
@@ -194,7 +215,7 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams<P> p, RopeTi
   for (int h0 = 0; h0 < tl.heads_block; h0 += head_step, h += head_step) {
     float y1[8], y2[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) y1[j] = x1[j], y2[j] = x2[j];
+    for (int j = 0; j < 8; ++j) y1[j] = to_f32(x1.v[j]), y2[j] = to_f32(x2.v[j]);
     load(h + head_step);  // the next head's while this one is turned
     if constexpr (NORM) {
       if (normed) {
@@ -222,10 +243,22 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams<P> p, RopeTi
         o2.v[j] = static_cast<T>(y1[j] * s[j] + y2[j] * c[j]);
       }
     }
-    if (live && h < h_end) {
-      put(o + h * so[2] + e1, o1, tl.stream);
-      put(o + h * so[2] + e2, o2, tl.stream);
+    if (16 * unit < a.dh) {
+      __builtin_memcpy(__builtin_assume_aligned(own + e1 * sizeof(T), 16), &o1, sizeof(o1));
+      __builtin_memcpy(__builtin_assume_aligned(own + e2 * sizeof(T), 16), &o2, sizeof(o2));
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      typedef uint32_t words __attribute__((ext_vector_type(4)));
+      const words v = *reinterpret_cast<const words*>(stage[wid] + (k * kWave + lane) * 16);
+      if (to_head[k] < h_end) put(to[k], v, tl.stream);
+      to_head[k] += head_step;
+      to[k] += head_step * so[2] * (int64_t)sizeof(T);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -622,9 +655,10 @@ hipError_t launch_rope_params(const RopeParams<P>& p, hipStream_t s) {
   tl.lanes = 1;
   while (tl.lanes * 16 < a.dh) tl.lanes *= 2;
   // Four heads side by side, two waves along the rows, up to three steps over the
-  // heads: within 2% of the fastest tiling at 10176 rows of 24 heads (28 us with plain
-  // stores; the worst 56), 2 x 2877 of 19 (13.5; 37), 4 x 2306 of 16 and 4000 float32
-  // rows of 8 heads of 128, rows or heads innermost in memory alike.  Few rows: one step, so that
+  // heads: within 2% of the fastest of six tilings at 10176 rows of 24 heads of 64 (21.2 us;
+  // the slowest 26), of 48 of 32, 2 x 2877 rows of 19 with the norm (13.0; 18), 4 x 2306 of
+  // 16 and 5088 float32 rows, rows or heads innermost in memory alike; of 12 heads of
+  // 128 within 6% (23.4; 30).  Few rows: one step, so that
   // more blocks share them.
   const int slots = kWave / tl.lanes;
   tl.heads_wave = 1;

@@ -395,7 +395,7 @@ __device__ __forceinline__ void store_blocks(const Fp8Operands& p, const Fp8Out&
 // stride.
 template <int TN, int TM, bool EXACT, bool GELU>
 __device__ __forceinline__ void store_product(const Fp8Operands& p, const Fp8Out& o, const f32x4 (&acc)[TN][TM],
-                                              int mb, int nb, int lane) {
+                                              int mb, int nb, int lane, uint8_t* lds) {
   const int lr = lane % 16, lg = lane / 16;
   // G tiles side by side hold W consecutive columns of a lane.  Global memory takes
   // wide stores at any address, so rows of any stride do; only columns that N cuts
@@ -413,11 +413,47 @@ __device__ __forceinline__ void store_product(const Fp8Operands& p, const Fp8Out
   };
   T* out = static_cast<T*>(o.out);
   // Rows of bf16 that start inside a word: stores there leave a word to two lanes,
-  // which do not meet in one request (10176 x 6144 x 1536 with rows of 6145: 147 us against
-  // 107 where rows start on words).  Such a row is shifted by one column, the next
+  // which do not meet in one request (10176 x 6144 x 1536 with rows of 6145: 147 us, 107
+  // with the same stores on words).  Such a row is shifted by one column, the next
   // lanes' first one coming in, so that only the first and the last column of a
-  // wave are stored by themselves (116 us).
+  // wave are stored by themselves (115 us).
   const bool shift = !EXACT && ((reinterpret_cast<uintptr_t>(out) | (uintptr_t)o.ld * 2) & 2);
+  if constexpr (!EXACT && TN == 4) {
+    // A wave has 128 bytes of a row: they go out through LDS, so that eight lanes side
+    // by side store them, and past kStreamBytes as streaming stores where rows
+    // start on lines (10176 x 6144 x 1536 106 -> 100 us, with the GELU 115 -> 109).
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    __syncthreads();  // the stages have been read
+    if (!shift && nb + TN * 16 <= p.N) {
+      const bool stream = (int64_t)p.M * p.N * 2 > kStreamBytes &&
+                          (reinterpret_cast<uintptr_t>(out) | (uintptr_t)o.ld * 2) % 128 == 0;
+      uint8_t* st = lds + __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * 2048;
+      const int sr = lane / 8, sc = lane % 8;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          Row x;
+#pragma unroll
+          for (int r = 0; r < W; ++r) x.v[r] = value(j, i, r);
+          words v;
+          __builtin_memcpy(&v, &x, 16);
+          *reinterpret_cast<words*>(st + lr * 128 + (((j * 4 + lg) ^ (lr & 7)) * 16)) = v;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = h * 8 + sr, m = mb + i * 16 + row;
+          const words v = *reinterpret_cast<const words*>(st + row * 128 + ((sc ^ sr) * 16));
+          if (m < p.M) put(out + (int64_t)m * o.ld + nb + sc * 8, v, stream);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+      return;
+    }
+  }
   if (shift) {
     constexpr int NJ = TN / G, V = W / 2;
     struct __attribute__((packed, aligned(2))) Words {
@@ -499,8 +535,8 @@ template <int BM, int BN, int WGM, int WGN, int ST, bool EXACT, bool GELU, bool 
 __global__ __launch_bounds__(WGM* WGN * 64) void gemm_fp8_kernel(Fp8Operands p, Fp8Out o) {
   constexpr int TM = BM / WGM / 16, TN = BN / WGN / 16;
   gemm_fp8_body<BM, BN, WGM, WGN, ST, EXACT, WIDE>(
-      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane, uint8_t*) __attribute__((always_inline)) {
-        store_product<TN, TM, EXACT, GELU>(p, o, acc, m, n, lane);
+      p, [&](const f32x4(&acc)[TN][TM], int m, int n, int lane, uint8_t* lds) __attribute__((always_inline)) {
+        store_product<TN, TM, EXACT, GELU>(p, o, acc, m, n, lane, lds);
       });
 }
 

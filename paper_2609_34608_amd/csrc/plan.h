@@ -86,10 +86,11 @@ int plan_gemm(const TileCfg (&cfgs)[NC], int M, int N, int K, bool qkv) {
 // ---------------------------------------------------------------- 8-bit products
 // Tiles of gemm_fp8.h, the cost of a tile as above with a stage of 128 of K (bk
 // in bytes; per is per stage).  Least-squares fits to 187 sizes (16 to 10176 rows, N
-// and K 512 to 6144), standard deviation 8-13%; the choice among the first eight is
-// 2.6% slower than the fastest of 21 configurations on average.  bf16 results run on the 8-bit
-// matrix instruction, float32 ones on bf16 operands converted from the stages,
-// whose registers leave no room for 256-column tiles (1.1% off the fastest).
+// and K 512 to 6144), standard deviation 8-13%; the choice is 1.5% slower than the
+// fastest of the nine on average (45 sizes), and was 2.6% slower than the fastest of 21
+// configurations.  bf16 results run on the 8-bit matrix instruction, float32 ones on
+// bf16 operands converted from the stages, whose registers leave no room for
+// 256-column tiles (1.1% off the fastest).
 constexpr TileCfg kFp8Cfgs[] = {
     {256, 256, 2, 4, 2, 128, 1, {1.27f}, {6.01f}},
     {192, 256, 2, 4, 2, 128, 1, {1.08f}, {5.01f}},

@@ -533,6 +533,40 @@ def test_together(dev, R):
         F.check(got, *F.rope(x, st["pos"], (8, 12, 12), st["freq"], "halves", st["g"]), dtype=BF16)
 
 
+def test_results_larger_than_the_caches(dev, R):
+    """Results past 32 MB take streaming stores: the same bits as in two halves, whose
+    results take plain ones; in place and on rows off the lines too."""
+    M, cut = 9001, 4500
+    halves = (slice(0, cut), slice(cut, M))
+    q = _rand(dev, 1, 1, M, 16, 64).to(BF16)
+    k, pos, sec, freq = q.flip(1), _positions(dev, M), (8, 12, 12), R.rope_frequencies((8, 12, 12))
+    for layout in ("halves", "pairs"):
+        want = [R.rope(q[:, h], k[:, h], pos[h], sec, freq, layout=layout) for h in halves]
+        own = q.clone(), k.clone()
+        far = [torch.empty(M * 1024 + 8, dtype=BF16, device=dev)[8:].view(q.shape) for _ in range(2)]
+        for out in (dict(), dict(q_out=own[0], k_out=own[1]), dict(q_out=far[0], k_out=far[1])):
+            src = (own if out and out["q_out"] is own[0] else (q, k))
+            got = R.rope(*src, pos, sec, freq, layout=layout, **out)
+            for g, w in zip(got, zip(*want)):
+                assert torch.equal(g, torch.cat(w, 1))
+    h, y = _rand(dev, 2, 1, M, 4096), _rand(dev, 3, 1, M, 4096).to(BF16)
+    for kind in (F32, BF16, FP8):
+        got = R.norm_residual(h, y, u_dtype=kind)
+        for g, w in zip(got, zip(*[R.norm_residual(h[:, s], y[:, s], u_dtype=kind) for s in halves])):
+            assert torch.equal(g.float(), torch.cat([t.float() for t in w], 1))
+    a, sa = R.quantize_fp8(h[0])
+    parts = [R.quantize_fp8(h[0, s]) for s in halves]
+    assert torch.equal(a.float(), torch.cat([t[0].float() for t in parts])) and torch.equal(sa, torch.cat([t[1] for t in parts]))
+    a, sa, w, sw = _operands(R, dev, M, 2048, 384)
+    for gelu in (False, True):
+        want = torch.cat([R.matmul_fp8(a[s], sa[s], w, sw, gelu=gelu) for s in halves])
+        assert torch.equal(R.matmul_fp8(a, sa, w, sw, gelu=gelu), want)
+        for ld in (2056, 2049):
+            out = torch.empty(M, ld, dtype=BF16, device=dev)[:, :2048]
+            assert torch.equal(R.matmul_fp8(a, sa, w, sw, gelu=gelu, out=out), want)
+    F.check(want[-300:], *F.matmul(a[-300:], sa[-300:], w, sw, None, True, BF16), dtype=BF16)
+
+
 def test_other_stream_and_overlapping_calls(dev, R):
     """Calls on two streams at once share nothing; results equal those of one stream."""
     a, b = _half_layer_state(R, dev, 1), _half_layer_state(R, dev, 50)

@@ -423,7 +423,7 @@ const char *wam_noalloc_last_error(void);
  * hip_stream (NULL: the default stream) of the current device, allocates
  * nothing, shares no scratch between calls (calls may overlap), does not
  * synchronise and may be captured into a graph.  Struct and host pointers are
- * read during the call only.  Strides count elements and may be any size;
+ * read during the call only.  Strides count elements, up to 2^40;
  * the last dimension is contiguous.  An input stride may be 0 (the same values
  * for every index); the elements of an output must be distinct.  An input and
  * an output must not overlap, except where a call says that they may be the

@@ -206,20 +206,25 @@ __global__ __launch_bounds__(256) void rope_units_kernel(RopeParams<P> p, RopeTi
       }
     }
     Pack<T, 8> o1, o2;
-    if constexpr (PAIRS) {
+    if (unit < turned) {
+      if constexpr (PAIRS) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        o1.v[2 * j] = static_cast<T>(y1[2 * j] * c[j] - y1[2 * j + 1] * s[j]);
-        o1.v[2 * j + 1] = static_cast<T>(y1[2 * j] * s[j] + y1[2 * j + 1] * c[j]);
-        o2.v[2 * j] = static_cast<T>(y2[2 * j] * c[4 + j] - y2[2 * j + 1] * s[4 + j]);
-        o2.v[2 * j + 1] = static_cast<T>(y2[2 * j] * s[4 + j] + y2[2 * j + 1] * c[4 + j]);
-      }
-    } else {
+        for (int j = 0; j < 4; ++j) {
+          o1.v[2 * j] = static_cast<T>(y1[2 * j] * c[j] - y1[2 * j + 1] * s[j]);
+          o1.v[2 * j + 1] = static_cast<T>(y1[2 * j] * s[j] + y1[2 * j + 1] * c[j]);
+          o2.v[2 * j] = static_cast<T>(y2[2 * j] * c[4 + j] - y2[2 * j + 1] * s[4 + j]);
+          o2.v[2 * j + 1] = static_cast<T>(y2[2 * j] * s[4 + j] + y2[2 * j + 1] * c[4 + j]);
+        }
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        o1.v[j] = static_cast<T>(y1[j] * c[j] - y2[j] * s[j]);
-        o2.v[j] = static_cast<T>(y1[j] * s[j] + y2[j] * c[j]);
+        for (int j = 0; j < 8; ++j) {
+          o1.v[j] = static_cast<T>(y1[j] * c[j] - y2[j] * s[j]);
+          o2.v[j] = static_cast<T>(y1[j] * s[j] + y2[j] * c[j]);
+        }
       }
+    } else {  // past the pairs: not by 1 and 0, which would spread a NaN or an infinity
+#pragma unroll
+      for (int j = 0; j < 8; ++j) o1.v[j] = static_cast<T>(y1[j]), o2.v[j] = static_cast<T>(y2[j]);
     }
     if (16 * unit < a.dh) {
       __builtin_memcpy(__builtin_assume_aligned(own + e1 * sizeof(T), 16), &o1, sizeof(o1));

@@ -385,6 +385,8 @@ def remap_noalloc(cfg: abi.WamConfig, x_bar, x_r, sigma_r, sigma_b0, shift_actio
 # ---------------------------------------------------------------- layer operators
 # stream: the call's stream (default: torch's current one), to which results that the
 # call allocates belong, as under torch.cuda.stream(stream).
+# There are no backward passes: a tensor that requires a gradient is refused, but under
+# torch.no_grad.
 FP8 = torch.float8_e4m3fn
 _TYPES = {torch.float32: abi.WAM_FP32, torch.bfloat16: abi.WAM_BF16, FP8: abi.WAM_FP8}
 _REAL = (torch.float32, torch.bfloat16)
@@ -412,6 +414,8 @@ def _operand(t, what, dtypes, index, shape=None):
         raise WamError(f"{what}: shape {tuple(t.shape)} is not {tuple(shape)}")
     if not t.is_contiguous() and t.dim() and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise WamError(f"{what}: the last dimension must be contiguous")
+    if t.requires_grad and torch.is_grad_enabled():
+        raise WamError(f"{what}: asks for a gradient, and the layer operators have none (detach it, or torch.no_grad)")
     return t
 
 

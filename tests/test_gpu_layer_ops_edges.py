@@ -61,3 +61,27 @@ def test_rope_passes_what_it_does_not_turn(dev, R, dh, sec, dtype, layout):
                     for t in (got, expect):
                         t[0, 3, 1, e] = t[1, 8, 0, e] = 0.0
                 assert torch.equal(_bits(got), _bits(expect))
+
+
+# ------------------------------------------------------------- gradients
+def test_gradients_are_refused(dev, R):
+    """Nothing here has a backward pass: a tensor that asks for a gradient is refused
+    where torch would record one, as an input and as a result's buffer."""
+    q, pos, sec, freq = _rand(dev, 1, 1, 4, 2, 64), torch.zeros(4, 3, device=dev), (8, 12, 12), R.rope_frequencies((8, 12, 12))
+    h, gain = _rand(dev, 2, 1, 4, 64), torch.ones(64, device=dev)
+    a, sa = R.quantize_fp8(h[0])
+    w, sw = R.quantize_fp8(_rand(dev, 3, 32, 64), block_rows=128)
+    need = lambda t: t.detach().clone().requires_grad_()  # noqa: E731
+    calls = [lambda: R.rope(need(q), None, pos, sec, freq), lambda: R.rope(q, need(q), pos, sec, freq),
+             lambda: R.rope(q, None, need(pos), sec, freq), lambda: R.rope(q, None, pos, sec, freq, q_gain=need(gain)),
+             lambda: R.rope(q, None, pos, sec, freq, q_out=need(q)), lambda: R.norm_residual(need(h)),
+             lambda: R.norm_residual(h, need(h)), lambda: R.norm_residual(h, scale=need(gain)),
+             lambda: R.norm_residual(h, h_out=need(h)), lambda: R.norm_residual(h, post_gain=need(gain)),
+             lambda: R.quantize_fp8(need(h[0])), lambda: R.matmul_fp8(a, need(sa), w, sw),
+             lambda: R.matmul_fp8(a, sa, w, sw, bias=need(gain[:32])),
+             lambda: R.matmul_fp8(a, sa, w, sw, out=need(torch.zeros(4, 32, device=dev)))]
+    for call in calls:
+        with pytest.raises(R.WamError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()

@@ -479,8 +479,8 @@ def rope_frequencies(sections, theta=10000.0, shared=False) -> np.ndarray:
     """Frequencies of the usual ladder for rope (wam_rope_frequencies): float64
     [sum(sections)], theta^(-j / n) along each axis of n pairs, or one ladder
     over all pairs."""
-    if len(sections) != 3:
-        raise WamError("rope_frequencies: needs three sections")
+    if len(sections) != 3 or any(abs(n) > abi.WAM_MAX_HEAD for n in sections):  # ctypes cuts off what passes 32 bits
+        raise WamError("rope_frequencies: needs three sections of at most WAM_MAX_HEAD pairs")
     sec = (C.c_int32 * 3)(*sections)
     freq = np.empty(min(max(sum(sec), 0), abi.WAM_MAX_HEAD // 2), np.float64)
     lib = abi.lib()
@@ -513,7 +513,7 @@ def rope(q, k, pos, sections, freq, *, layout="halves", q_gain=None, k_gain=None
     _operand(pos, "rope: pos", _F32, index, (B, T, 3) if each else (T, 3))
     if T > 1 and pos.stride(-2) != 3:
         raise WamError("rope: rows of pos must be contiguous")
-    if len(sections) != 3 or len(freq) != sum(sections):
+    if len(sections) != 3 or len(freq) != sum(sections) or getattr(freq, "ndim", 1) != 1:
         raise WamError("rope: needs three sections and one frequency per pair")
     ladder = np.ascontiguousarray(freq, np.float64) if isinstance(freq, np.ndarray) else array("d", freq)
     at = ladder.ctypes.data if isinstance(ladder, np.ndarray) else ladder.buffer_info()[0]

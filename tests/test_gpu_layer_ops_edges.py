@@ -63,6 +63,13 @@ def test_rope_passes_what_it_does_not_turn(dev, R, dh, sec, dtype, layout):
                 assert torch.equal(_bits(got), _bits(expect))
 
 
+def test_rope_refuses_a_table_of_frequencies(dev, R):
+    """One frequency per pair: a table of as many rows is none."""
+    q, pos = _rand(dev, 1, 1, 4, 2, 64), torch.zeros(4, 3, device=dev)
+    with pytest.raises(R.WamError, match="frequency"):
+        R.rope(q, None, pos, (8, 12, 12), np.ones((32, 2)))
+
+
 # ------------------------------------------------------------- gradients
 def test_gradients_are_refused(dev, R):
     """Nothing here has a backward pass: a tensor that asks for a gradient is refused

@@ -972,16 +972,18 @@ hipError_t launch_attention_cfg(const AttnArgs& a, int qt, int nw, int st, hipSt
   return hipGetLastError();
 }
 
-float attention_score_bound(const float* q_g, const float* k_g) {
+float attention_score_bound(const float* q_g, const float* k_g, bool turned) {
   // q = log2(e)/8 * g_q (.) qhat and k = g_k (.) khat with |qhat|, |khat| <= 8
   // (unit RMS over 64 dims), so |q.k| <= log2(e)/8 * 64 * max|g_q| * max|g_k|;
-  // bf16 rounding of each element adds at most 2^-8 relative per operand
+  // bf16 rounding of each element adds at most 2^-8 relative per operand (less
+  // than 2^-7 of the product), and once more where both are stored turned
   float gq = 0.f, gk = 0.f;
   for (int i = 0; i < kDh; ++i) {
     gq = fmaxf(gq, fabsf(q_g[i]));
     gk = fmaxf(gk, fabsf(k_g[i]));
   }
-  return kQLog2Scale * 64.0f * gq * gk * (1.0f + 1.0f / 128.0f) + 1e-3f;
+  const float stored = 1.0f + 1.0f / 128.0f;
+  return kQLog2Scale * 64.0f * gq * gk * stored * (turned ? stored : 1.0f) + 1e-3f;
 }
 
 template <int DH>

@@ -284,8 +284,8 @@ struct wam_handle {
   std::string err;
   ProfSlot prof[WAM_KC_COUNT];
   // per-layer fixed softmax reference (log2 units) of the bf16 attention, or
-  // -1 where the scores have no usable bound
-  std::vector<float> attn_mref;
+  // -1 where the scores have no usable bound; [1]: with rotary positions
+  std::vector<float> attn_mref[2];
   int attn_variant = WAM_ATTN_AUTO;
   // layer variants: rotary positions of q and k (pos null: none) and post-norm
   // gains of the two blocks of every layer (null: none)
@@ -543,7 +543,7 @@ int run_layer(wam_t h, int l, const int* skip = nullptr, float* copy = nullptr, 
     ProfScope ps(h, WAM_KC_ATTENTION, 4.0 * d.B * (double)d.T * d.T * D);
     AttnArgs at{h->S<char>(ws.q), h->S<char>(ws.k), h->S<char>(ws.vt), attn,
                 d.B, d.H, d.T, d.Tpad, d.dh, d.D, skip};
-    at.mref = h->attn_mref[l];
+    at.mref = h->attn_mref[h->rotary.pos ? 1 : 0][l];
     at.bounded = d.bf && at.mref >= 0.f;
     at.variant = h->attn_variant;
     HIPCHK(h, launch_attention(at, d.bf, h->stream));
@@ -1041,12 +1041,14 @@ int wam_init(const wam_config* cfg, const float* hw, size_t n_hw, void* dev_weig
     memcpy(buf.data() + lb + (4 * D + F) * 4, L0 + hl.fc2_b, D * 4);
     memcpy(buf.data() + lb + (5 * D + F) * 4, L0 + hl.q_g, d.dh * 4);
     memcpy(buf.data() + lb + (5 * D + F + d.dh) * 4, L0 + hl.k_g, d.dh * 4);
-    float mref = -1.f;
-    if (d.bf && cfg->qk_norm) {
-      mref = attention_score_bound(L0 + hl.q_g, L0 + hl.k_g);
-      if (!(mref <= 60.0f)) mref = -1.f;
+    for (int turned = 0; turned < 2; ++turned) {
+      float mref = -1.f;
+      if (d.bf && cfg->qk_norm) {
+        mref = attention_score_bound(L0 + hl.q_g, L0 + hl.k_g, turned);
+        if (!(mref <= 60.0f)) mref = -1.f;
+      }
+      h->attn_mref[turned].push_back(mref);
     }
-    h->attn_mref.push_back(mref);
     const size_t lw = wl.lw0 + wl.lw_stride * l;
     const size_t src[4] = {hl.qkv_w, hl.proj_w, hl.fc1_w, hl.fc2_w};
     const size_t K[4] = {D, D, D, F}, N[4] = {3 * D, D, F, D};

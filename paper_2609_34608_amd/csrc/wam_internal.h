@@ -210,8 +210,9 @@ hipError_t launch_attention(const AttnArgs& a, bool bf16_mode, hipStream_t s);
 // a.bounded
 hipError_t launch_attention_cfg(const AttnArgs& a, int qt, int nw, int st, hipStream_t s, int form = ATTN_RUNNING);
 // Largest score magnitude, log2 units, that the bf16 QKV epilogue can produce
-// for head size 64 with QK-norm gains q_g, k_g (host arrays of 64)
-float attention_score_bound(const float* q_g, const float* k_g);
+// for head size 64 with QK-norm gains q_g, k_g (host arrays of 64); turned: of q and
+// k that rotary positions have turned and stored again
+float attention_score_bound(const float* q_g, const float* k_g, bool turned);
 
 // ---------------------------------------------------------------- small kernels
 // y[n] = out_act(sum_k in_act(x[k]) W[k][n] + b[n]), W row-major [K][N]

@@ -37,12 +37,23 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   return v;
 }
 
-// x / s rounded to float32 from r, the rounded reciprocal of s: the quotient
+// x / s rounded to float32 from the rounded reciprocal of s: the quotient
 // estimate corrected by its exact remainder (three instructions; the compiler's
-// division takes ten).  Where s is infinite or NaN the result is NaN.
-__device__ __forceinline__ float divide_by(float x, float s, float r) {
-  const float q = x * r;
-  return fmaf(fmaf(-q, s, x), r, q);
+// division takes ten).  The remainder is exact above 2^-149 only, so with a small
+// s both sides are first raised by 2^64.  Where s is infinite or NaN the result is
+// NaN.
+struct Divisor {
+  float s, r, raise;
+};
+__device__ __forceinline__ Divisor divisor(float s) {
+  const float raise = s < 5.421010862e-20f ? 1.8446744073709552e19f : 1.0f;  // 2^-64, 2^64
+  s *= raise;
+  return {s, 1.0f / s, raise};
+}
+__device__ __forceinline__ float divide_by(float x, const Divisor& d) {
+  x *= d.raise;
+  const float q = x * d.r;
+  return fmaf(fmaf(-q, d.s, x), d.r, q);
 }
 
 // scale of a block whose largest magnitude has these bits

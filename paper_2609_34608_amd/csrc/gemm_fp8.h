@@ -358,7 +358,8 @@ __device__ __forceinline__ void store_blocks(const Fp8Operands& p, const Fp8Out&
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int m = mb + i * 16 + lr;
-    const float s = block_scale(max(top[wid][i * 16 + lr], top[wid ^ 1][i * 16 + lr])), rs = 1.0f / s;
+    const float s = block_scale(max(top[wid][i * 16 + lr], top[wid ^ 1][i * 16 + lr]));
+    const Divisor by = divisor(s);
     if (m >= p.M) continue;
     if (lg == 0 && wid % 2 == 0 && nb < p.N) o.scale[m * o.ldscale + nb / kScaleBlock] = s;
     uint8_t* row = out + m * o.ld + nb;
@@ -369,8 +370,7 @@ __device__ __forceinline__ void store_blocks(const Fp8Operands& p, const Fp8Out&
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         const f32x4 v = acc[j + w][i];
-        x.v[w] = pack_e4m3(divide_by(v[0], s, rs), divide_by(v[1], s, rs), divide_by(v[2], s, rs),
-                           divide_by(v[3], s, rs));
+        x.v[w] = pack_e4m3(divide_by(v[0], by), divide_by(v[1], by), divide_by(v[2], by), divide_by(v[3], by));
       }
       if (nb + c + W <= p.N) *reinterpret_cast<Row*>(row + c) = x;
     }

@@ -319,12 +319,12 @@ __device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&x)[N], floa
   struct __attribute__((packed, aligned(1))) Bytes {
     uint32_t v[N / 4];
   };
-  const float r = 1.0f / s;
+  const Divisor by = divisor(s);
   Bytes w;
 #pragma unroll
   for (int i = 0; i < N / 4; ++i)
-    w.v[i] = pack_e4m3(divide_by(x[4 * i], s, r), divide_by(x[4 * i + 1], s, r), divide_by(x[4 * i + 2], s, r),
-                       divide_by(x[4 * i + 3], s, r));
+    w.v[i] = pack_e4m3(divide_by(x[4 * i], by), divide_by(x[4 * i + 1], by), divide_by(x[4 * i + 2], by),
+                       divide_by(x[4 * i + 3], by));
   if (n >= N) {
     put(q, w, stream);
   } else {

@@ -92,3 +92,41 @@ def test_gradients_are_refused(dev, R):
             call()
         with torch.no_grad():
             call()
+
+
+# ------------------------------------------------------------- ends of the float32 range
+def _blocks32(x, rows):
+    """Bytes and scales of x (float32, on the host) by the definition, a division in
+    float32 and one rounding."""
+    M, K = x.shape
+    q, s = torch.empty(M, K, dtype=torch.uint8), torch.empty(-(-M // rows), -(-K // 128))
+    for i in range(s.shape[0]):
+        for j in range(s.shape[1]):
+            at = (slice(i * rows, (i + 1) * rows), slice(j * 128, (j + 1) * 128))
+            top = x[at].abs().max()
+            s[i, j] = torch.where(top == 0, torch.ones(()), (top / torch.tensor(448.0)).clamp_min(2.0 ** -126))
+            q[at] = (x[at] / s[i, j]).to(FP8).view(torch.uint8)
+    return q, s
+
+
+@pytest.mark.parametrize("rows", [1, 128])
+def test_blocks_of_the_smallest_scales(dev, R, rows):
+    """Blocks down to the smallest scale, their values on the borders between two e4m3
+    values or beside one: the bytes of the float32 quotient."""
+    rng = np.random.default_rng(7)
+    M, K = 256, 384
+    scale = np.float32(2.0) ** rng.integers(-126, -112, (M // rows, 3)) * rng.uniform(1, 2, (M // rows, 3)).astype(np.float32)
+    scale = np.repeat(np.repeat(scale.astype(np.float32), rows, 0), 128, 1)
+    odd = 2.0 * rng.integers(8, 16, (M, K)) + 1.0
+    v = np.where(rng.random((M, K)) < 0.3, (2 * rng.integers(0, 8, (M, K)) + 1) * 2.0 ** -10,
+                 odd / 16 * 2.0 ** rng.integers(-6, 8, (M, K)))
+    v[:, ::128] = 448.0
+    x = torch.from_numpy((v * scale.astype(np.float64)).astype(np.float32))
+    want = _blocks32(x, rows)
+    q, s = R.quantize_fp8(x.to(dev), block_rows=rows)
+    assert torch.equal(s.cpu(), want[1])
+    assert torch.equal(q.contiguous().view(torch.uint8).cpu(), want[0])
+    if rows == 1:  # the same values as a norm's result
+        _, q, s = R.norm_residual(x.to(dev)[None], pre="none", u_dtype=FP8)
+        assert torch.equal(s[0].cpu(), want[1])
+        assert torch.equal(q[0].contiguous().view(torch.uint8).cpu(), want[0])

@@ -525,7 +525,9 @@ int wam_quantize_fp8(const wam_quantize_args *args, void *hip_stream);
  *                   sum_{k in block j} a[m][k] w[n][k] + bias[n])
  * a [M][K] with scales per row (blocks of 1 x 128), w [N][K] with scales per
  * block of 128 x 128, as wam_quantize_fp8 makes them.  Block products and their
- * scaled sum are float32; with a bf16 or e4m3 result the products of 8
+ * scaled sum are float32.  The two scales of a block are multiplied first, in float32:
+ * their product must be zero or a normal number (below 2^-126 the result keeps a
+ * subnormal's digits, past the range it is an infinity or NaN).  With a bf16 or e4m3 result the products of 8
  * consecutive k are cut below 2^-13 of the power of two of the largest of them
  * (the 8-bit matrix instruction), with a float32 result they are not.  a and w
  * must start on 16 bytes and their row strides be multiples of 16; the bytes of a

@@ -130,3 +130,30 @@ def test_blocks_of_the_smallest_scales(dev, R, rows):
         _, q, s = R.norm_residual(x.to(dev)[None], pre="none", u_dtype=FP8)
         assert torch.equal(s[0].cpu(), want[1])
         assert torch.equal(q[0].contiguous().view(torch.uint8).cpu(), want[0])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("M,N", [(1, 64), (40, 200), (700, 1000)])
+@pytest.mark.parametrize("ea,ew", [(-62, -62), (-114, -10), (63, 62), (14, 111)])
+def test_products_of_far_scales(dev, R, ea, ew, M, N, dtype):
+    """Scales whose product is at either end of the normal float32 range: no digit is
+    lost, and a zero block stays zero."""
+    K = 384
+    kb = 3
+    a, w = _rand(dev, 1, M, K), _rand(dev, 2, N, K)
+    if ea < 0:  # values that bring the result back into the range: sums of large ones, or small ones
+        a, w = ((100.0 * t).abs().clamp_max(448.0) for t in (a, w))
+    else:
+        a, w = a * 2.0 ** -7, w * 2.0 ** -7
+    a, w = a.to(FP8), w.to(FP8)
+    sa = 2.0 ** ea * (1 + torch.rand(M, kb, generator=torch.Generator().manual_seed(3))).to(dev)
+    sw = 2.0 ** ew * (1 + torch.rand(-(-N // 128), kb, generator=torch.Generator().manual_seed(4))).to(dev)
+    near = torch.arange(M, device=dev) % 3 == 1  # rows of ordinary products between the others
+    sa[near] = sa[near] * 2.0 ** -ea * 2.0 ** -ew
+    a.view(torch.uint8)[M // 2, 128:256] = 0
+    c, err = F.matmul(a, sa, w, sw, None, False, dtype)
+    out = F.f64(R.matmul_fp8(a, sa, w, sw, out_dtype=dtype))
+    assert c.abs().max() < 2.0 ** 127 and out.isfinite().all()
+    # below the normal range a rounding is off by 2^-150, three a block
+    tol = err * (1 + 2.0 ** -8) + F.HALF[dtype] * (c.abs() + err) + (3 * kb + 1) * 2.0 ** -150
+    assert ((out - c).abs() <= tol).all(), float(((out - c).abs() / tol).max())

@@ -157,3 +157,39 @@ def test_products_of_far_scales(dev, R, ea, ew, M, N, dtype):
     # below the normal range a rounding is off by 2^-150, three a block
     tol = err * (1 + 2.0 ** -8) + F.HALF[dtype] * (c.abs() + err) + (3 * kb + 1) * 2.0 ** -150
     assert ((out - c).abs() <= tol).all(), float(((out - c).abs() / tol).max())
+
+
+# ------------------------------------------------------------- rows far apart
+@pytest.mark.parametrize("K", [256, 333])
+@pytest.mark.parametrize("far", ["a", "w"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_matmul_rows_far_apart(dev, R, dtype, far, K):
+    """Rows past the 32-bit offsets of a tile (2^23 bytes apart): the same bits as rows
+    side by side, where the near ones take the same tile, and the bound either way."""
+    M, N = 70, 90
+    a, sa = R.quantize_fp8(_rand(dev, 1, M, K))
+    w, sw = R.quantize_fp8(_rand(dev, 2, N, K), block_rows=128)
+    bias = _rand(dev, 3, N)
+    step = (1 << 23) + 16
+    x = a if far == "a" else w
+    buf = torch.empty((x.shape[0] - 1) * step + 352, dtype=torch.uint8, device=dev)
+    view = buf.as_strided((x.shape[0], 352), (step, 1))
+    view.fill_(127)  # NaN behind the rows
+    view[:, :K] = x.view(torch.uint8)
+    there = view.view(FP8)[:, :K]
+    ops = (there, sa, w, sw) if far == "a" else (a, sa, there, sw)
+    for gelu in (False, True):
+        out = R.matmul_fp8(*ops, bias=bias, gelu=gelu, out_dtype=dtype)
+        F.check(out, *F.matmul(a, sa, w, sw, bias, gelu, dtype), dtype=dtype)
+        assert torch.equal(out, R.matmul_fp8(a, sa, w, sw, bias=bias, gelu=gelu, out_dtype=dtype))
+
+
+def test_matmul_last_row_ends_inside_a_chunk(dev, R):
+    """One contiguous row of K off 16: what lies behind it does not enter."""
+    K, N = 333, 40
+    w, sw = R.quantize_fp8(_rand(dev, 2, N, K), block_rows=128)
+    a, sa = R.quantize_fp8(_rand(dev, 1, 1, K))
+    want = R.matmul_fp8(a, sa, w, sw, out_dtype=F32)
+    buf = torch.full((400,), 127, dtype=torch.uint8, device=dev)
+    buf[:K] = a.view(torch.uint8)[0]
+    assert torch.equal(R.matmul_fp8(buf.view(FP8)[:K].view(1, K), sa, w, sw, out_dtype=F32), want)

@@ -421,7 +421,8 @@ __device__ __forceinline__ void store_product(const Fp8Operands& p, const Fp8Out
   if constexpr (!EXACT && TN == 4) {
     // A wave has 128 bytes of a row: they go out through LDS, so that eight lanes side
     // by side store them, and past kStreamBytes as streaming stores where rows
-    // start on lines (10176 x 6144 x 1536 106 -> 100 us, with the GELU 115 -> 109).
+    // start on lines (10176 x 6144 x 1536 106 -> 100 us, with the GELU 115 -> 109; rows of
+    // 6152, whose lines two waves share, 106 -> 119).
     typedef uint32_t words __attribute__((ext_vector_type(4)));
     __syncthreads();  // the stages have been read
     if (!shift && nb + TN * 16 <= p.N) {

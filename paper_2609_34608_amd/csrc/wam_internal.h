@@ -125,8 +125,12 @@ __device__ __forceinline__ float gelu_tanh_f(float x) {
 // A result larger than the chip's L2s (8 x 4 MB) cannot wait there for its reader:
 // streaming stores leave the caches to what is read (10176 rows of 24 + 24 heads 27.7 ->
 // 22.0 us, norms of 10176 rows of 1536 40.8 -> 36.9, 8-bit blocks of 10176 x 6144 34.2 ->
-// 32.6).  They have to be whole lines.  A smaller result is read from there by the
-// next kernel: streaming 28 MB of q and k made them and their reader together 29.7
+// 32.6).  A wave has to store its bytes side by side.  Where rows begin and end inside a
+// line, in place or not, that still holds (norms of 10176 rows of 1537 41.5 -> 39.7, of
+// 2047 56.2 -> 53.6, of 20000 of 1000 48.4 -> 45.7 and in place 50.5 -> 43.7; blocks of
+// 10176 x 6101 37.6 -> 35.9); lines of which two waves hold a part each do not stand it
+// (the product's rows of 128 bytes a wave).  A smaller result is read from the L2s by
+// the next kernel: streaming 28 MB of q and k made them and their reader together 29.7
 // us instead of 26.5.
 constexpr int64_t kStreamBytes = (int64_t)32 << 20;
 template <typename P>

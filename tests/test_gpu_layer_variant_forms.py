@@ -113,3 +113,53 @@ def test_float32_post_norm_tiles(dev, B, T, D, F):
     m.set_post_norm(gains)
     _check(dev, spec, "fp32", m, W, f32_sigmas(spec.K), post=post)
     m.close()
+
+
+def _near(got, h, gate, y, bias):
+    """got = h + gate (y + bias), y known to half a bf16 step: three float32 roundings."""
+    y, h, gate, bias = (t.double().cpu() for t in (y, h, gate, bias))
+    want = h + gate * (y + bias)
+    tol = gate.abs() * (2.0 ** -8 * y.abs() + 2.0 ** -24 * (y + bias).abs()) + 2.0 ** -23 * (want.abs() + h.abs())
+    off = (got.double().cpu() - want).abs()
+    assert (off <= tol).all(), float((off / tol).max())
+
+
+@pytest.mark.parametrize("B,T,D,F", [(2, 89, 320, 640), (16, 1, 192, 384), (16, 70, 704, 1408)])
+def test_fp8_layer_is_its_operators(dev, B, T, D, F):
+    """A layer of the 8-bit mode from the operators without a handle, on the weights
+    that they quantise: the MLP behind a closed attention gate, and (one row a sample, so
+    that attention returns v) the attention block in front of a closed MLP gate.  What is
+    left is the product's rounding to bf16, which the layer does without."""
+    from paper_2609_34608_amd import runtime as R
+    spec = _shape("fp8", B, T, D, F)
+    W = make_weights(spec, bias_std=0.02, gain_std=0.1)
+    W["l0.mod_w"][:] = 0  # the modulation is its bias
+    rng = np.random.default_rng(3)
+    shift1, scale1, gate1, shift2, scale2, gate2 = mod = (0.3 * rng.standard_normal((6, D))).astype(np.float32)
+    x, cond = to_dev(make_initial_noise(spec), dev), to_dev(make_observations(spec, 0)[0], dev)
+    dv = lambda a: to_dev(np.ascontiguousarray(a), dev)  # noqa: E731
+    weight = {n: R.quantize_fp8(dv(np.asarray(W[f"l0.{n}_w"]).T), block_rows=128) for n in ("qkv", "proj", "fc1", "fc2")}
+
+    def layer(closed):
+        own = mod.copy()
+        own[closed] = 0
+        W["l0.mod_b"][:] = own.reshape(-1)
+        m = _make(dev, spec, "fp8", W)
+        h0, h1 = (m.hidden(3, x, cond, n).view(1, B * T, D).clone() for n in (0, 1))
+        m.close()
+        return h0, h1
+
+    def project(u, s, name, **kw):
+        return R.matmul_fp8(u.reshape(B * T, -1), s.reshape(B * T, -1), *weight[name], **kw)
+
+    h0, h1 = layer(2)
+    _, u, s = R.norm_residual(h0, scale=dv(scale2), shift=dv(shift2), eps=spec.ln_eps, u_dtype=R.FP8)
+    q, s = project(u, s, "fc1", bias=dv(W["l0.fc1_b"]), gelu=True, out_dtype=R.FP8)
+    _near(h1[0], h0[0], dv(gate2), project(q, s, "fc2"), dv(W["l0.fc2_b"]))
+    if T > 1:
+        return
+    h0, h1 = layer(5)
+    _, u, s = R.norm_residual(h0, scale=dv(scale1), shift=dv(shift1), eps=spec.ln_eps, u_dtype=R.FP8)
+    v = project(u, s, "qkv", bias=dv(W["l0.qkv_b"]))[:, 2 * D:]
+    q, s = R.quantize_fp8(v)
+    _near(h1[0], h0[0], dv(gate1), project(q, s, "proj"), dv(W["l0.proj_b"]))

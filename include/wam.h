@@ -66,7 +66,9 @@ extern "C" {
 #define WAM_FP8 2  /* as WAM_BF16, but the four projections of a layer multiply
                       e4m3 blocks: weights 128 x 128, packed by wam_init,
                       activations 1 x 128, each with a float32 scale (as
-                      wam_quantize_fp8 makes them); modulation, attention and
+                      wam_quantize_fp8 makes them), by the 8-bit matrix
+                      instruction (wam_matmul_fp8 with a bf16 result) also where
+                      they add to the float32 residual; modulation, attention and
                       everything else stay as they are.  As an element type: e4m3 */
 
 /* ---- Residual Rescaling modes ------------------------------------------ */

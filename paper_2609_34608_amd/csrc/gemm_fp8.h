@@ -14,10 +14,19 @@
 // The 8-bit matrix instruction does not add all products in float32: in each
 // group of 8 consecutive values of K it cuts every product, toward zero, below
 // 2^-13 of the power of two of the group's largest one (measured; 16x16x32 the
-// same), and only the groups' sums add in float32.  That is under the rounding
-// of a bf16 result.  For float32 results (EXACT) the operands are converted to
-// bf16, which holds every e4m3 value, and go through v_mfma_f32_16x16x32_bf16,
-// whose products add in float32, at half the matrix rate.
+// same), and only the groups' sums add in float32.  Against those products that is
+// finer than a bf16 result's rounding (2^-8); against a sum in which they cancel it
+// need not be.  bf16 and e4m3 results take it, and so do the gated residuals of the
+// 8-bit layers, whose operands are rounded to 2^-4 anyway.  For the operator's float32
+// results (EXACT) the operands are converted to bf16, which holds every e4m3 value,
+// and go through v_mfma_f32_16x16x32_bf16, whose products add in float32, at half the
+// matrix rate.
+//
+// The two scales of a block are multiplied first and their product has to be zero or a
+// normal number.  A check of every stage's scales, with a second pass over the tile
+// that splits far ones into a power of two and a rest, was right at any scale and
+// cost every product its registers and issue slots (10176 x 6144 x 1536 102 -> 128 us, 9224
+// x 1024 x 4096 44.7 -> 47.4, 864 x 2304 x 768 7.5 -> 7.9).
 //
 // K advances one block (128 bytes of a row) per LDS stage; stages, swizzle and
 // direct-to-LDS loads are those of gemm_tile.h, in bytes.  A lane's 32-byte

@@ -353,7 +353,7 @@ constexpr int kNormCols = 4;  // columns of a lane and chunk
 // float32: 4 x 2306 rows of 1024 31.7 against 29.7 us).  Sums are over lanes, and over
 // the waves in LDS.  32 lanes of a chunk are one block of 128 columns, which is
 // what 8-bit results need.  HBM bound: 10176 rows of 1536 into 8-bit blocks move
-// 172 MB in 37 us (4.7 TB/s), 4 x 2306 rows of 1024 with modulation per row 227 MB in
+// 172 MB in 37 us (4.6 TB/s), 4 x 2306 rows of 1024 with modulation per row 227 MB in
 // 42.5 (5.3); requesting gate and modulation ahead of the sums was 3-5% slower
 // (registers).
 template <int CH, int W, typename TH, typename TY>

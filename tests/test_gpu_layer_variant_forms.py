@@ -163,3 +163,19 @@ def test_fp8_layer_is_its_operators(dev, B, T, D, F):
     v = project(u, s, "qkv", bias=dv(W["l0.qkv_b"]))[:, 2 * D:]
     q, s = R.quantize_fp8(v)
     _near(h1[0], h0[0], dv(gate1), project(q, s, "proj"), dv(W["l0.proj_b"]))
+
+
+@pytest.mark.parametrize("layout", ["halves", "pairs"])
+@pytest.mark.parametrize("sections", [(8, 8, 0), (0, 0, 8), (10, 10, 10), (1, 0, 2)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32", "fp8"])
+def test_layers_that_turn_a_part_of_the_head(dev, dtype, sections, layout):
+    """Fewer pairs than half the head, whole units of eight and others, where q and k
+    lie."""
+    from paper_2609_34608_amd import runtime as R
+    spec = _spec(dtype, L=1)
+    W = make_weights(spec, bias_std=0.02, gain_std=0.1)
+    m = _make(dev, spec, dtype, W)
+    pos, freq = _positions(spec), R.rope_frequencies(sections, 100.0)
+    m.set_rotary(to_dev(pos, dev), sections, freq, layout)
+    _check(dev, spec, dtype, m, W, f32_sigmas(spec.K), rot=(pos, freq, sections, layout))
+    m.close()

@@ -504,9 +504,9 @@ int wam_norm_residual(const wam_norm_args *args, void *hip_stream);
 
 /* 8-bit blocks: x [M][K] is cut into blocks of block_rows (1 or 128) rows and
  * 128 columns (the last ones smaller); a block's scale is max|x| / 448 in
- * float32, at least 2^-126 (1 where the block is zero), and q = x / scale rounded
- * to e4m3, to nearest, ties to even.  A block with a NaN or an infinity has that
- * as its scale, and stands for NaN.  scale: [ceil(M / block_rows)][ceil(K / 128)].
+ * float32, at least 2^-126 (1 where the block is zero), and q the float32 quotient
+ * x / scale rounded to e4m3, to nearest, ties to even.  A block with a NaN or an
+ * infinity has that as its scale, and stands for NaN.  scale: [ceil(M / block_rows)][ceil(K / 128)].
  * Bytes of a row of q past K are left as they are.  At most 2^29 - 32 blocks of
  * one row or 2^24 - 1 of 128 rows. */
 typedef struct {
@@ -528,14 +528,14 @@ int wam_quantize_fp8(const wam_quantize_args *args, void *hip_stream);
  * a [M][K] with scales per row (blocks of 1 x 128), w [N][K] with scales per
  * block of 128 x 128, as wam_quantize_fp8 makes them.  Block products and their
  * scaled sum are float32.  The two scales of a block are multiplied first, in float32:
- * their product must be zero or a normal number (below 2^-126 the result keeps a
- * subnormal's digits, past the range it is an infinity or NaN).  With a bf16 or e4m3 result the products of 8
- * consecutive k are cut below 2^-13 of the power of two of the largest of them
- * (the 8-bit matrix instruction), with a float32 result they are not.  a and w
- * must start on 16 bytes and their row strides be multiples of 16; the bytes of a
- * row past K, up to the next multiple of 16, are read but may hold anything (behind
- * the last row too: they lie in the same 16 bytes as its last value).  WAM_E_SHAPE
- * where the tiles pass a grid (from 2^24 of 32 x 32 on).  act:
+ * where that is below 2^-126 the block's share of the result has a subnormal's digits,
+ * and where it passes the range the result is an infinity or NaN.  With a bf16 or e4m3
+ * result the products of 8 consecutive k are cut below 2^-13 of the power of two of
+ * the largest of them (the 8-bit matrix instruction), with a float32 result they are
+ * not.  a and w must start on 16 bytes and their row strides be multiples of 16; the
+ * bytes of a row past K, up to the next multiple of 16, are read but may hold
+ * anything (behind the last row too: they lie in the same 16 bytes as its last
+ * value).  WAM_E_SHAPE where the tiles pass a grid (from 2^24 of 32 x 32 on).  act:
  * WAM_ACT_NONE or WAM_ACT_GELU (tanh form).  out: WAM_FP32, WAM_BF16, or WAM_FP8:
  * blocks of 1 x 128 of the result before any rounding, with their scales in out_scale
  * [M][ceil(N / 128)], as wam_quantize_fp8 makes them, for the next product (rows

@@ -41,7 +41,9 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
 // estimate corrected by its exact remainder (three instructions; the compiler's
 // division takes ten).  The remainder is exact above 2^-149 only, so with a small
 // s both sides are first raised by 2^64.  Where s is infinite or NaN the result is
-// NaN.
+// NaN.  Its rounding comes before that to e4m3: 4 of 10^7 values (normal ones, float32
+// blocks) lie so near to a border between two e4m3 values that one rounding would
+// have gone to the other side, as in any form that divides in float32.
 struct Divisor {
   float s, r, raise;
 };

@@ -22,8 +22,8 @@
 // and go through v_mfma_f32_16x16x32_bf16, whose products add in float32, at half the
 // matrix rate.
 //
-// The two scales of a block are multiplied first and their product has to be zero or a
-// normal number.  A check of every stage's scales, with a second pass over the tile
+// The two scales of a block are multiplied first, so a block whose product of scales is
+// subnormal or infinite is not what float64 makes of it.  A check of every stage's scales, with a second pass over the tile
 // that splits far ones into a power of two and a rest, was right at any scale and
 // cost every product its registers and issue slots (10176 x 6144 x 1536 102 -> 128 us, 9224
 // x 1024 x 4096 44.7 -> 47.4, 864 x 2304 x 768 7.5 -> 7.9).

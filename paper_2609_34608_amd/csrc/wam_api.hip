@@ -495,9 +495,9 @@ int rotate_heads(wam_t h, const int* skip) {
 
 // copy: when non-null, the layer's MLP-down epilogue (the last writer of h)
 // also stores the layer's output h there (never together with skip: behind a
-// post-norm the copy is a launch that does not look at the flag).  out: when non-null, that epilogue
-// stores the layer's output there instead of in h, which then holds the
-// residual stream before the MLP.
+// post-norm the copy is a launch that does not look at the flag).  out: when
+// non-null, that epilogue stores the layer's output there instead of in h, which
+// then holds the residual stream before the MLP.
 //
 // With post-norms the two projections in front of the residual only add their
 // bias, and the norm, gate and residual are one pass over the rows together with

@@ -642,9 +642,9 @@ def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_d
                stream: torch.cuda.Stream | None = None):
     """out [M, N] = act((a * a_scale) (w * w_scale)^T + bias) of 8-bit blocks
     (wam_matmul_fp8): a [M, K] with scales per row and 128 columns, w [N, K] with
-    scales per 128 x 128, both as quantize_fp8 gives them (the product of two scales
-    zero or a normal float32 number); rows are read up to the next multiple of 16
-    bytes, what lies there does not enter.  bias float32 [N]; gelu: the tanh form.
+    scales per 128 x 128, both as quantize_fp8 gives them (a block's two scales are
+    multiplied first, in float32); rows are read up to the next multiple of 16 bytes,
+    what lies there does not enter.  bias float32 [N]; gelu: the tanh form.
     out float32, bfloat16 (default: a new bfloat16 one) or
     float8_e4m3fn: then returns (out, out_scale), blocks for the next product."""
     index = _first(a, "matmul_fp8: a", _F8, 2)

@@ -561,6 +561,152 @@ typedef struct {
 } wam_matmul_args;
 int wam_matmul_fp8(const wam_matmul_args *args, void *hip_stream);
 
+/* 4-bit blocks.  A block is 32 neighbouring values of a row: their codes, two to a
+ * byte (the first value in the low half; 1 sign, 2 exponent and 1 mantissa bit: 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 and their negatives), and one byte s that stands for 2^(s - 127),
+ * or for NaN where it is 255.
+ *
+ * wam_quantize_fp4: x [M][K] into q [M][ceil(K / 2)] and scale [M][ceil(K / 32)]
+ * (the last block of a row smaller).  With the largest magnitude of a block in
+ * [2^e, 2^(e + 1)) its byte is e - 2 + 127, at least 0, and a code the nearest value to
+ * x / 2^(e - 2), ties to the even code, magnitudes above 6 to 6.  A block of zeros has
+ * the byte 0; one with a NaN or an infinity has 255, codes zero, and stands for NaN.
+ * With an odd K the last byte's high half is zero.  No other byte is written.
+ *
+ * wam_dequantize_fp4: the values of q, scale as x [M][K], float32 or bf16 (which holds
+ * each of them but those past its range; K columns of q, odd ones too).
+ *
+ * Both: at most 2^29 - 32 blocks, strides of rows in elements and bytes. */
+#define WAM_FP4_BLOCK 32
+typedef struct {
+  int32_t M, K;
+  int32_t dtype;       /* of x: WAM_FP32 | WAM_BF16 */
+  const void *x;
+  int64_t x_stride;
+  uint8_t *q;
+  int64_t q_stride;
+  uint8_t *scale;
+  int64_t scale_stride;
+} wam_quantize_fp4_args;
+int wam_quantize_fp4(const wam_quantize_fp4_args *args, void *hip_stream);
+typedef struct {
+  int32_t M, K;
+  int32_t dtype;       /* of x: WAM_FP32 | WAM_BF16 */
+  const uint8_t *q;
+  int64_t q_stride;
+  const uint8_t *scale;
+  int64_t scale_stride;
+  void *x;
+  int64_t x_stride;
+} wam_dequantize_fp4_args;
+int wam_dequantize_fp4(const wam_dequantize_fp4_args *args, void *hip_stream);
+
+/* Product of matrices in 4-bit blocks:
+ *   out[m][n] = act(sum_j 2^(a_scale[m][j] + w_scale[n][j] - 254)
+ *                   sum_{k in block j} a[m][k] w[n][k] + bias[n])
+ * a [M][K] and w [N][K] with K even, as wam_quantize_fp4 makes them (an odd K: one more
+ * column, which is zero).  Sums are float32: each step of the scaled matrix instruction
+ * (128 of K) is off by at most 2^-22 of the sum of its products' magnitudes and of what
+ * it adds to; where those pass the float32 range the result may be infinite or NaN.
+ * Data must start on 16 bytes with row strides a multiple of 16, scales on
+ * 4 bytes with row strides a multiple of 4; the bytes of a row past its end, up to the
+ * next multiple of 16 (4), are read but may hold anything (behind the last row too).
+ * act: WAM_ACT_NONE or WAM_ACT_GELU (tanh form).  out: WAM_FP32, WAM_BF16, or WAM_FP4:
+ * blocks of the result before any rounding in out [M][ceil(N / 2)] and out_scale
+ * [M][ceil(N / 32)], for the next product.  WAM_E_SHAPE where the tiles pass a grid. */
+#define WAM_FP4 3
+typedef struct {
+  int32_t M, N, K;
+  int32_t out_dtype, act;
+  const uint8_t *a;
+  int64_t a_stride;
+  const uint8_t *a_scale;
+  int64_t a_scale_stride;
+  const uint8_t *w;
+  int64_t w_stride;
+  const uint8_t *w_scale;
+  int64_t w_scale_stride;
+  const float *bias;   /* device [N] or NULL */
+  void *out;
+  int64_t out_stride;  /* in elements; bytes of WAM_FP4 */
+  uint8_t *out_scale;  /* out of WAM_FP4 */
+  int64_t out_scale_stride;
+} wam_matmul_fp4_args;
+int wam_matmul_fp4(const wam_matmul_fp4_args *args, void *hip_stream);
+
+/* A cache of keys and values in 4-bit blocks: a pool of pages of `page` tokens (a power
+ * of two, 16 to 4096) with H heads of dh values (32, 64, 96 or 128), i.e. dh / 2 bytes of
+ * codes and dh / 32 scales a head, all contiguous; strides in bytes of page, token and
+ * head, those of codes (and their base) multiples of 4.  A sequence has a row of
+ * table: its token t lies at place t % page of page table[b][t / page].  An entry
+ * outside 0 .. pages - 1 stands for no page, and tokens past the table for none. */
+typedef struct {
+  int32_t pages, page, H, dh;
+  uint8_t *k, *k_scale, *v, *v_scale;
+  int64_t k_stride[3], k_scale_stride[3], v_stride[3], v_scale_stride[3]; /* of page, token, head */
+} wam_cache;
+typedef struct {
+  const int32_t *entry; /* device [B][width] */
+  int64_t stride;       /* of a sequence, in entries */
+  int32_t width;
+} wam_page_table;
+
+/* Appends T rows of B sequences: row t of sequence b becomes token start[b] + t.  v goes
+ * into blocks as it is; k first gets the RMS norm with k_gain (NULL: none) and the
+ * rotary positions of wam_rope (sections, layout, pos, freq; no pairs: none), both in
+ * float64, and is rounded to float32 once.  rows[b] (NULL: T) is how many rows of b
+ * count; those past it, tokens below 0 and tokens without a page are dropped.  Nothing
+ * but the tokens' own bytes is written.  The tokens of a call must lie at
+ * different places of the pool.  B * T <= WAM_MAX_ROWS. */
+typedef struct {
+  int32_t B, T, dtype;             /* of k and v: WAM_FP32 | WAM_BF16 */
+  int32_t layout, sections[3];
+  wam_cache cache;
+  wam_page_table table;
+  const void *k, *v;               /* device [B][T][H][dh] */
+  int64_t k_stride[3], v_stride[3]; /* of sample, row, head */
+  const int32_t *start, *rows;     /* device [B]; rows may be NULL */
+  const float *pos;                /* device [T][3] per sample, contiguous; NULL without pairs */
+  int64_t pos_stride;              /* floats between samples; 0: the same for all */
+  const double *freq;              /* host [P]: radians per unit of position */
+  const float *k_gain;             /* device [dh] or NULL */
+  double eps;                      /* >= 0; used with a gain */
+} wam_cache_append_args;
+int wam_cache_append(const wam_cache_append_args *args, void *hip_stream);
+
+/* Attention of T rows of B sequences over the cache:
+ *   out[b][t][h] = sum_j softmax_j(scale q[b][t][h] . k_j) v_j
+ * over the tokens j < seen(b, t) of key head h / (Hq / cache.H), without those that
+ * have no page.  seen is lengths[b], or, causal, lengths[b] - rows[b] + t + 1 (the last
+ * rows[b] tokens are the rows' own), between 0 and the table's end.  A row that sees no
+ * token, or past rows[b] (NULL: T), is 0.  What lies in tokens that a row does not see,
+ * NaN included, does not enter; a value of v past the bf16 range counts as NaN.  lse
+ * (NULL: not stored) is the natural logarithm of the sum of the exponentials, -inf for
+ * such a row; two results over different tokens join with it.  Scores and sums are
+ * float32; with bf16 q a probability is rounded to bf16 once, with float32 q neither q nor
+ * the probabilities lose a bit that float32 holds.  Hq is a multiple of cache.H, scale > 0.
+ * Where a sequence's tokens are shared among blocks, their parts meet in workspace:
+ * wam_cache_attention_workspace bytes (0: none) on 16 bytes, any content, which the
+ * call owns until its work is done.  B * T <= WAM_MAX_ROWS, B * T * Hq <= 2^31 - 2^16. */
+typedef struct {
+  int32_t B, T, Hq, dtype;         /* of q and out: WAM_FP32 | WAM_BF16 */
+  int32_t causal;
+  wam_cache cache;
+  wam_page_table table;
+  const void *q;                   /* device [B][T][Hq][dh] */
+  int64_t q_stride[3];             /* of sample, row, head */
+  void *out;
+  int64_t out_stride[3];
+  float *lse;                      /* device [B][T][Hq] or NULL */
+  int64_t lse_stride[3];
+  const int32_t *lengths, *rows;   /* device [B]; rows may be NULL */
+  double scale;
+  void *workspace;
+  size_t workspace_bytes;
+} wam_cache_attention_args;
+size_t wam_cache_attention_workspace(const wam_cache_attention_args *args);
+int wam_cache_attention(const wam_cache_attention_args *args, void *hip_stream);
+
 /* ---- measurement ------------------------------------------------------------ */
 /* Time every launch of kernel class kc (WAM_KC_*), up to max_launches
  * launches: a HIP event pair per launch, stamped by the dispatches themselves

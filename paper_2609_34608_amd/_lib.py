@@ -27,6 +27,7 @@ WAM_ATTN_AUTO, WAM_ATTN_RUNNING_MAX, WAM_ATTN_BOUNDED, WAM_ATTN_PINGPONG, WAM_AT
 WAM_ROPE_HALVES, WAM_ROPE_PAIRS, WAM_MAX_HEAD, WAM_MAX_ROWS = 0, 1, 256, 16777215
 WAM_NORM_NONE, WAM_NORM_RMS, WAM_NORM_LAYER, WAM_MAX_NORM_D = 0, 1, 2, 8192
 WAM_ACT_NONE, WAM_ACT_GELU = 0, 1
+WAM_FP4, WAM_FP4_BLOCK = 3, 32
 
 KERNEL_CLASS_NAMES = ["gemm_qkv", "gemm_proj", "gemm_fc1", "gemm_fc2", "attention",
                       "rr_gate", "rr_inject", "rr_refresh"]
@@ -122,6 +123,45 @@ class WamMatmulArgs(C.Structure):
                 ("out_scale_stride", C.c_int64)]
 
 
+class WamQuantizeFp4Args(C.Structure):
+    _fields_ = [("M", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("x", C.c_void_p), ("x_stride", C.c_int64),
+                ("q", C.c_void_p), ("q_stride", C.c_int64), ("scale", C.c_void_p), ("scale_stride", C.c_int64)]
+
+
+class WamDequantizeFp4Args(C.Structure):
+    _fields_ = [("M", C.c_int32), ("K", C.c_int32), ("dtype", C.c_int32), ("q", C.c_void_p), ("q_stride", C.c_int64),
+                ("scale", C.c_void_p), ("scale_stride", C.c_int64), ("x", C.c_void_p), ("x_stride", C.c_int64)]
+
+
+WamMatmulFp4Args = type("WamMatmulFp4Args", (C.Structure,), {"_fields_": WamMatmulArgs._fields_})
+
+
+class WamCache(C.Structure):
+    _fields_ = [("pages", C.c_int32), ("page", C.c_int32), ("H", C.c_int32), ("dh", C.c_int32), ("k", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v", C.c_void_p), ("v_scale", C.c_void_p), ("k_stride", C.c_int64 * 3),
+                ("k_scale_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3), ("v_scale_stride", C.c_int64 * 3)]
+
+
+class WamPageTable(C.Structure):
+    _fields_ = [("entry", C.c_void_p), ("stride", C.c_int64), ("width", C.c_int32)]
+
+
+class WamCacheAppendArgs(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("dtype", C.c_int32), ("layout", C.c_int32),
+                ("sections", C.c_int32 * 3), ("cache", WamCache), ("table", WamPageTable), ("k", C.c_void_p),
+                ("v", C.c_void_p), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3), ("start", C.c_void_p),
+                ("rows", C.c_void_p), ("pos", C.c_void_p), ("pos_stride", C.c_int64), ("freq", C.c_void_p),
+                ("k_gain", C.c_void_p), ("eps", C.c_double)]
+
+
+class WamCacheAttentionArgs(C.Structure):
+    _fields_ = [("B", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("dtype", C.c_int32), ("causal", C.c_int32),
+                ("cache", WamCache), ("table", WamPageTable), ("q", C.c_void_p), ("q_stride", C.c_int64 * 3),
+                ("out", C.c_void_p), ("out_stride", C.c_int64 * 3), ("lse", C.c_void_p), ("lse_stride", C.c_int64 * 3),
+                ("lengths", C.c_void_p), ("rows", C.c_void_p), ("scale", C.c_double), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_size_t)]
+
+
 EXPORTS = {
     # name: (restype, argtypes)
     "wam_host_weight_count": (C.c_size_t, [C.POINTER(WamConfig)]),
@@ -165,6 +205,12 @@ EXPORTS = {
     "wam_norm_residual": (C.c_int, [C.c_void_p, C.c_void_p]),
     "wam_quantize_fp8": (C.c_int, [C.c_void_p, C.c_void_p]),
     "wam_matmul_fp8": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_quantize_fp4": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_dequantize_fp4": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_matmul_fp4": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_cache_append": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_cache_attention": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "wam_cache_attention_workspace": (C.c_size_t, [C.c_void_p]),
     "wam_probe_mfma_bf16": (C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.POINTER(C.c_double),
                                       C.POINTER(C.c_double)]),
     "wam_probe_copy": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_int, C.POINTER(C.c_double),

@@ -36,7 +36,7 @@ COMMON = [
     "-Wno-unused-result", f"-I{INCLUDE}", f"-I{CSRC}",
 ]
 
-SOURCES = ["k_small.hip", "k_gemm.hip", "k_attention.hip", "k_layer.hip", "k_gemm_fp8.hip", "k_probe.hip", "wam_api.hip"]
+SOURCES = ["k_small.hip", "k_gemm.hip", "k_attention.hip", "k_layer.hip", "k_gemm_fp8.hip", "k_fp4.hip", "k_gemm_fp4.hip", "k_cache_attention.hip", "k_probe.hip", "wam_api.hip"]
 
 
 def _compile(src: str) -> str:

@@ -400,10 +400,10 @@ __device__ __forceinline__ void store_blocks(const Fp8Operands& p, const Fp8Out&
   }
 }
 
-// Bias, activation and rounding of a wave's accumulators into a result of any row
-// stride.
-template <int TN, int TM, bool EXACT, bool GELU>
-__device__ __forceinline__ void store_product(const Fp8Operands& p, const Fp8Out& o, const f32x4 (&acc)[TN][TM],
+// Bias, activation and rounding of a wave's accumulators into an M x N result (p.M, p.N)
+// of any row stride.
+template <int TN, int TM, bool EXACT, bool GELU, typename SIZES>
+__device__ __forceinline__ void store_product(const SIZES& p, const Fp8Out& o, const f32x4 (&acc)[TN][TM],
                                               int mb, int nb, int lane, uint8_t* lds) {
   const int lr = lane % 16, lg = lane / 16;
   // G tiles side by side hold W consecutive columns of a lane.  Global memory takes

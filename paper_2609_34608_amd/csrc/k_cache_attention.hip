@@ -1,0 +1,561 @@
+// Attention over a paged cache of 4-bit blocks (gfx950).
+//
+// Per key head, the query rows (t, head of the group) of a sequence are tiled by 16 and
+// the tokens by 64.  As in k_attention.hip, S^T = K Q^T and O^T = V^T P^T on
+// v_mfma_f32_16x16x32_bf16, so a lane's scores all belong to one query and feed the
+// second product without leaving the lane.
+//
+// Codes go from memory straight into registers.  A code times its power of two has two
+// significant bits and is exact in bf16, so both products are those of bf16 operands:
+//  * K: lane (r, g) holds the dh / 4 values of token r from dh / 4 * g on, whole words of
+//    codes, which the conversions turn into the chunks of 8 that the MFMA takes.  Which
+//    dims a lane holds does not matter as long as q's chunks are the same.
+//  * V: the second product runs over tokens, which lie in different rows of codes.  A
+//    wave puts its converted tile (token rows) into LDS and reads it back with
+//    ds_read_b64_tr_b16, four tokens of a dim a lane, at the tokens whose scores the
+//    lane group holds.
+// The softmax has a running maximum m (in units of log2) that moves when a tile passes it
+// by more than 8, so most tiles have no rescale; its denominator is one more MFMA
+// against ones, which sums exactly the rounded probabilities that multiply V.
+//
+// A block's four waves share the tokens of its rows (few rows), taking tiles in turn, and
+// join through LDS; where blocks are few, a sequence's tokens are split over blocks
+// too, whose parts go to the workspace for a second launch to join in order.
+#include <math.h>
+
+#include <algorithm>
+
+#include "cache.h"
+#include "fp4.h"
+#include "layer_util.h"
+
+namespace wam {
+
+int check_cache(const wam_cache& c, const wam_page_table& t, bool written, bool empty, const char* what);
+
+namespace {
+
+constexpr int kKeys = 64;      // tokens of a tile
+constexpr int kWaves = 4;
+constexpr float kNone = -3e38f;  // running maximum of a row that has seen nothing
+constexpr float kSlack = 8.f;    // a probability reaches 2^8 before the maximum moves
+constexpr uint32_t kFar = 253;   // scales from here on may pass the bf16 range
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct AttendParams {
+  wam_cache_attention_args a;
+  int shift;       // of a page
+  int group;       // query heads of a key head
+  int row_blocks;  // blocks of rows of a (sequence, key head)
+  int splits;      // blocks that share the tokens of a row block
+  float log2_scale;
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// The logical block of a grid of n blocks: each XCD (workgroups go to them round-robin)
+// takes a contiguous range, so that the blocks of a head share an L2.
+__device__ __forceinline__ int xcd_block(int i, int n) {
+  const int per = n / 8, rem = n % 8, x = i % 8;
+  return x * per + min(x, rem) + i / 8;
+}
+
+// bf16 parts of a float32: the first alone, or three that add up to it
+template <int NS>
+__device__ __forceinline__ void split(float x, bf16 (&part)[NS]) {
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    part[s] = static_cast<bf16>(x);
+    x -= static_cast<float>(part[s]);
+  }
+}
+
+// Codes and scales of 16 tokens: lane (r, g) has the words g DB .. + DB - 1 of token r
+template <int DB>
+struct Codes {
+  uint32_t w[DB];
+  uint8_t s[DB];
+};
+
+template <int DB>
+__device__ __forceinline__ void load_codes(Codes<DB>& c, const uint8_t* q, const uint8_t* scale, int lg) {
+  struct __attribute__((packed, aligned(4))) Words {
+    uint32_t w[DB];
+  };
+  const Words v = *reinterpret_cast<const Words*>(q + lg * DB * 4);
+#pragma unroll
+  for (int i = 0; i < DB; ++i) c.w[i] = v.w[i];
+  if constexpr (DB == 3) {  // a lane's words lie in two blocks
+#pragma unroll
+    for (int i = 0; i < DB; ++i) c.s[i] = scale[(lg * DB + i) / 4];
+  } else {
+    c.s[0] = scale[lg * DB / 4];
+  }
+}
+template <int DB>
+__device__ __forceinline__ uint32_t scale_of(const Codes<DB>& c, int i) { return DB == 3 ? c.s[i] : c.s[0]; }
+
+// DB: blocks of a head; QT: tiles of 16 rows; NS: bf16 parts of q and of a probability
+template <int DB, int QT, int NS>
+__global__ __launch_bounds__(kWaves* kWave) void attend_kernel(AttendParams p) {
+  typedef typename std::conditional<NS == 1, bf16, float>::type T;
+  constexpr int DH = DB * 32, DT = DH / 16;
+  constexpr int VROW = DH * 2 + 32;  // bytes of a token in LDS: the reads of 16 rows meet no bank twice
+  __shared__ __attribute__((aligned(64))) uint8_t vt[kWaves][kKeys * VROW];
+  __shared__ float part_m[kWaves][QT * 16], part_l[kWaves][QT * 16];
+
+  const wam_cache_attention_args& a = p.a;
+  const wam_cache& ca = a.cache;
+  const int lane = threadIdx.x % kWave, wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int lr = lane % 16, lg = lane / 16;
+  int id = xcd_block(blockIdx.x, gridDim.x);
+  const int split_at = id % p.splits;
+  id /= p.splits;
+  const int rb = id % p.row_blocks;
+  id /= p.row_blocks;
+  const int hk = id % ca.H, b = id / ca.H;
+
+  const int R = p.group * a.T, r0 = rb * QT * 16;
+  const int rows = a.rows ? min(max(a.rows[b], 0), a.T) : a.T;
+  const int length = a.lengths[b], held = tokens_held(length, a.table.width, p.shift);
+  // what the rows of this block see at least and at most (row r is t = r / group, in order)
+  // rows past the last are never stored and hinder nothing
+  int most = 0, least = INT32_MAX;
+  int vis[QT];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const int r = r0 + i * 16 + lr;
+    vis[i] = r < R ? tokens_seen(held, length, a.causal, rows, r / p.group) : INT32_MAX;
+    int hi = r < R ? vis[i] : 0, lo = vis[i];
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) hi = max(hi, __shfl_xor(hi, o, 64)), lo = min(lo, __shfl_xor(lo, o, 64));
+    most = max(most, hi), least = min(least, lo);
+  }
+  most = __builtin_amdgcn_readfirstlane(most), least = __builtin_amdgcn_readfirstlane(least);
+  const int tiles = (most + kKeys - 1) / kKeys;
+  const int t_lo = (int)((int64_t)tiles * split_at / p.splits), t_hi = (int)((int64_t)tiles * (split_at + 1) / p.splits);
+
+  // q, in chunks of the dims that the K operand has
+  bf16x8 qf[QT][DB][NS];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const int r = min(r0 + i * 16 + lr, R - 1);
+    const T* q = static_cast<const T*>(a.q) + b * a.q_stride[0] + r / p.group * a.q_stride[1] +
+                 (hk * p.group + r % p.group) * a.q_stride[2];
+#pragma unroll
+    for (int s = 0; s < DB; ++s) {
+      float x[8];
+      load_n(x, q + (lg * DB + s) * 8, 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        bf16 part[NS];
+        split<NS>(x[e], part);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) qf[i][s][n][e] = part[n];
+      }
+    }
+  }
+
+  const int32_t* table = a.table.entry + b * a.table.stride;
+  const int64_t head_k = hk * ca.k_stride[2], head_ks = hk * ca.k_scale_stride[2];
+  const int64_t head_v = hk * ca.v_stride[2], head_vs = hk * ca.v_scale_stride[2];
+  Codes<DB> kc[4], vc[4];
+  bool there[4];  // the 16 tokens have a page
+  auto request = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int t = tile * kKeys + g * 16;
+      const int page = page_of(table, a.table.width, p.shift, ca.pages, t);
+      there[g] = page >= 0;
+      const int64_t pg = max(page, 0), place = (t & ((1 << p.shift) - 1)) + lr;
+      load_codes(kc[g], ca.k + pg * ca.k_stride[0] + place * ca.k_stride[1] + head_k,
+                 ca.k_scale + pg * ca.k_scale_stride[0] + place * ca.k_scale_stride[1] + head_ks, lg);
+      load_codes(vc[g], ca.v + pg * ca.v_stride[0] + place * ca.v_stride[1] + head_v,
+                 ca.v_scale + pg * ca.v_scale_stride[0] + place * ca.v_scale_stride[1] + head_vs, lg);
+    }
+  };
+
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  bf16x8 ones;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) ones[e] = (bf16)1.0f;
+  f32x4 o[QT][DT], l[QT];
+  float m[QT];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    m[i] = kNone, l[i] = zero;
+#pragma unroll
+    for (int j = 0; j < DT; ++j) o[i][j] = zero;
+  }
+  uint8_t* own = vt[wid];
+  // fn(j, c, V^T of dims 16 j .. + 15 and the tokens of score tiles 2 c, 2 c + 1); lane s of
+  // a group reads dims 4 (s % 4) .. + 3 of token s / 4 of its four
+  auto for_dims = [&](auto fn) __attribute__((always_inline)) {
+    const uint8_t* from = own + (4 * lg + lr / 4) * VROW + lr % 4 * 8;
+    static_for<DT>([&](auto J) __attribute__((always_inline)) {
+      static_for<2>([&](auto C) __attribute__((always_inline)) {
+        const uint8_t* at = from + 2 * decltype(C)::value * 16 * VROW + decltype(J)::value * 32;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * VROW));
+        bf16x8 vf;
+        __builtin_memcpy(&vf, &lo, 8);
+        __builtin_memcpy(reinterpret_cast<char*>(&vf) + 8, &hi, 8);
+        fn(J, C, vf);
+      });
+    });
+  };
+
+  const int first = t_lo + wid;
+  if (first < t_hi) request(first);
+  for (int tile = first; tile < t_hi; tile += kWaves) {
+    const int k0 = tile * kKeys;
+    const bool whole = k0 + kKeys <= least && there[0] && there[1] && there[2] && there[3];
+    bool has[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) has[g] = there[g];
+    if (!whole) {
+      // tokens that the sequence does not hold count as zeros, whatever lies there
+      bool far = false;
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const bool live = has[g] && k0 + g * 16 + lr < held;
+#pragma unroll
+        for (int s = 0; s < DB; ++s) {
+          if (!live) vc[g].w[s] = 0, vc[g].s[s] = 0;
+          far |= scale_of(vc[g], s) >= kFar;
+        }
+      }
+      if (a.causal && __any(far)) {
+        // A probability of zero does not keep a NaN of a later token out of a sum.  Rare:
+        // count such values by dim among the tokens that a row sees, then drop them.
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int s = 0; s < DB; ++s) {
+            const bf16x8 v = fp4_to_bf16(vc[g].w[s], fp4_scale_operand(scale_of(vc[g], s)));
+            bf16x8 odd;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool is = !(fabsf((float)v[e]) < INFINITY);
+              odd[e] = (bf16)(is ? 1.f : 0.f);
+              if (is) vc[g].w[s] &= ~(0xfu << (4 * e));
+            }
+            *reinterpret_cast<bf16x8*>(own + (g * 16 + lr) * VROW + (lg * DB + s) * 16) = odd;
+            if (scale_of(vc[g], s) == kFp4NaN) vc[g].w[s] = 0;
+          }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int s = 0; s < DB; ++s)
+            if (vc[g].s[s] == kFp4NaN) vc[g].s[s] = 0;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        bf16x8 sees[QT][2];
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              sees[i][g / 2][g % 2 * 4 + r] = (bf16)(k0 + g * 16 + 4 * lg + r < vis[i] ? 1.f : 0.f);
+        for_dims([&](auto J, auto C, const bf16x8& vf) __attribute__((always_inline)) {
+          constexpr int j = decltype(J)::value, c = decltype(C)::value;
+#pragma unroll
+          for (int i = 0; i < QT; ++i) {
+            const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, sees[i][c], zero, 0, 0, 0);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (n[r] > 0.f) o[i][j][r] = NAN;
+          }
+        });
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int s = 0; s < DB; ++s)
+        *reinterpret_cast<bf16x8*>(own + (g * 16 + lr) * VROW + (lg * DB + s) * 16) =
+            fp4_to_bf16(vc[g].w[s], fp4_scale_operand(scale_of(vc[g], s)));
+    f32x4 st[QT][4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i) st[i][g] = zero;
+#pragma unroll
+      for (int s = 0; s < DB; ++s) {
+        const bf16x8 kf = fp4_to_bf16(kc[g].w[s], fp4_scale_operand(scale_of(kc[g], s)));
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+          for (int n = 0; n < NS; ++n)
+            st[i][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][s][n], st[i][g], 0, 0, 0);
+      }
+    }
+    if (tile + kWaves < t_hi) request(tile + kWaves);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+
+    bf16x8 pf[QT][2][NS];
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float x = st[i][g][r] * p.log2_scale;
+          if (!whole) x = has[g] && k0 + g * 16 + 4 * lg + r < vis[i] ? x : -INFINITY;
+          st[i][g][r] = x;
+          top = fmaxf(top, x);
+        }
+      if (__any(top > m[i] + kSlack)) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float to = fmaxf(m[i], top), f = __builtin_amdgcn_exp2f(m[i] - to);
+        m[i] = to;
+        l[i] *= f;
+#pragma unroll
+        for (int j = 0; j < DT; ++j) o[i][j] *= f;
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          bf16 part[NS];
+          split<NS>(__builtin_amdgcn_exp2f(st[i][g][r] - m[i]), part);
+#pragma unroll
+          for (int n = 0; n < NS; ++n) pf[i][g / 2][n][g % 2 * 4 + r] = part[n];
+        }
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+          l[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[i][c][n], l[i], 0, 0, 0);
+    }
+    for_dims([&](auto J, auto C, const bf16x8& vf) __attribute__((always_inline)) {
+      constexpr int j = decltype(J)::value, c = decltype(C)::value;
+#pragma unroll
+      for (int i = 0; i < QT; ++i)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+          o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i][c][n], o[i][j], 0, 0, 0);
+    });
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // The waves' parts join in LDS, in the order of the waves: maximum, then the sums at
+  // that maximum.
+#pragma unroll
+  for (int i = 0; i < QT; ++i)
+    if (lg == 0) part_m[wid][i * 16 + lr] = m[i];
+  __syncthreads();
+  float f[QT];
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    float to = part_m[0][i * 16 + lr];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) to = fmaxf(to, part_m[w][i * 16 + lr]);
+    f[i] = __builtin_amdgcn_exp2f(m[i] - to);
+    m[i] = to;
+    if (lg == 0) part_l[wid][i * 16 + lr] = l[i][0] * f[i];
+  }
+  // a slice of the dims at a time, so that the waves' slices fit where V was
+  constexpr int kRow = DT * 16 + 4;  // floats of a row, apart from the banks of the next
+  static_assert(16 * kRow * 4 <= kKeys * VROW, "a tile of rows fits a wave's V");
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    float* mine = reinterpret_cast<float*>(vt[wid]);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < DT; ++j)
+      *reinterpret_cast<f32x4*>(mine + lr * kRow + j * 16 + 4 * lg) = o[i][j] * f[i];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 16 * DH / 4; e += kWaves * kWave) {
+      const int row = e / (DH / 4), d = e % (DH / 4) * 4, r = r0 + i * 16 + row;
+      f32x4 sum = zero;
+      float total = 0.f, top = kNone;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        sum += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(vt[w]) + row * kRow + d);
+        total += part_l[w][i * 16 + row];
+        top = fmaxf(top, part_m[w][i * 16 + row]);
+      }
+      if (r >= R) continue;
+      if (p.splits > 1) {
+        const int64_t at = (((int64_t)b * ca.H + hk) * p.splits + split_at) * R + r;
+        float* ws = static_cast<float*>(a.workspace);
+        *reinterpret_cast<f32x4*>(ws + at * DH + d) = sum;
+        if (d == 0) {
+          float* ml = ws + (int64_t)a.B * ca.H * p.splits * R * DH + at * 2;
+          ml[0] = top, ml[1] = total;
+        }
+        continue;
+      }
+      const int t = r / p.group, h = hk * p.group + r % p.group;
+      const float inv = 1.0f / total;
+      T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + t * a.out_stride[1] + h * a.out_stride[2];
+      Pack<T, 4> w;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w.v[k] = static_cast<T>(total == 0.f ? 0.f : sum[k] * inv);  // 0: a row that sees nothing
+      *reinterpret_cast<Pack<T, 4>*>(out + d) = w;
+      if (a.lse && d == 0)
+        a.lse[b * a.lse_stride[0] + t * a.lse_stride[1] + h * a.lse_stride[2]] =
+            total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+  }
+}
+
+// Joins the parts of a row, in the order of the splits: a wave a row.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
+  const wam_cache_attention_args& a = p.a;
+  const int R = p.group * a.T, DH = a.cache.dh, lane = threadIdx.x % kWave;
+  const int64_t i = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;  // (b, hk, r)
+  if (i >= (int64_t)a.B * a.cache.H * R) return;
+  const int64_t bh = i / R;
+  const int r = (int)(i % R), b = (int)(bh / a.cache.H), hk = (int)(bh % a.cache.H);
+  const float* ws = static_cast<const float*>(a.workspace);
+  const float* ml = ws + (int64_t)a.B * a.cache.H * p.splits * R * DH;
+  auto at = [&](int s) { return (bh * p.splits + s) * R + r; };
+  float top = kNone;
+  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ml[at(s) * 2]);
+  float total = 0.f, x[2] = {0.f, 0.f};
+  for (int s = 0; s < p.splits; ++s) {
+    const float f = __builtin_amdgcn_exp2f(ml[at(s) * 2] - top);
+    total += ml[at(s) * 2 + 1] * f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (lane + j * kWave < DH) x[j] += ws[at(s) * DH + lane + j * kWave] * f;
+  }
+  const int t = r / p.group, h = hk * p.group + r % p.group;
+  const float inv = 1.0f / total;
+  T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + t * a.out_stride[1] + h * a.out_stride[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    if (lane + j * kWave < DH) out[lane + j * kWave] = static_cast<T>(total == 0.f ? 0.f : x[j] * inv);
+  if (a.lse && lane == 0)
+    a.lse[b * a.lse_stride[0] + t * a.lse_stride[1] + h * a.lse_stride[2]] =
+        total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// Tiles of 16 rows a block takes, and over how many blocks a sequence's tokens go.
+struct AttendPlan {
+  int qt, row_blocks, splits;
+};
+AttendPlan plan_attend(const wam_cache_attention_args& a) {
+  AttendPlan pl;
+  const int64_t R = (int64_t)(a.Hq / a.cache.H) * a.T;
+  const bool exact = a.dtype == WAM_FP32;
+  const int most = exact ? 1 : a.cache.dh <= 64 ? 4 : 2;
+  pl.qt = 1;
+  while (pl.qt < most && pl.qt * 16 < R) pl.qt *= 2;
+  pl.row_blocks = (int)((R + pl.qt * 16 - 1) / (pl.qt * 16));
+  const int64_t blocks = (int64_t)a.B * a.cache.H * pl.row_blocks;
+  const int64_t tiles = ((int64_t)a.table.width * a.cache.page + kKeys - 1) / kKeys;
+  // about four blocks a CU, each wave with two tiles at least
+  const int64_t want = (1024 + blocks - 1) / blocks;
+  pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want, tiles / (2 * kWaves)));
+  return pl;
+}
+
+size_t workspace_of(const wam_cache_attention_args& a, const AttendPlan& pl) {
+  if (pl.splits == 1) return 0;
+  const size_t rows = (size_t)a.B * a.Hq * a.T * pl.splits;
+  return rows * (a.cache.dh + 2) * sizeof(float);
+}
+
+template <int DB, int NS>
+hipError_t launch_blocks_of(const AttendParams& p, const AttendPlan& pl, dim3 grid, hipStream_t s) {
+  if (pl.qt == 1) launch_k(attend_kernel<DB, 1, NS>, grid, kWaves * kWave, 0, s, p);
+  else if constexpr (NS == 1) {
+    if (pl.qt == 2) launch_k(attend_kernel<DB, 2, NS>, grid, kWaves * kWave, 0, s, p);
+    else if constexpr (DB <= 2) launch_k(attend_kernel<DB, 4, NS>, grid, kWaves * kWave, 0, s, p);
+  }
+  return hipGetLastError();
+}
+template <int NS>
+hipError_t launch_attend(const AttendParams& p, const AttendPlan& pl, hipStream_t s) {
+  const int64_t blocks = (int64_t)p.a.B * p.a.cache.H * pl.row_blocks * pl.splits;
+  if (blocks * kWaves * kWave > 0xffffffffll) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)blocks);
+  hipError_t e;
+  switch (p.a.cache.dh) {
+    case 32: e = launch_blocks_of<1, NS>(p, pl, grid, s); break;
+    case 64: e = launch_blocks_of<2, NS>(p, pl, grid, s); break;
+    case 96: e = launch_blocks_of<3, NS>(p, pl, grid, s); break;
+    default: e = launch_blocks_of<4, NS>(p, pl, grid, s); break;
+  }
+  if (e != hipSuccess || pl.splits == 1) return e;
+  typedef typename std::conditional<NS == 1, bf16, float>::type T;
+  const int64_t rows = (int64_t)p.a.B * p.a.Hq * p.a.T;
+  launch_k(join_kernel<T>, dim3((unsigned)((rows + 3) / 4)), 256, 0, s, p);
+  return hipGetLastError();
+}
+
+int check_attention(const wam_cache_attention_args* a) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: null argument");
+  if (a->B < 0 || a->T < 0) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: sizes must be >= 0");
+  if (!float_type(a->dtype)) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: q must be WAM_FP32 or WAM_BF16");
+  const int st = check_cache(a->cache, a->table, false, a->B == 0 || a->T == 0, "wam_cache_attention");
+  if (st) return st;
+  if (a->Hq < 1 || a->Hq % a->cache.H)
+    return noalloc_fail(WAM_E_SHAPE, "wam_cache_attention: Hq must be a multiple of the cache's heads");
+  if (!(a->scale > 0.0) || !(a->scale < 1e30)) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: scale must be > 0");
+  if ((int64_t)a->B * a->T > WAM_MAX_ROWS || (int64_t)a->B * a->T * a->Hq > INT32_MAX - 65536)
+    return noalloc_fail(WAM_E_SHAPE, "wam_cache_attention: too many rows");
+  return WAM_OK;
+}
+
+}  // namespace
+
+}  // namespace wam
+
+using namespace wam;
+
+extern "C" {
+
+size_t wam_cache_attention_workspace(const wam_cache_attention_args* a) {
+  if (check_attention(a) || a->B == 0 || a->T == 0) return 0;
+  return workspace_of(*a, plan_attend(*a));
+}
+
+int wam_cache_attention(const wam_cache_attention_args* a, void* hip_stream) {
+  const int st = check_attention(a);
+  if (st) return st;
+  if (a->B == 0 || a->T == 0) return WAM_OK;
+  if (!a->q || !a->out || !a->lengths) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: null q, out or lengths");
+  const int64_t unit = type_size(a->dtype), size[3] = {a->B, a->T, a->Hq};
+  if (!aligned_to(a->q, unit) || !aligned_to(a->out, unit) || !aligned_to(a->lse, 4) || !aligned_to(a->lengths, 4) ||
+      !aligned_to(a->rows, 4))
+    return noalloc_fail(WAM_E_ARG, "wam_cache_attention: buffers must be aligned to their elements");
+  if (!strides_ok(a->q_stride, 3)) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: strides must be >= 0");
+  if (!strides_ok(a->out_stride, 3) || !distinct(a->out_stride, size, 3, a->cache.dh) ||
+      (a->lse && (!strides_ok(a->lse_stride, 3) || !distinct(a->lse_stride, size, 3, 1))))
+    return noalloc_fail(WAM_E_ARG, "wam_cache_attention: the elements of a result must be distinct");
+  if (a->q == a->out) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: out must not be q");
+  const AttendPlan pl = plan_attend(*a);
+  if (const size_t need = workspace_of(*a, pl)) {
+    if (!a->workspace || !aligned_to(a->workspace, 16) || a->workspace_bytes < need)
+      return noalloc_fail(WAM_E_WORKSPACE, "wam_cache_attention: workspace too small or not on 16 bytes");
+  }
+  AttendParams p;
+  p.a = *a;
+  if (a->cache.pages == 0) p.a.table.width = 0;  // no token has a page
+  p.shift = 0;
+  while ((1 << p.shift) < a->cache.page) ++p.shift;
+  p.group = a->Hq / a->cache.H;
+  p.row_blocks = pl.row_blocks;
+  p.splits = pl.splits;
+  p.log2_scale = (float)(a->scale * 1.4426950408889634);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  const hipError_t e = a->dtype == WAM_BF16 ? launch_attend<1>(p, pl, s) : launch_attend<3>(p, pl, s);
+  if (e == hipErrorInvalidConfiguration) return noalloc_fail(WAM_E_SHAPE, "wam_cache_attention: too many blocks for one launch");
+  if (e != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_cache_attention: kernel launch failed");
+  return WAM_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,309 @@
+// 4-bit blocks: into them, back to values, and new keys and values into a paged cache
+// of them (gfx950).  All are bound by memory.
+#include <math.h>
+
+#include <algorithm>
+
+#include "cache.h"
+#include "fp4.h"
+#include "layer_util.h"
+
+namespace wam {
+
+namespace {
+
+// ------------------------------------------------------------- blocks of a matrix
+// A lane takes eight neighbouring columns (16 bytes of bf16), four lanes a block, whose
+// maximum they share without LDS; a wave stores its codes as 256 bytes side by side.
+template <typename T>
+__global__ __launch_bounds__(256) void quantize_fp4_kernel(wam_quantize_fp4_args a, int kb) {
+  const uint32_t i = blockIdx.x * 64u + threadIdx.x / 4;  // block
+  const int m = (int)(i / (uint32_t)kb), bk = (int)(i % (uint32_t)kb);
+  if (m >= a.M) return;
+  const int col = bk * kFp4Block + (threadIdx.x % 4) * 8;
+  float x[8];
+  load_n(x, static_cast<const T*>(a.x) + m * a.x_stride + col, a.K - col);
+  const uint32_t byte = fp4_scale(quad_max(most_of(x)));
+  if (threadIdx.x % 4 == 0) a.scale[m * a.scale_stride + bk] = (uint8_t)byte;
+  store_fp4(a.q + m * a.q_stride + col / 2, pack_fp4(x, byte), a.K - col);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void dequantize_fp4_kernel(wam_dequantize_fp4_args a, int kb, bool stream) {
+  const uint32_t i = blockIdx.x * 64u + threadIdx.x / 4;
+  const int m = (int)(i / (uint32_t)kb), bk = (int)(i % (uint32_t)kb);
+  if (m >= a.M) return;
+  const int col = bk * kFp4Block + (threadIdx.x % 4) * 8, n = a.K - col;
+  if (n <= 0) return;
+  const uint8_t* q = a.q + m * a.q_stride + col / 2;
+  uint32_t w = 0;
+  if (n >= 7) {
+    struct __attribute__((packed, aligned(1))) Word {
+      uint32_t v;
+    };
+    w = reinterpret_cast<const Word*>(q)->v;
+  } else {
+#pragma unroll
+    for (int b = 0; b < 3; ++b)
+      if (2 * b < n) w |= (uint32_t)q[b] << (8 * b);
+  }
+  float x[8];
+  fp4_to_f32(x, w, fp4_scale_operand(a.scale[m * a.scale_stride + bk]));
+  store_n(static_cast<T*>(a.x) + m * a.x_stride + col, x, n, stream);
+}
+
+// ------------------------------------------------------------- appending to a cache
+constexpr int kAppendMaxPairs = 64;  // heads of at most 128
+template <int P>
+struct AppendParams {
+  wam_cache_append_args a;
+  int pairs, end0, end1, shift;
+  int lanes;        // lanes of a head vector, a power of two >= dh / 8
+  int rows_block;   // rows of a thread block
+  int heads_block;  // and heads
+  double turns[P];  // revolutions per unit of position
+};
+
+__device__ __forceinline__ double lanes_sum_d(double v, int n) {
+  for (int o = 1; o < n; o *= 2) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// A lane takes eight neighbouring values of a head vector, four lanes a block of it.
+// Keys are normed and turned in float64 and rounded to float32 once: a value next to a
+// border between two codes moves by a whole step, so with float32 arithmetic the codes
+// would hang on the order of its roundings.  The matrix pipe is idle and the vector
+// pipe does float64 at the rate of float32, so that costs little beside the loads.
+// A block's angles are computed once, in LDS, for all its heads; the other value of a
+// pair is loaded again (from the cache that has just delivered it) rather than
+// exchanged, which holds for any sections and layout.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams<P> p) {
+  extern __shared__ double2 turn[];  // [rows_block][pairs]: cos, sin
+  const wam_cache_append_args& a = p.a;
+  const wam_cache& ca = a.cache;
+  const bool isk = blockIdx.z == 0;
+  const int rows = a.B * a.T, row0 = blockIdx.x * p.rows_block;
+  const int vectors = 256 / p.lanes;  // of the block at a time
+  const int slot = threadIdx.x / p.lanes, unit = threadIdx.x % p.lanes;
+  const int col = 8 * unit;
+  const int h0 = blockIdx.y * p.heads_block, heads = min(p.heads_block, ca.H - h0);
+  const int live_rows = min(p.rows_block, rows - row0);
+
+  if (isk) {
+    for (int i = threadIdx.x; i < live_rows * p.pairs; i += 256) {
+      const int row = row0 + i / p.pairs, j = i % p.pairs;
+      const float* pos = a.pos + row / a.T * a.pos_stride + row % a.T * 3;
+      // in revolutions, so that dropping the whole ones is exact
+      double t = (double)pos[j < p.end0 ? 0 : j < p.end1 ? 1 : 2] * p.turns[j];
+      t -= rint(t);
+      double c, s;
+      sincospi(2.0 * t, &s, &c);
+      turn[i] = make_double2(c, s);
+    }
+    __syncthreads();
+  }
+  const double inv = 1.0 / (double)ca.dh;
+  for (int v = slot; v < live_rows * heads; v += vectors) {
+    const int r = v / heads, h = h0 + v % heads, row = row0 + r;
+    const int b = row / a.T, t = row % a.T;
+    if (a.rows && t >= a.rows[b]) continue;
+    const int64_t token = (int64_t)a.start[b] + t;
+    const int page = token > INT32_MAX ? -1 : page_of(a.table.entry + b * a.table.stride, a.table.width, p.shift, ca.pages, (int)token);
+    if (page < 0) continue;
+    const int64_t place = token & ((1 << p.shift) - 1);
+    float y[8];
+    const T* x = static_cast<const T*>(isk ? a.k : a.v) + (isk ? b * a.k_stride[0] + t * a.k_stride[1] + h * a.k_stride[2]
+                                                              : b * a.v_stride[0] + t * a.v_stride[1] + h * a.v_stride[2]);
+    const int n = col < ca.dh ? 8 : 0;
+    load_n(y, x + col, n);
+    if (isk && (p.pairs || a.k_gain)) {
+      double d[8], rs = 1.0;
+      if (a.k_gain) {
+        double ss = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss += (double)y[i] * (double)y[i];
+        rs = 1.0 / sqrt(lanes_sum_d(ss, p.lanes) * inv + a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[i] = (double)y[i] * rs;
+        if (a.k_gain && n) d[i] *= (double)a.k_gain[col + i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int e = col + i;
+        if (e >= 2 * p.pairs || !n) continue;
+        const bool pairs = a.layout == WAM_ROPE_PAIRS;
+        const bool first = pairs ? e % 2 == 0 : e < p.pairs;
+        const int partner = pairs ? e ^ 1 : first ? e + p.pairs : e - p.pairs;
+        double o = (double)to_f32(x[partner]) * rs;
+        if (a.k_gain) o *= (double)a.k_gain[partner];
+        const double2 cs = turn[r * p.pairs + (pairs ? e / 2 : first ? e : partner)];
+        y[i] = (float)(d[i] * cs.x + (first ? -o : o) * cs.y);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i >= 2 * p.pairs) y[i] = (float)d[i];
+    }
+    const uint32_t byte = fp4_scale(quad_max(most_of(y)));
+    if (!n) continue;
+    const int64_t* st = isk ? ca.k_stride : ca.v_stride;
+    const int64_t* ss = isk ? ca.k_scale_stride : ca.v_scale_stride;
+    uint8_t* q = (isk ? ca.k : ca.v) + page * st[0] + place * st[1] + h * st[2];
+    *reinterpret_cast<uint32_t*>(q + col / 2) = pack_fp4(y, byte);
+    if (unit % 4 == 0)
+      ((isk ? ca.k_scale : ca.v_scale) + page * ss[0] + place * ss[1] + h * ss[2])[col / kFp4Block] = (uint8_t)byte;
+  }
+}
+
+template <int P>
+hipError_t launch_append(const wam_cache_append_args& a, int shift, hipStream_t s) {
+  AppendParams<P> p;
+  p.a = a;
+  p.shift = shift;
+  p.end0 = a.sections[0];
+  p.end1 = p.end0 + a.sections[1];
+  p.pairs = p.end1 + a.sections[2];
+  for (int i = 0; i < p.pairs; ++i) p.turns[i] = a.freq[i] * (0.5 / M_PI);
+  p.lanes = 4;
+  while (p.lanes * 8 < a.cache.dh) p.lanes *= 2;
+  const int rows = a.B * a.T, H = a.cache.H;
+  // rows and heads of a block: all heads of a row share its angles
+  p.rows_block = std::min(rows, 8);
+  p.heads_block = H;
+  const dim3 grid((rows + p.rows_block - 1) / p.rows_block, (H + p.heads_block - 1) / p.heads_block, 2);
+  const size_t lds = sizeof(double2) * p.rows_block * p.pairs;
+  if (a.dtype == WAM_BF16) launch_k(cache_append_kernel<bf16, P>, grid, 256, lds, s, p);
+  else launch_k(cache_append_kernel<float, P>, grid, 256, lds, s, p);
+  return hipGetLastError();
+}
+
+int page_shift(int page) {
+  int s = 0;
+  while ((1 << s) < page) ++s;
+  return s;
+}
+
+}  // namespace
+
+// Status of a cache and its table; `what` is the call's name.  empty: the call has no
+// rows, so that nothing needs to be there.
+int check_cache(const wam_cache& c, const wam_page_table& t, bool written, bool empty, const char* what) {
+  static thread_local char msg[160];
+  auto fail = [&](int code, const char* text) {
+    snprintf(msg, sizeof(msg), "%s: %s", what, text);
+    return noalloc_fail(code, msg);
+  };
+  if (c.pages < 0 || c.H < 1 || t.width < 0) return fail(WAM_E_ARG, "a cache needs heads, and pages and table >= 0");
+  if (c.dh < 32 || c.dh > 128 || c.dh % kFp4Block) return fail(WAM_E_SHAPE, "head size must be 32, 64, 96 or 128");
+  if (c.page < 16 || c.page > 4096 || (c.page & (c.page - 1)))
+    return fail(WAM_E_SHAPE, "pages must hold a power of two of tokens, 16 to 4096");
+  if ((int64_t)t.width * c.page > INT32_MAX - 4096) return fail(WAM_E_SHAPE, "a sequence must stay below 2^31 - 4096 tokens");
+  if (c.H > WAM_MAX_ROWS) return fail(WAM_E_SHAPE, "too many heads");
+  if (empty || c.pages == 0 || t.width == 0) return WAM_OK;
+  if (!c.k || !c.v || !c.k_scale || !c.v_scale || !t.entry) return fail(WAM_E_ARG, "null cache or table");
+  if (!aligned_to(c.k, 4) || !aligned_to(c.v, 4) || !aligned_to(t.entry, 4))
+    return fail(WAM_E_ARG, "codes and table must start on 4 bytes");
+  if (!strides_ok(c.k_stride, 3) || !strides_ok(c.v_stride, 3) || !strides_ok(c.k_scale_stride, 3) ||
+      !strides_ok(c.v_scale_stride, 3) || !strides_ok(&t.stride, 1))
+    return fail(WAM_E_ARG, "strides must be >= 0");
+  for (int i = 0; i < 3; ++i)
+    if (c.k_stride[i] % 4 || c.v_stride[i] % 4) return fail(WAM_E_ARG, "strides of codes must be multiples of 4");
+  const int64_t size[3] = {c.pages, c.page, c.H};
+  if (written && (!distinct(c.k_stride, size, 3, c.dh / 2) || !distinct(c.v_stride, size, 3, c.dh / 2) ||
+                  !distinct(c.k_scale_stride, size, 3, c.dh / kFp4Block) ||
+                  !distinct(c.v_scale_stride, size, 3, c.dh / kFp4Block)))
+    return fail(WAM_E_ARG, "the bytes of the cache must be distinct");
+  return WAM_OK;
+}
+
+}  // namespace wam
+
+using namespace wam;
+
+extern "C" {
+
+int wam_quantize_fp4(const wam_quantize_fp4_args* a, void* hip_stream) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp4: null argument");
+  if (a->M < 0 || a->K < 0) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp4: sizes must be >= 0");
+  if (!float_type(a->dtype)) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp4: x must be WAM_FP32 or WAM_BF16");
+  if (a->M == 0 || a->K == 0) return WAM_OK;
+  if (!a->x || !a->q || !a->scale) return noalloc_fail(WAM_E_ARG, "wam_quantize_fp4: null buffer");
+  if (!aligned_to(a->x, type_size(a->dtype)))
+    return noalloc_fail(WAM_E_ARG, "wam_quantize_fp4: x must be aligned to its elements");
+  if (a->x == a->q || a->x == a->scale || a->q == a->scale)
+    return noalloc_fail(WAM_E_ARG, "wam_quantize_fp4: x, q and scale must be different buffers");
+  const int64_t kb = ((int64_t)a->K + kFp4Block - 1) / kFp4Block;
+  if (!strides_ok(&a->x_stride, 1) || !strides_ok(&a->q_stride, 1) || !strides_ok(&a->scale_stride, 1) ||
+      (a->M > 1 && (a->q_stride < ((int64_t)a->K + 1) / 2 || a->scale_stride < kb)))
+    return noalloc_fail(WAM_E_ARG, "wam_quantize_fp4: strides must be >= 0, and rows of the results distinct");
+  if (a->M * kb > 32 * kMaxGrid || a->K > INT32_MAX - kFp4Block)
+    return noalloc_fail(WAM_E_SHAPE, "wam_quantize_fp4: too many blocks for one launch");
+  const dim3 grid((unsigned)((a->M * kb + 63) / 64));
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (a->dtype == WAM_BF16) launch_k(quantize_fp4_kernel<bf16>, grid, 256, 0, s, *a, (int)kb);
+  else launch_k(quantize_fp4_kernel<float>, grid, 256, 0, s, *a, (int)kb);
+  if (hipGetLastError() != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_quantize_fp4: kernel launch failed");
+  return WAM_OK;
+}
+
+int wam_dequantize_fp4(const wam_dequantize_fp4_args* a, void* hip_stream) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_dequantize_fp4: null argument");
+  if (a->M < 0 || a->K < 0) return noalloc_fail(WAM_E_ARG, "wam_dequantize_fp4: sizes must be >= 0");
+  if (!float_type(a->dtype)) return noalloc_fail(WAM_E_ARG, "wam_dequantize_fp4: x must be WAM_FP32 or WAM_BF16");
+  if (a->M == 0 || a->K == 0) return WAM_OK;
+  if (!a->x || !a->q || !a->scale) return noalloc_fail(WAM_E_ARG, "wam_dequantize_fp4: null buffer");
+  if (!aligned_to(a->x, type_size(a->dtype)))
+    return noalloc_fail(WAM_E_ARG, "wam_dequantize_fp4: x must be aligned to its elements");
+  if (a->x == a->q || a->x == a->scale) return noalloc_fail(WAM_E_ARG, "wam_dequantize_fp4: x must not be q or scale");
+  const int64_t kb = ((int64_t)a->K + kFp4Block - 1) / kFp4Block;
+  if (!strides_ok(&a->x_stride, 1) || !strides_ok(&a->q_stride, 1) || !strides_ok(&a->scale_stride, 1) ||
+      (a->M > 1 && a->x_stride < a->K))
+    return noalloc_fail(WAM_E_ARG, "wam_dequantize_fp4: strides must be >= 0, and rows of x distinct");
+  if (a->M * kb > 32 * kMaxGrid || a->K > INT32_MAX - kFp4Block)
+    return noalloc_fail(WAM_E_SHAPE, "wam_dequantize_fp4: too many blocks for one launch");
+  const dim3 grid((unsigned)((a->M * kb + 63) / 64));
+  const bool stream = (int64_t)a->M * a->K * type_size(a->dtype) > kStreamBytes;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (a->dtype == WAM_BF16) launch_k(dequantize_fp4_kernel<bf16>, grid, 256, 0, s, *a, (int)kb, stream);
+  else launch_k(dequantize_fp4_kernel<float>, grid, 256, 0, s, *a, (int)kb, stream);
+  if (hipGetLastError() != hipSuccess) return noalloc_fail(WAM_E_HIP, "wam_dequantize_fp4: kernel launch failed");
+  return WAM_OK;
+}
+
+int wam_cache_append(const wam_cache_append_args* a, void* hip_stream) {
+  if (!a) return noalloc_fail(WAM_E_ARG, "wam_cache_append: null argument");
+  if (a->B < 0 || a->T < 0) return noalloc_fail(WAM_E_ARG, "wam_cache_append: sizes must be >= 0");
+  if (!float_type(a->dtype)) return noalloc_fail(WAM_E_ARG, "wam_cache_append: k and v must be WAM_FP32 or WAM_BF16");
+  if (a->layout != WAM_ROPE_HALVES && a->layout != WAM_ROPE_PAIRS)
+    return noalloc_fail(WAM_E_ARG, "wam_cache_append: unknown layout");
+  int st = check_cache(a->cache, a->table, true, a->B == 0 || a->T == 0, "wam_cache_append");
+  if (st) return st;
+  int64_t pairs = 0;
+  for (int i = 0; i < 3; ++i) {
+    if (a->sections[i] < 0) return noalloc_fail(WAM_E_ARG, "wam_cache_append: sections must be >= 0");
+    pairs += a->sections[i];
+  }
+  if (2 * pairs > a->cache.dh)
+    return noalloc_fail(WAM_E_SHAPE, "wam_cache_append: the sections' pairs must fit the head (2 P <= dh)");
+  if (pairs > 0 && !a->freq) return noalloc_fail(WAM_E_ARG, "wam_cache_append: null freq");
+  if (a->k_gain && (!(a->eps >= 0.0) || !aligned_to(a->k_gain, 4)))
+    return noalloc_fail(WAM_E_ARG, "wam_cache_append: eps must be >= 0");
+  if ((int64_t)a->B * a->T > WAM_MAX_ROWS) return noalloc_fail(WAM_E_SHAPE, "wam_cache_append: too many rows");
+  if (a->B == 0 || a->T == 0) return WAM_OK;
+  if (pairs > 0 && (!a->pos || !aligned_to(a->pos, 4) || !strides_ok(&a->pos_stride, 1)))
+    return noalloc_fail(WAM_E_ARG, "wam_cache_append: pairs need pos, aligned, with a stride >= 0");
+  if (!a->k || !a->v || !a->start) return noalloc_fail(WAM_E_ARG, "wam_cache_append: null k, v or start");
+  if (!aligned_to(a->k, type_size(a->dtype)) || !aligned_to(a->v, type_size(a->dtype)) || !aligned_to(a->start, 4) ||
+      !aligned_to(a->rows, 4) || !strides_ok(a->k_stride, 3) || !strides_ok(a->v_stride, 3))
+    return noalloc_fail(WAM_E_ARG, "wam_cache_append: strides must be >= 0 and buffers aligned to their elements");
+  if (a->cache.pages == 0 || a->table.width == 0) return WAM_OK;  // no token has a page
+  const int shift = page_shift(a->cache.page);
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  if (launch_append<kAppendMaxPairs>(*a, shift, s) != hipSuccess)
+    return noalloc_fail(WAM_E_HIP, "wam_cache_append: kernel launch failed");
+  return WAM_OK;
+}
+
+}  // extern "C"

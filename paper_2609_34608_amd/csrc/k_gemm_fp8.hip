@@ -4,6 +4,7 @@
 #include <utility>
 
 #include "gemm_fp8.h"
+#include "layer_util.h"
 
 namespace wam {
 
@@ -113,8 +114,6 @@ hipError_t launch_layer_any(const Fp8Operands& p, const GemmArgs& g, int cfg, hi
   ((cfg == C ? (void)(e = launch_layer_cfg<C>(p, g, s)) : (void)0), ...);
   return e;
 }
-
-bool aligned_to(const void* p, int64_t n) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)n == 0; }
 
 }  // namespace
 

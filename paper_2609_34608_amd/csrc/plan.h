@@ -127,6 +127,32 @@ int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K, Fp8Result result = 
   return best;
 }
 
+// ---------------------------------------------------------------- 4-bit products
+// Tiles of gemm_fp4.h and their cost, a stage being 256 of K.
+constexpr TileCfg kFp4Cfgs[] = {
+    {256, 256, 2, 4, 2, 256, 1, {1.27f}, {6.01f}},
+    {192, 256, 2, 4, 2, 256, 1, {1.08f}, {5.01f}},
+    {128, 256, 2, 4, 3, 256, 1, {0.77f}, {4.60f}},
+    {160, 128, 2, 2, 2, 256, 2, {0.63f, 1.14f}, {3.97f, 4.92f}},
+    {64, 128, 2, 2, 2, 256, 3, {0.42f, 0.59f, 0.95f}, {2.86f, 3.44f, 2.65f}},
+    {96, 64, 2, 2, 3, 256, 2, {0.30f, 0.54f}, {2.90f, 2.11f}},
+    {64, 64, 2, 2, 3, 256, 3, {0.24f, 0.38f, 0.62f}, {2.83f, 3.11f, 1.54f}},
+    {32, 32, 2, 2, 4, 256, 4, {0.15f, 0.18f, 0.26f, 0.36f}, {2.56f, 2.70f, 3.09f, 1.26f}},
+};
+// blocks: 4-bit results, only tiles whose waves hold whole blocks of 32 columns
+template <int NC>
+int plan_fp4(const TileCfg (&cfgs)[NC], int M, int N, int K, bool blocks) {
+  int best = -1;
+  double bc = 0.0;
+  for (int c = 0; c < NC; ++c) {
+    const TileCfg& t = cfgs[c];
+    if (blocks && (t.bn / t.wgn) % 32) continue;
+    const double v = tile_cost(t, M, N, (K + 255) / 256 * 64);  // tile_cost counts stages of 64
+    if (best < 0 || v < bc) best = c, bc = v;
+  }
+  return best;
+}
+
 // ---------------------------------------------------------------- attention
 // bf16 kernel forms: running max; and with a bound on the scores the fixed
 // reference in a software-pipelined loop, a plain loop (also with two wave

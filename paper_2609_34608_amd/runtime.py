@@ -6,9 +6,11 @@ denoising path and of the adaptation operators runs in libwam's kernels.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import struct
 from array import array
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import numpy as np
 import torch
@@ -401,6 +403,10 @@ _ROPE_ARGS = struct.Struct("@10i4P12qPqP2Pf")
 _NORM_ARGS = struct.Struct("@8i5P10q3P6q2P2f")
 _QUANTIZE_ARGS = struct.Struct("@4iPqPqPq")
 _MATMUL_ARGS = struct.Struct("@5iPqPqPqPqPPqPq")
+_FP4_ARGS = struct.Struct("@3iPqPqPq")
+_CACHE_ARGS = "4i4P12qPqi0P"  # the cache and its table, inside the calls' structs
+_APPEND_ARGS = struct.Struct("@7i0P" + _CACHE_ARGS + "2P6q3PqPPd")
+_ATTENTION_ARGS = struct.Struct("@5i0P" + _CACHE_ARGS + "P3qP3qP3q2PdPN")
 
 
 def _operand(t, what, dtypes, index, shape=None):
@@ -675,6 +681,221 @@ def matmul_fp8(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_d
                  scale_stride)
     _call(abi.lib().wam_matmul_fp8, args, index, stream, "wam_matmul_fp8")
     return (out, out_scale) if kind == abi.WAM_FP8 else out
+
+
+_U8 = (torch.uint8,)
+_I32 = (torch.int32,)
+
+
+def _byte_rows(shape, dev, unit):
+    """A new tensor of bytes whose rows start a multiple of `unit` bytes apart."""
+    n = shape[-1]
+    if n % unit == 0:
+        return torch.empty(shape, dtype=torch.uint8, device=dev)
+    return torch.empty((*shape[:-1], -(-n // unit) * unit), dtype=torch.uint8, device=dev)[..., :n]
+
+
+def quantize_fp4(x, *, q=None, scale=None, stream: torch.cuda.Stream | None = None):
+    """4-bit blocks of 32 columns (wam_quantize_fp4) of x [M, K], float32 or bfloat16.
+    Returns (q, scale): uint8 [M, ceil(K / 2)], two codes a byte, and uint8
+    [M, ceil(K / 32)], a power of two each, with rows as matmul_fp4 takes them (a
+    multiple of 16 and 4 bytes apart)."""
+    index = _first(x, "quantize_fp4: x", _REAL, 2)
+    M, K = x.shape
+    codes, blocks = (M, -(-K // 2)), (M, -(-K // 32))
+    q = (_new(stream, _byte_rows, codes, x.device, 16) if q is None else
+         _operand(q, "quantize_fp4: q", _U8, index, codes))
+    scale = (_new(stream, _byte_rows, blocks, x.device, 4) if scale is None else
+             _operand(scale, "quantize_fp4: scale", _U8, index, blocks))
+    a = _pack(_FP4_ARGS, "quantize_fp4", M, K, _TYPES[x.dtype], x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0),
+              scale.data_ptr(), scale.stride(0))
+    _call(abi.lib().wam_quantize_fp4, a, index, stream, "wam_quantize_fp4")
+    return q, scale
+
+
+def dequantize_fp4(q, scale, *, columns=None, dtype=None, out=None, stream: torch.cuda.Stream | None = None):
+    """The values that 4-bit blocks stand for (wam_dequantize_fp4): q [M, n] and scale
+    [M, ceil(columns / 32)] as quantize_fp4 gives them; columns: 2 n (the default), or
+    2 n - 1 where the last code is none.  dtype: bfloat16 (the default) or float32 of
+    a new result, [M, columns]."""
+    index = _first(q, "dequantize_fp4: q", _U8, 2)
+    M, n = q.shape
+    K = 2 * n if columns is None else columns
+    if K not in (2 * n, 2 * n - 1) or K < 0:
+        raise WamError("dequantize_fp4: columns must be twice those of q, or one less")
+    _operand(scale, "dequantize_fp4: scale", _U8, index, (M, -(-K // 32)))
+    if out is None:
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in _REAL:
+            raise WamError(f"dequantize_fp4: dtype {dtype} is not supported")
+        out = _new(stream, torch.empty, (M, K), dtype=dtype, device=q.device)
+    else:
+        _operand(out, "dequantize_fp4: out", _REAL if dtype is None else (dtype,), index, (M, K))
+    a = _pack(_FP4_ARGS, "dequantize_fp4", M, K, _choice(_TYPES, out.dtype, "dequantize_fp4: dtype"), q.data_ptr(),
+              q.stride(0), scale.data_ptr(), scale.stride(0), out.data_ptr(), out.stride(0))
+    _call(abi.lib().wam_dequantize_fp4, a, index, stream, "wam_dequantize_fp4")
+    return out
+
+
+def matmul_fp4(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_dtype=None, out_scale=None,
+               stream: torch.cuda.Stream | None = None):
+    """out [M, N] = act(a w^T + bias) of matrices in 4-bit blocks (wam_matmul_fp4): codes a
+    [M, n] and w [N, n] with their scales [M or N, ceil(n / 16)], as quantize_fp4 gives
+    them (each byte of a row is two values: an odd last one has a zero beside it); rows
+    are read up to the next multiple of 16 bytes (scales: of 4), what lies there does not
+    enter.  bias float32 [N]; gelu: the tanh form.  out: float32, bfloat16 (default: a
+    new bfloat16 one); uint8 asks for 4-bit blocks of the result: then returns
+    (out [M, ceil(N / 2)], out_scale [M, ceil(N / 32)]) for the next product."""
+    index = _first(a, "matmul_fp4: a", _U8, 2)
+    _operand(w, "matmul_fp4: w", _U8, index)
+    M, n = a.shape
+    if w.dim() != 2 or w.shape[1] != n:
+        raise WamError("matmul_fp4: needs a and w with the same number of columns")
+    N, kb = w.shape[0], -(-n // 16)
+    _operand(a_scale, "matmul_fp4: a_scale", _U8, index, (M, kb))
+    _operand(w_scale, "matmul_fp4: w_scale", _U8, index, (N, kb))
+    if bias is not None:
+        _operand(bias, "matmul_fp4: bias", _F32, index, (N,))
+    kind = torch.bfloat16 if out is None and out_dtype is None else out_dtype if out is None else out.dtype
+    blocks = kind == torch.uint8
+    if not blocks and kind not in _REAL:
+        raise WamError(f"matmul_fp4: out_dtype {kind} is not supported")
+    shape = (M, -(-N // 2)) if blocks else (M, N)
+    if out is None:
+        out = (_new(stream, _byte_rows, shape, a.device, 16) if blocks else
+               _new(stream, torch.empty, shape, dtype=kind, device=a.device))
+    else:
+        _operand(out, "matmul_fp4: out", (kind,) if out_dtype is None else (out_dtype,), index, shape)
+    scale_at = scale_stride = 0
+    if blocks:
+        shape = (M, -(-N // 32))
+        out_scale = (_new(stream, _byte_rows, shape, a.device, 4) if out_scale is None else
+                     _operand(out_scale, "matmul_fp4: out_scale", _U8, index, shape))
+        scale_at, scale_stride = out_scale.data_ptr(), out_scale.stride(0)
+    args = _pack(_MATMUL_ARGS, "matmul_fp4", M, N, 2 * n, abi.WAM_FP4 if blocks else _TYPES[kind],
+                 abi.WAM_ACT_GELU if gelu else abi.WAM_ACT_NONE, a.data_ptr(), a.stride(0), a_scale.data_ptr(),
+                 a_scale.stride(0), w.data_ptr(), w.stride(0), w_scale.data_ptr(), w_scale.stride(0), _ptr_or_0(bias),
+                 out.data_ptr(), out.stride(0), scale_at, scale_stride)
+    _call(abi.lib().wam_matmul_fp4, args, index, stream, "wam_matmul_fp4")
+    return (out, out_scale) if blocks else out
+
+
+class KvCache(NamedTuple):
+    """Keys and values of a layer in 4-bit blocks, in pages of tokens: codes uint8
+    [pages, page, H, dh / 2] and scales uint8 [pages, page, H, dh / 32], any strides
+    with a head contiguous (a plain tuple of the four does too)."""
+    k: torch.Tensor
+    k_scale: torch.Tensor
+    v: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def new_kv_cache(pages, page, heads, dh, device="cuda:0") -> KvCache:
+    """A KvCache of zeros whose pages hold a head's tokens side by side, as
+    cache_attention reads them fastest."""
+    if dh % 32 or min(pages, page, heads, dh) < 0:
+        raise WamError("new_kv_cache: sizes must be >= 0, heads whole blocks of 32")
+    make = lambda n: torch.zeros((pages, heads, page, n), dtype=torch.uint8, device=device).transpose(1, 2)  # noqa: E731
+    return KvCache(make(dh // 2), make(dh // 32), make(dh // 2), make(dh // 32))
+
+
+def _cache_values(cache, table, index, B, H, dh, what):
+    """A cache and its page table as the calls' structs hold them."""
+    if not isinstance(cache, tuple) or len(cache) != 4:
+        raise WamError(f"{what}: cache must be a KvCache")
+    k, k_scale, v, v_scale = cache
+    _operand(k, f"{what}: cache", _U8, index)
+    if k.dim() != 4 or (H is not None and k.shape[2] != H) or 2 * k.shape[3] != dh:
+        raise WamError(f"{what}: the cache's codes must be [pages, page, H, dh / 2]")
+    pages, page, H, half = k.shape
+    _operand(v, f"{what}: cache", _U8, index, k.shape)
+    scales = (pages, page, H, half // 16)
+    _operand(k_scale, f"{what}: cache", _U8, index, scales)
+    _operand(v_scale, f"{what}: cache", _U8, index, scales)
+    _operand(table, f"{what}: table", _I32, index)
+    if table.dim() != 2 or table.shape[0] != B:
+        raise WamError(f"{what}: table must be [B, pages of a sequence]")
+    return (pages, page, H, dh, k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), *k.stride()[:3],
+            *k_scale.stride()[:3], *v.stride()[:3], *v_scale.stride()[:3], table.data_ptr(), table.stride(0),
+            table.shape[1])
+
+
+def _per_sequence(t, what, index, B):
+    """Pointer of int32 [B] or None."""
+    if t is None:
+        return 0
+    _operand(t, what, _I32, index, (B,))
+    return t.data_ptr()
+
+
+def cache_append(cache, k, v, table, start, *, rows=None, pos=None, sections=(0, 0, 0), freq=(), layout="halves",
+                 k_gain=None, eps=1e-6, stream: torch.cuda.Stream | None = None):
+    """Appends new rows' keys and values to a paged cache in 4-bit blocks
+    (wam_cache_append), in place: k, v [B, T, H, dh], float32 or bfloat16, any strides
+    with dh contiguous; row t of sequence b becomes token start[b] + t, which lies in
+    page table[b, token // page] (table int32 [B, n], start int32 [B]; an entry that is no
+    page drops its tokens).  rows int32 [B]: only the first rows[b] of a sequence count.
+    Keys first get the RMS norm with k_gain, float32 [dh], and the rotary positions pos
+    float32 [T, 3] or [B, T, 3], sections, freq and layout of rope.  Returns cache."""
+    index = _first(k, "cache_append: k", _REAL, 4)
+    B, T, H, dh = k.shape
+    _operand(v, "cache_append: v", (k.dtype,), index, k.shape)
+    held = _cache_values(cache, table, index, B, H, dh, "cache_append")
+    _operand(start, "cache_append: start", _I32, index, (B,))
+    count = _per_sequence(rows, "cache_append: rows", index, B)
+    if len(sections) != 3 or len(freq) != sum(sections) or getattr(freq, "ndim", 1) != 1:
+        raise WamError("cache_append: needs three sections and one frequency per pair")
+    ladder = np.ascontiguousarray(freq, np.float64) if isinstance(freq, np.ndarray) else array("d", freq)
+    at = ladder.ctypes.data if isinstance(ladder, np.ndarray) else ladder.buffer_info()[0]
+    pos_at = pos_stride = 0
+    if pos is not None:
+        each = isinstance(pos, torch.Tensor) and pos.dim() == 3  # sample has its own positions
+        _operand(pos, "cache_append: pos", _F32, index, (B, T, 3) if each else (T, 3))
+        if T > 1 and pos.stride(-2) != 3:
+            raise WamError("cache_append: rows of pos must be contiguous")
+        pos_at, pos_stride = pos.data_ptr(), pos.stride(0) if each else 0
+    if k_gain is not None:
+        _operand(k_gain, "cache_append: k_gain", _F32, index, (dh,))
+    a = _pack(_APPEND_ARGS, "cache_append", B, T, _TYPES[k.dtype], _choice(_LAYOUTS, layout, "cache_append: layout"),
+              *sections, *held, k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], start.data_ptr(), count,
+              pos_at, pos_stride, at, _ptr_or_0(k_gain), eps)
+    _call(abi.lib().wam_cache_append, a, index, stream, "wam_cache_append")
+    return cache
+
+
+def cache_attention(q, cache, table, lengths, *, rows=None, causal=False, scale=None, out=None, lse=None,
+                    stream: torch.cuda.Stream | None = None):
+    """Attention of new rows over a paged cache in 4-bit blocks (wam_cache_attention): q
+    [B, T, Hq, dh], float32 or bfloat16, any strides with dh contiguous, Hq a multiple of
+    the cache's heads; sequence b has lengths[b] tokens (int32 [B]) in the pages of
+    table[b] (int32 [B, n]; an entry that is no page leaves its tokens out).  causal: the
+    last tokens are the rows' own, and row t sees those up to its own.  rows int32 [B]:
+    only the first rows[b] of a sequence count, the others' results are 0, as are those
+    of rows that see no token.  scale: default 1 / sqrt(dh).  Returns out, of q's shape
+    and type; lse: a float32 [B, T, Hq] buffer for the logarithm of each row's sum."""
+    index = _first(q, "cache_attention: q", _REAL, 4)
+    B, T, Hq, dh = q.shape
+    held = _cache_values(cache, table, index, B, None, dh, "cache_attention")
+    _operand(lengths, "cache_attention: lengths", _I32, index, (B,))
+    count = _per_sequence(rows, "cache_attention: rows", index, B)
+    out = (_new(stream, torch.empty, q.shape, dtype=q.dtype, device=q.device) if out is None else
+           _operand(out, "cache_attention: out", (q.dtype,), index, q.shape))
+    lse_stride = _NO_HEADS
+    if lse is not None:
+        _operand(lse, "cache_attention: lse", _F32, index, (B, T, Hq))
+        lse_stride = lse.stride()
+    head = (B, T, Hq, _TYPES[q.dtype], int(bool(causal)), *held, q.data_ptr(), *q.stride()[:3], out.data_ptr(),
+            *out.stride()[:3], _ptr_or_0(lse), *lse_stride, lengths.data_ptr(), count,
+            1.0 / math.sqrt(dh) if scale is None and dh else scale)
+    lib = abi.lib()
+    a = _pack(_ATTENTION_ARGS, "cache_attention", *head, 0, 0)
+    need = lib.wam_cache_attention_workspace(a)
+    if need:
+        # freed to the call's own stream when this returns: later work there may take it
+        work = _new(stream, torch.empty, need, dtype=torch.uint8, device=q.device)
+        a = _pack(_ATTENTION_ARGS, "cache_attention", *head, work.data_ptr(), need)
+    _call(lib.wam_cache_attention, a, index, stream, "wam_cache_attention")
+    return out
 
 
 def probe_mfma_bf16(shape: int = 0, n_blocks: int = 1024, iters: int = 20000, device="cuda:0"):

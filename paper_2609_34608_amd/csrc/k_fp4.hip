@@ -54,85 +54,186 @@ __global__ __launch_bounds__(256) void dequantize_fp4_kernel(wam_dequantize_fp4_
 
 // ------------------------------------------------------------- appending to a cache
 constexpr int kAppendMaxPairs = 64;  // heads of at most 128
+constexpr int kAppendFewPairs = 32;  // arguments travel with every launch: a form for heads of up to 64
 template <int P>
 struct AppendParams {
   wam_cache_append_args a;
   int pairs, end0, end1, shift;
   int lanes;        // lanes of a head vector, a power of two >= dh / 8
   int rows_block;   // rows of a thread block
-  int heads_block;  // and heads
+  double inverse;   // 1 / dh
   double turns[P];  // revolutions per unit of position
 };
 
+// Sum over aligned groups of n lanes (4, 8 or 16), in every lane.
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)dpp<CTRL>((uint32_t)(u >> 32)) << 32 | dpp<CTRL>((uint32_t)u));
+}
 __device__ __forceinline__ double lanes_sum_d(double v, int n) {
-  for (int o = 1; o < n; o *= 2) v += __shfl_xor(v, o, 64);
+  v += dpp_d<0xb1>(v);
+  v += dpp_d<0x4e>(v);
+  if (n >= 8) v += dpp_d<0x141>(v);
+  if (n >= 16) v += dpp_d<0x140>(v);
   return v;
+}
+
+// cos and sin of the angles of a block's rows, [row][pair], into LDS.  The product with the
+// position is taken in revolutions, so that dropping the whole ones is exact.
+template <int P>
+__device__ __forceinline__ void append_turns(const AppendParams<P>& p, int row0, int rows, double2* turn) {
+  for (int i = threadIdx.x; i < rows * p.pairs; i += 256) {
+    const int row = row0 + i / p.pairs, j = i % p.pairs;
+    const float* pos = p.a.pos + row / p.a.T * p.a.pos_stride + row % p.a.T * 3;
+    double t = (double)pos[j < p.end0 ? 0 : j < p.end1 ? 1 : 2] * p.turns[j];
+    t -= rint(t);
+    double c, s;
+    sincospi(2.0 * t, &s, &c);
+    turn[i] = make_double2(c, s);
+  }
+}
+
+// Place of a row's token in its page, and the page: -1 where the row is dropped.
+template <int P>
+__device__ __forceinline__ int append_page(const AppendParams<P>& p, int b, int t, int& place) {
+  const wam_cache_append_args& a = p.a;
+  if (a.rows && t >= a.rows[b]) return -1;
+  const int64_t token = (int64_t)a.start[b] + t;
+  place = (int)(token & ((1 << p.shift) - 1));
+  if (token > INT32_MAX) return -1;
+  return page_of(a.table.entry + b * a.table.stride, a.table.width, p.shift, a.cache.pages, (int)token);
 }
 
 // A lane takes eight neighbouring values of a head vector, four lanes a block of it.
 // Keys are normed and turned in float64 and rounded to float32 once: a value next to a
 // border between two codes moves by a whole step, so with float32 arithmetic the codes
-// would hang on the order of its roundings.  The matrix pipe is idle and the vector
-// pipe does float64 at the rate of float32, so that costs little beside the loads.
-// A block's angles are computed once, in LDS, for all its heads; the other value of a
-// pair is loaded again (from the cache that has just delivered it) rather than
-// exchanged, which holds for any sections and layout.
-template <typename T, int P>
-__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams<P> p) {
-  extern __shared__ double2 turn[];  // [rows_block][pairs]: cos, sin
+// would hang on the order of its roundings.  The vector pipe does float64 at the rate of
+// float32, so that costs little beside the loads.  A block's angles are computed once, in
+// LDS; a thread keeps one row for all the heads it visits, with the products of its
+// cosines, sines and gains in registers.  The other values of its pairs are a load of
+// their own (a lane's eight are neighbours, so that a block of 32 lies in four lanes).
+// Heads are loaded one ahead of the arithmetic.
+template <typename T, bool PAIRS, int P>
+__global__ __launch_bounds__(256) void cache_append_units_kernel(AppendParams<P> p) {
+  extern __shared__ double2 turn[];
   const wam_cache_append_args& a = p.a;
   const wam_cache& ca = a.cache;
   const bool isk = blockIdx.z == 0;
-  const int rows = a.B * a.T, row0 = blockIdx.x * p.rows_block;
-  const int vectors = 256 / p.lanes;  // of the block at a time
-  const int slot = threadIdx.x / p.lanes, unit = threadIdx.x % p.lanes;
-  const int col = 8 * unit;
-  const int h0 = blockIdx.y * p.heads_block, heads = min(p.heads_block, ca.H - h0);
-  const int live_rows = min(p.rows_block, rows - row0);
+  const int rows = a.B * a.T, row0 = blockIdx.x * p.rows_block, live_rows = min(p.rows_block, rows - row0);
+  const int slot = threadIdx.x / p.lanes, unit = threadIdx.x % p.lanes, col = 8 * unit;
+  const int heads_par = 256 / p.lanes / p.rows_block;
+  const int row = row0 + slot / heads_par, b = row / a.T, t = row % a.T;
+  int h = blockIdx.y * heads_par + slot % heads_par;
+  const int step = gridDim.y * heads_par;
+  const bool mine = row < rows && col < ca.dh;  // idle lanes of 96 values take part in the exchanges
+  int place = 0;
+  const int page = row < rows ? append_page(p, b, t, place) : -1;
 
-  if (isk) {
-    for (int i = threadIdx.x; i < live_rows * p.pairs; i += 256) {
-      const int row = row0 + i / p.pairs, j = i % p.pairs;
-      const float* pos = a.pos + row / a.T * a.pos_stride + row % a.T * 3;
-      // in revolutions, so that dropping the whole ones is exact
-      double t = (double)pos[j < p.end0 ? 0 : j < p.end1 ? 1 : 2] * p.turns[j];
-      t -= rint(t);
-      double c, s;
-      sincospi(2.0 * t, &s, &c);
-      turn[i] = make_double2(c, s);
+  const T* x = static_cast<const T*>(isk ? a.k : a.v);
+  const int64_t* si = isk ? a.k_stride : a.v_stride;
+  if (mine) x += b * si[0] + t * si[1];
+  const bool turned = isk && col < 2 * p.pairs;
+  const int other = PAIRS || !turned ? col : col < p.pairs ? col + p.pairs : col - p.pairs;
+  Pack<T, 8> own{}, far{};
+  auto load = [&](int hh) __attribute__((always_inline)) {
+    if (mine && page >= 0 && hh < ca.H) {
+      own = *reinterpret_cast<const Pack<T, 8>*>(x + hh * si[2] + col);
+      if (!PAIRS && turned) far = *reinterpret_cast<const Pack<T, 8>*>(x + hh * si[2] + other);
     }
+  };
+  load(h);
+  double gc[8], gs[8];  // factors of the lane's own values and of the others
+  const bool normed = isk && a.k_gain;
+  if (isk) {
+    append_turns(p, row0, live_rows, turn);
     __syncthreads();
-  }
-  const double inv = 1.0 / (double)ca.dh;
-  for (int v = slot; v < live_rows * heads; v += vectors) {
-    const int r = v / heads, h = h0 + v % heads, row = row0 + r;
-    const int b = row / a.T, t = row % a.T;
-    if (a.rows && t >= a.rows[b]) continue;
-    const int64_t token = (int64_t)a.start[b] + t;
-    const int page = token > INT32_MAX ? -1 : page_of(a.table.entry + b * a.table.stride, a.table.width, p.shift, ca.pages, (int)token);
-    if (page < 0) continue;
-    const int64_t place = token & ((1 << p.shift) - 1);
-    float y[8];
-    const T* x = static_cast<const T*>(isk ? a.k : a.v) + (isk ? b * a.k_stride[0] + t * a.k_stride[1] + h * a.k_stride[2]
-                                                              : b * a.v_stride[0] + t * a.v_stride[1] + h * a.v_stride[2]);
-    const int n = col < ca.dh ? 8 : 0;
-    load_n(y, x + col, n);
-    if (isk && (p.pairs || a.k_gain)) {
-      double d[8], rs = 1.0;
-      if (a.k_gain) {
-        double ss = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss += (double)y[i] * (double)y[i];
-        rs = 1.0 / sqrt(lanes_sum_d(ss, p.lanes) * inv + a.eps);
+    for (int i = 0; i < 8; ++i) {
+      const int j = PAIRS ? 4 * unit + i / 2 : (col < p.pairs ? col : other) + i;
+      const bool first = PAIRS ? i % 2 == 0 : col < p.pairs;
+      const double2 cs = turned && mine ? turn[slot / heads_par * p.pairs + j] : make_double2(1.0, 0.0);
+      gc[i] = cs.x, gs[i] = first ? -cs.y : cs.y;
+      if (normed && mine) {
+        gc[i] *= (double)a.k_gain[col + i];
+        gs[i] *= (double)a.k_gain[PAIRS ? col + (i ^ 1) : other + i];
       }
+    }
+  }
+  const int64_t* so = isk ? ca.k_stride : ca.v_stride;
+  const int64_t* ss = isk ? ca.k_scale_stride : ca.v_scale_stride;
+  uint8_t* q = (isk ? ca.k : ca.v) + page * so[0] + place * so[1] + col / 2;
+  uint8_t* scale = (isk ? ca.k_scale : ca.v_scale) + page * ss[0] + place * ss[1] + col / kFp4Block;
+  for (int h0 = blockIdx.y * heads_par; h0 < ca.H; h0 += step, h += step) {
+    float y[8];
+    double z[8], w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = to_f32(own.v[i]);
+    if (isk && (p.pairs || normed)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        d[i] = (double)y[i] * rs;
-        if (a.k_gain && n) d[i] *= (double)a.k_gain[col + i];
+        z[i] = (double)y[i];
+        w[i] = (double)to_f32(PAIRS ? own.v[i ^ 1] : far.v[i]);
       }
+    }
+    load(h + step);  // the next head's while this one is turned
+    if (isk && (p.pairs || normed)) {
+      double rs = 1.0;
+      if (normed) {
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += z[i] * z[i];
+        rs = rsqrt(lanes_sum_d(mine ? sum : 0.0, p.lanes) * p.inverse + a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i)  // past the pairs: not plus 0, which would spread a NaN or an infinity
+        y[i] = (float)((turned ? z[i] * gc[i] + w[i] * gs[i] : z[i] * gc[i]) * rs);
+    }
+    const uint32_t byte = fp4_scale(quad_max(mine ? most_of(y) : 0));
+    if (!mine || page < 0 || h >= ca.H) continue;
+    *reinterpret_cast<uint32_t*>(q + h * so[2]) = pack_fp4(y, byte);
+    if (unit % 4 == 0) scale[h * ss[2]] = (uint8_t)byte;
+  }
+}
+
+// Sections of any number of pairs: value by value.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendParams<P> p) {
+  extern __shared__ double2 turn[];
+  const wam_cache_append_args& a = p.a;
+  const wam_cache& ca = a.cache;
+  const bool isk = blockIdx.z == 0;
+  const int rows = a.B * a.T, row0 = blockIdx.x * p.rows_block, live_rows = min(p.rows_block, rows - row0);
+  const int vectors = 256 / p.lanes;  // of the block at a time
+  const int slot = threadIdx.x / p.lanes, unit = threadIdx.x % p.lanes, col = 8 * unit;
+  if (isk) {
+    append_turns(p, row0, live_rows, turn);
+    __syncthreads();
+  }
+  for (int v = slot; v < live_rows * ca.H; v += vectors) {
+    const int r = v / ca.H, h = v % ca.H, row = row0 + r, b = row / a.T, t = row % a.T;
+    int place = 0;
+    const int page = append_page(p, b, t, place);
+    if (page < 0) continue;
+    float y[8];
+    const int64_t* si = isk ? a.k_stride : a.v_stride;
+    const T* x = static_cast<const T*>(isk ? a.k : a.v) + b * si[0] + t * si[1] + h * si[2];
+    const int n = col < ca.dh ? 8 : 0;
+    load_n(y, x + col, n);
+    if (isk) {
+      double d[8], rs = 1.0;
+      if (a.k_gain) {
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += (double)y[i] * (double)y[i];
+        rs = rsqrt(lanes_sum_d(sum, p.lanes) * p.inverse + a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = (double)y[i] * rs * (a.k_gain && n ? (double)a.k_gain[col + i] : 1.0);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int e = col + i;
+        y[i] = (float)d[i];
         if (e >= 2 * p.pairs || !n) continue;
         const bool pairs = a.layout == WAM_ROPE_PAIRS;
         const bool first = pairs ? e % 2 == 0 : e < p.pairs;
@@ -142,19 +243,23 @@ __global__ __launch_bounds__(256) void cache_append_kernel(AppendParams<P> p) {
         const double2 cs = turn[r * p.pairs + (pairs ? e / 2 : first ? e : partner)];
         y[i] = (float)(d[i] * cs.x + (first ? -o : o) * cs.y);
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (col + i >= 2 * p.pairs) y[i] = (float)d[i];
     }
     const uint32_t byte = fp4_scale(quad_max(most_of(y)));
     if (!n) continue;
-    const int64_t* st = isk ? ca.k_stride : ca.v_stride;
+    const int64_t* so = isk ? ca.k_stride : ca.v_stride;
     const int64_t* ss = isk ? ca.k_scale_stride : ca.v_scale_stride;
-    uint8_t* q = (isk ? ca.k : ca.v) + page * st[0] + place * st[1] + h * st[2];
+    uint8_t* q = (isk ? ca.k : ca.v) + page * so[0] + place * so[1] + h * so[2];
     *reinterpret_cast<uint32_t*>(q + col / 2) = pack_fp4(y, byte);
     if (unit % 4 == 0)
       ((isk ? ca.k_scale : ca.v_scale) + page * ss[0] + place * ss[1] + h * ss[2])[col / kFp4Block] = (uint8_t)byte;
   }
+}
+
+template <typename T, int P>
+void launch_append_type(const AppendParams<P>& p, dim3 grid, size_t lds, hipStream_t s) {
+  if (p.pairs % 8) launch_k(cache_append_kernel<T, P>, dim3(grid.x, 1, 2), 256, lds, s, p);
+  else if (p.a.layout == WAM_ROPE_PAIRS) launch_k(cache_append_units_kernel<T, true, P>, grid, 256, lds, s, p);
+  else launch_k(cache_append_units_kernel<T, false, P>, grid, 256, lds, s, p);
 }
 
 template <int P>
@@ -166,16 +271,20 @@ hipError_t launch_append(const wam_cache_append_args& a, int shift, hipStream_t 
   p.end1 = p.end0 + a.sections[1];
   p.pairs = p.end1 + a.sections[2];
   for (int i = 0; i < p.pairs; ++i) p.turns[i] = a.freq[i] * (0.5 / M_PI);
+  p.inverse = 1.0 / a.cache.dh;
   p.lanes = 4;
   while (p.lanes * 8 < a.cache.dh) p.lanes *= 2;
-  const int rows = a.B * a.T, H = a.cache.H;
-  // rows and heads of a block: all heads of a row share its angles
-  p.rows_block = std::min(rows, 8);
-  p.heads_block = H;
-  const dim3 grid((rows + p.rows_block - 1) / p.rows_block, (H + p.heads_block - 1) / p.heads_block, 2);
+  const int rows = a.B * a.T, H = a.cache.H, slots = 256 / p.lanes;
+  // eight rows a block, whose codes of a head lie side by side in its page; fewer where
+  // that leaves CUs without a block
+  p.rows_block = 8;
+  while (p.rows_block > 1 && (rows + p.rows_block - 1) / p.rows_block < 512) p.rows_block /= 2;
+  const int heads_par = slots / p.rows_block, head_blocks = (H + heads_par - 1) / heads_par;
+  const int row_blocks = (rows + p.rows_block - 1) / p.rows_block;
+  const dim3 grid(row_blocks, row_blocks >= 512 ? 1 : std::min(head_blocks, 65535), 2);
   const size_t lds = sizeof(double2) * p.rows_block * p.pairs;
-  if (a.dtype == WAM_BF16) launch_k(cache_append_kernel<bf16, P>, grid, 256, lds, s, p);
-  else launch_k(cache_append_kernel<float, P>, grid, 256, lds, s, p);
+  if (a.dtype == WAM_BF16) launch_append_type<bf16>(p, grid, lds, s);
+  else launch_append_type<float>(p, grid, lds, s);
   return hipGetLastError();
 }
 
@@ -301,7 +410,9 @@ int wam_cache_append(const wam_cache_append_args* a, void* hip_stream) {
   if (a->cache.pages == 0 || a->table.width == 0) return WAM_OK;  // no token has a page
   const int shift = page_shift(a->cache.page);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  if (launch_append<kAppendMaxPairs>(*a, shift, s) != hipSuccess)
+  const hipError_t e = pairs <= kAppendFewPairs ? launch_append<kAppendFewPairs>(*a, shift, s)
+                                                : launch_append<kAppendMaxPairs>(*a, shift, s);
+  if (e != hipSuccess)
     return noalloc_fail(WAM_E_HIP, "wam_cache_append: kernel launch failed");
   return WAM_OK;
 }

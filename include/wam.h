@@ -637,7 +637,7 @@ int wam_matmul_fp4(const wam_matmul_fp4_args *args, void *hip_stream);
 /* A cache of keys and values in 4-bit blocks: a pool of pages of `page` tokens (a power
  * of two, 16 to 4096) with H heads of dh values (32, 64, 96 or 128), i.e. dh / 2 bytes of
  * codes and dh / 32 scales a head, all contiguous; strides in bytes of page, token and
- * head, those of codes (and their base) multiples of 4.  A sequence has a row of
+ * head, those of codes (and their base) multiples of 4, those of tokens at most 2^26.  A sequence has a row of
  * table: its token t lies at place t % page of page table[b][t / page].  An entry
  * outside 0 .. pages - 1 stands for no page, and tokens past the table for none. */
 typedef struct {

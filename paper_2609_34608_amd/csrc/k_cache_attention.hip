@@ -78,19 +78,21 @@ struct Codes {
   uint8_t s[DB];
 };
 
+// q, scale: the first of the tokens (uniform); at, sat: the lane's place from there
 template <int DB>
-__device__ __forceinline__ void load_codes(Codes<DB>& c, const uint8_t* q, const uint8_t* scale, int lg) {
+__device__ __forceinline__ void load_codes(Codes<DB>& c, const uint8_t* q, const uint8_t* scale, uint32_t at,
+                                           uint32_t sat, int lg) {
   struct __attribute__((packed, aligned(4))) Words {
     uint32_t w[DB];
   };
-  const Words v = *reinterpret_cast<const Words*>(q + lg * DB * 4);
+  const Words v = *reinterpret_cast<const Words*>(q + at);
 #pragma unroll
   for (int i = 0; i < DB; ++i) c.w[i] = v.w[i];
   if constexpr (DB == 3) {  // a lane's words lie in two blocks
 #pragma unroll
-    for (int i = 0; i < DB; ++i) c.s[i] = scale[(lg * DB + i) / 4];
+    for (int i = 0; i < DB; ++i) c.s[i] = scale[sat + (uint32_t)(lg * DB + i) / 4];
   } else {
-    c.s[0] = scale[lg * DB / 4];
+    c.s[0] = scale[sat + (uint32_t)(lg * DB) / 4];
   }
 }
 template <int DB>
@@ -98,7 +100,7 @@ __device__ __forceinline__ uint32_t scale_of(const Codes<DB>& c, int i) { return
 
 // DB: blocks of a head; QT: tiles of 16 rows; NS: bf16 parts of q and of a probability
 template <int DB, int QT, int NS>
-__global__ __launch_bounds__(kWaves* kWave) void attend_kernel(AttendParams p) {
+__global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p) {
   typedef typename std::conditional<NS == 1, bf16, float>::type T;
   constexpr int DH = DB * 32, DT = DH / 16;
   constexpr int VROW = DH * 2 + 32;  // bytes of a token in LDS: the reads of 16 rows meet no bank twice
@@ -157,22 +159,32 @@ __global__ __launch_bounds__(kWaves* kWave) void attend_kernel(AttendParams p) {
     }
   }
 
+  // Pages of the wave's next 16 tiles, four groups of 16 tokens each, one a lane: a table
+  // that is read when its pages are needed costs a tile the latency of one more load.
   const int32_t* table = a.table.entry + b * a.table.stride;
-  const int64_t head_k = hk * ca.k_stride[2], head_ks = hk * ca.k_scale_stride[2];
-  const int64_t head_v = hk * ca.v_stride[2], head_vs = hk * ca.v_scale_stride[2];
+  auto pages_from = [&](int tile) __attribute__((always_inline)) {
+    const int64_t t = ((int64_t)tile + lane / 4 * kWaves) * kKeys + lane % 4 * 16;
+    return t < held ? page_of(table, a.table.width, p.shift, ca.pages, (int)t) : -1;
+  };
+  const uint8_t* head_k = ca.k + hk * ca.k_stride[2];
+  const uint8_t* head_v = ca.v + hk * ca.v_stride[2];
+  const uint8_t* head_ks = ca.k_scale + hk * ca.k_scale_stride[2];
+  const uint8_t* head_vs = ca.v_scale + hk * ca.v_scale_stride[2];
+  const uint32_t at_k = lr * (uint32_t)ca.k_stride[1] + lg * DB * 4, at_v = lr * (uint32_t)ca.v_stride[1] + lg * DB * 4;
+  const uint32_t at_ks = lr * (uint32_t)ca.k_scale_stride[1], at_vs = lr * (uint32_t)ca.v_scale_stride[1];
   Codes<DB> kc[4], vc[4];
-  bool there[4];  // the 16 tokens have a page
-  auto request = [&](int tile) __attribute__((always_inline)) {
+  uint32_t there = 0;  // bit g: the 16 tokens have a page
+  auto request = [&](int tile, int pages, int turn) __attribute__((always_inline)) {
+    there = 0;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int t = tile * kKeys + g * 16;
-      const int page = page_of(table, a.table.width, p.shift, ca.pages, t);
-      there[g] = page >= 0;
-      const int64_t pg = max(page, 0), place = (t & ((1 << p.shift) - 1)) + lr;
-      load_codes(kc[g], ca.k + pg * ca.k_stride[0] + place * ca.k_stride[1] + head_k,
-                 ca.k_scale + pg * ca.k_scale_stride[0] + place * ca.k_scale_stride[1] + head_ks, lg);
-      load_codes(vc[g], ca.v + pg * ca.v_stride[0] + place * ca.v_stride[1] + head_v,
-                 ca.v_scale + pg * ca.v_scale_stride[0] + place * ca.v_scale_stride[1] + head_vs, lg);
+      const int page = __builtin_amdgcn_readlane(pages, turn * 4 + g);
+      there |= page >= 0 ? 1u << g : 0u;
+      const int64_t pg = max(page, 0), place = (tile * kKeys + g * 16) & ((1 << p.shift) - 1);
+      load_codes(kc[g], head_k + (pg * ca.k_stride[0] + place * ca.k_stride[1]),
+                 head_ks + (pg * ca.k_scale_stride[0] + place * ca.k_scale_stride[1]), at_k, at_ks, lg);
+      load_codes(vc[g], head_v + (pg * ca.v_stride[0] + place * ca.v_stride[1]),
+                 head_vs + (pg * ca.v_scale_stride[0] + place * ca.v_scale_stride[1]), at_v, at_vs, lg);
     }
   };
 
@@ -207,19 +219,22 @@ __global__ __launch_bounds__(kWaves* kWave) void attend_kernel(AttendParams p) {
   };
 
   const int first = t_lo + wid;
-  if (first < t_hi) request(first);
+  int pages = -1, more = -1, turn = 0;
+  if (first < t_hi) {
+    pages = pages_from(first);
+    more = pages_from(first + 16 * kWaves);
+    request(first, pages, 0);
+  }
   for (int tile = first; tile < t_hi; tile += kWaves) {
     const int k0 = tile * kKeys;
-    const bool whole = k0 + kKeys <= least && there[0] && there[1] && there[2] && there[3];
-    bool has[4];
-#pragma unroll
-    for (int g = 0; g < 4; ++g) has[g] = there[g];
+    const uint32_t has = there;
+    const bool whole = k0 + kKeys <= least && has == 15;
     if (!whole) {
       // tokens that the sequence does not hold count as zeros, whatever lies there
       bool far = false;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const bool live = has[g] && k0 + g * 16 + lr < held;
+        const bool live = (has >> g & 1) && k0 + g * 16 + lr < held;
 #pragma unroll
         for (int s = 0; s < DB; ++s) {
           if (!live) vc[g].w[s] = 0, vc[g].s[s] = 0;
@@ -294,23 +309,34 @@ __global__ __launch_bounds__(kWaves* kWave) void attend_kernel(AttendParams p) {
             st[i][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][s][n], st[i][g], 0, 0, 0);
       }
     }
-    if (tile + kWaves < t_hi) request(tile + kWaves);
+    if (tile + kWaves < t_hi) {
+      if (++turn == 16) {
+        turn = 0, pages = more;
+        more = pages_from(tile + 17 * kWaves);
+      }
+      request(tile + kWaves, pages, turn);
+    }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (!((has >> g & 1) && k0 + g * 16 + 4 * lg + r < vis[i])) st[i][g][r] = -INFINITY;
+    }
     bf16x8 pf[QT][2][NS];
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-      float top = -INFINITY;
+      float top = st[i][0][0];
 #pragma unroll
       for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float x = st[i][g][r] * p.log2_scale;
-          if (!whole) x = has[g] && k0 + g * 16 + 4 * lg + r < vis[i] ? x : -INFINITY;
-          st[i][g][r] = x;
-          top = fmaxf(top, x);
-        }
+        for (int r = 0; r < 4; ++r) top = fmaxf(top, st[i][g][r]);
+      top *= p.log2_scale;
       if (__any(top > m[i] + kSlack)) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -325,7 +351,7 @@ __global__ __launch_bounds__(kWaves* kWave) void attend_kernel(AttendParams p) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           bf16 part[NS];
-          split<NS>(__builtin_amdgcn_exp2f(st[i][g][r] - m[i]), part);
+          split<NS>(__builtin_amdgcn_exp2f(fmaf(st[i][g][r], p.log2_scale, -m[i])), part);
 #pragma unroll
           for (int n = 0; n < NS; ++n) pf[i][g / 2][n][g % 2 * 4 + r] = part[n];
         }
@@ -409,7 +435,9 @@ __global__ __launch_bounds__(kWaves* kWave) void attend_kernel(AttendParams p) {
   }
 }
 
-// Joins the parts of a row, in the order of the splits: a wave a row.
+// Joins the parts of a row, a wave a row: a lane takes four values of dh in every G-th
+// split, so that the loads of G splits go out together, and the lanes of a value add up
+// in a fixed order.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
   const wam_cache_attention_args& a = p.a;
@@ -418,25 +446,38 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
   if (i >= (int64_t)a.B * a.cache.H * R) return;
   const int64_t bh = i / R;
   const int r = (int)(i % R), b = (int)(bh / a.cache.H), hk = (int)(bh % a.cache.H);
-  const float* ws = static_cast<const float*>(a.workspace);
-  const float* ml = ws + (int64_t)a.B * a.cache.H * p.splits * R * DH;
-  auto at = [&](int s) { return (bh * p.splits + s) * R + r; };
+  const float* ws = static_cast<const float*>(a.workspace) + (bh * p.splits * R + r) * DH;
+  const float* ml = static_cast<const float*>(a.workspace) + (int64_t)a.B * a.cache.H * p.splits * R * DH +
+                    (bh * p.splits * R + r) * 2;
   float top = kNone;
-  for (int s = 0; s < p.splits; ++s) top = fmaxf(top, ml[at(s) * 2]);
-  float total = 0.f, x[2] = {0.f, 0.f};
-  for (int s = 0; s < p.splits; ++s) {
-    const float f = __builtin_amdgcn_exp2f(ml[at(s) * 2] - top);
-    total += ml[at(s) * 2 + 1] * f;
+  for (int s = lane; s < p.splits; s += kWave) top = fmaxf(top, ml[(int64_t)s * R * 2]);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (lane + j * kWave < DH) x[j] += ws[at(s) * DH + lane + j * kWave] * f;
+  for (int o = 1; o < kWave; o *= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
+  const int lanes = DH <= 64 ? DH / 4 <= 8 ? 8 : 16 : 32;  // of a row's values, a power of two
+  const int at = lane % lanes, from = lane / lanes, G = kWave / lanes;
+  const bool mine = 4 * at < DH;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  float total = 0.f;
+#pragma unroll 4
+  for (int s = from; s < p.splits; s += G) {
+    const int64_t row = (int64_t)s * R;
+    const float f = __builtin_amdgcn_exp2f(ml[row * 2] - top);
+    total += ml[row * 2 + 1] * f;
+    if (mine) x += *reinterpret_cast<const f32x4*>(ws + row * DH + 4 * at) * f;
   }
+  for (int o = lanes; o < kWave; o *= 2) {
+    total += __shfl_xor(total, o, 64);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] += __shfl_xor(x[k], o, 64);
+  }
+  if (from) return;
   const int t = r / p.group, h = hk * p.group + r % p.group;
   const float inv = 1.0f / total;
   T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + t * a.out_stride[1] + h * a.out_stride[2];
+  Pack<T, 4> w;
 #pragma unroll
-  for (int j = 0; j < 2; ++j)
-    if (lane + j * kWave < DH) out[lane + j * kWave] = static_cast<T>(total == 0.f ? 0.f : x[j] * inv);
+  for (int k = 0; k < 4; ++k) w.v[k] = static_cast<T>(total == 0.f ? 0.f : x[k] * inv);
+  if (mine) *reinterpret_cast<Pack<T, 4>*>(out + 4 * at) = w;
   if (a.lse && lane == 0)
     a.lse[b * a.lse_stride[0] + t * a.lse_stride[1] + h * a.lse_stride[2]] =
         total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;

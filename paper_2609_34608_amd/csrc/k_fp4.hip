@@ -319,6 +319,9 @@ int check_cache(const wam_cache& c, const wam_page_table& t, bool written, bool 
     return fail(WAM_E_ARG, "strides must be >= 0");
   for (int i = 0; i < 3; ++i)
     if (c.k_stride[i] % 4 || c.v_stride[i] % 4) return fail(WAM_E_ARG, "strides of codes must be multiples of 4");
+  const int64_t near = (int64_t)1 << 26;  // offsets of 16 tokens in 32 bits
+  if (c.k_stride[1] > near || c.v_stride[1] > near || c.k_scale_stride[1] > near || c.v_scale_stride[1] > near)
+    return fail(WAM_E_SHAPE, "tokens of a page must be at most 2^26 bytes apart");
   const int64_t size[3] = {c.pages, c.page, c.H};
   if (written && (!distinct(c.k_stride, size, 3, c.dh / 2) || !distinct(c.v_stride, size, 3, c.dh / 2) ||
                   !distinct(c.k_scale_stride, size, 3, c.dh / kFp4Block) ||

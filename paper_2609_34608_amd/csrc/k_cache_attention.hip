@@ -71,6 +71,8 @@ __device__ __forceinline__ void split(float x, bf16 (&part)[NS]) {
   }
 }
 
+typedef __attribute__((address_space(1))) const uint8_t global_byte;
+
 // Codes and scales of 16 tokens: lane (r, g) has the words g DB .. + DB - 1 of token r
 template <int DB>
 struct Codes {
@@ -80,14 +82,17 @@ struct Codes {
 
 // q, scale: the first of the tokens (uniform); at, sat: the lane's place from there
 template <int DB>
-__device__ __forceinline__ void load_codes(Codes<DB>& c, const uint8_t* q, const uint8_t* scale, uint32_t at,
+__device__ __forceinline__ void load_codes(Codes<DB>& c, const global_byte* q, const global_byte* scale, uint32_t at,
                                            uint32_t sat, int lg) {
-  struct __attribute__((packed, aligned(4))) Words {
-    uint32_t w[DB];
-  };
-  const Words v = *reinterpret_cast<const Words*>(q + at);
+  typedef uint32_t words __attribute__((ext_vector_type(DB), aligned(4)));
+  typedef __attribute__((address_space(1))) const words global_words;
+  if constexpr (DB == 1) {
+    c.w[0] = *reinterpret_cast<__attribute__((address_space(1))) const uint32_t*>(q + at);
+  } else {
+    const words v = *reinterpret_cast<global_words*>(q + at);
 #pragma unroll
-  for (int i = 0; i < DB; ++i) c.w[i] = v.w[i];
+    for (int i = 0; i < DB; ++i) c.w[i] = v[i];
+  }
   if constexpr (DB == 3) {  // a lane's words lie in two blocks
 #pragma unroll
     for (int i = 0; i < DB; ++i) c.s[i] = scale[sat + (uint32_t)(lg * DB + i) / 4];
@@ -159,32 +164,41 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     }
   }
 
-  // Pages of the wave's next 16 tiles, four groups of 16 tokens each, one a lane: a table
-  // that is read when its pages are needed costs a tile the latency of one more load.
+  // Where the groups of 16 tokens of the wave's next 16 tiles lie, one a lane: a table that
+  // is read when its pages are needed costs a tile the latency of one more load, and
+  // addresses that every tile works out anew cost it 200 scalar instructions.
   const int32_t* table = a.table.entry + b * a.table.stride;
+  auto token_of = [&](int tile) { return ((int64_t)tile + lane / 4 * kWaves) * kKeys + lane % 4 * 16; };
   auto pages_from = [&](int tile) __attribute__((always_inline)) {
-    const int64_t t = ((int64_t)tile + lane / 4 * kWaves) * kKeys + lane % 4 * 16;
+    const int64_t t = token_of(tile);
     return t < held ? page_of(table, a.table.width, p.shift, ca.pages, (int)t) : -1;
   };
-  const uint8_t* head_k = ca.k + hk * ca.k_stride[2];
-  const uint8_t* head_v = ca.v + hk * ca.v_stride[2];
-  const uint8_t* head_ks = ca.k_scale + hk * ca.k_scale_stride[2];
-  const uint8_t* head_vs = ca.v_scale + hk * ca.v_scale_stride[2];
+  const uint8_t *group_k, *group_ks, *group_v, *group_vs;
+  uint64_t have = 0;  // lanes whose tokens have a page
+  auto place_groups = [&](int tile, int page) __attribute__((always_inline)) {
+    have = __ballot(page >= 0);
+    const int64_t pg = max(page, 0), place = token_of(tile) & ((1 << p.shift) - 1);
+    group_k = ca.k + (pg * ca.k_stride[0] + place * ca.k_stride[1] + hk * ca.k_stride[2]);
+    group_ks = ca.k_scale + (pg * ca.k_scale_stride[0] + place * ca.k_scale_stride[1] + hk * ca.k_scale_stride[2]);
+    group_v = ca.v + (pg * ca.v_stride[0] + place * ca.v_stride[1] + hk * ca.v_stride[2]);
+    group_vs = ca.v_scale + (pg * ca.v_scale_stride[0] + place * ca.v_scale_stride[1] + hk * ca.v_scale_stride[2]);
+  };
   const uint32_t at_k = lr * (uint32_t)ca.k_stride[1] + lg * DB * 4, at_v = lr * (uint32_t)ca.v_stride[1] + lg * DB * 4;
   const uint32_t at_ks = lr * (uint32_t)ca.k_scale_stride[1], at_vs = lr * (uint32_t)ca.v_scale_stride[1];
   Codes<DB> kc[4], vc[4];
   uint32_t there = 0;  // bit g: the 16 tokens have a page
-  auto request = [&](int tile, int pages, int turn) __attribute__((always_inline)) {
-    there = 0;
+  auto request = [&](int turn) __attribute__((always_inline)) {
+    auto of = [&](const uint8_t* x, int g) __attribute__((always_inline)) {
+      const uint64_t u = reinterpret_cast<uint64_t>(x);
+      const uint32_t lo = __builtin_amdgcn_readlane((int)u, turn * 4 + g);
+      const uint32_t hi = __builtin_amdgcn_readlane((int)(u >> 32), turn * 4 + g);
+      return reinterpret_cast<const global_byte*>((uint64_t)hi << 32 | lo);
+    };
+    there = (uint32_t)(have >> (turn * 4)) & 15;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int page = __builtin_amdgcn_readlane(pages, turn * 4 + g);
-      there |= page >= 0 ? 1u << g : 0u;
-      const int64_t pg = max(page, 0), place = (tile * kKeys + g * 16) & ((1 << p.shift) - 1);
-      load_codes(kc[g], head_k + (pg * ca.k_stride[0] + place * ca.k_stride[1]),
-                 head_ks + (pg * ca.k_scale_stride[0] + place * ca.k_scale_stride[1]), at_k, at_ks, lg);
-      load_codes(vc[g], head_v + (pg * ca.v_stride[0] + place * ca.v_stride[1]),
-                 head_vs + (pg * ca.v_scale_stride[0] + place * ca.v_scale_stride[1]), at_v, at_vs, lg);
+      load_codes(kc[g], of(group_k, g), of(group_ks, g), at_k, at_ks, lg);
+      load_codes(vc[g], of(group_v, g), of(group_vs, g), at_v, at_vs, lg);
     }
   };
 
@@ -201,29 +215,25 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     for (int j = 0; j < DT; ++j) o[i][j] = zero;
   }
   uint8_t* own = vt[wid];
-  // fn(j, c, V^T of dims 16 j .. + 15 and the tokens of score tiles 2 c, 2 c + 1); lane s of
-  // a group reads dims 4 (s % 4) .. + 3 of token s / 4 of its four
-  auto for_dims = [&](auto fn) __attribute__((always_inline)) {
-    const uint8_t* from = own + (4 * lg + lr / 4) * VROW + lr % 4 * 8;
-    static_for<DT>([&](auto J) __attribute__((always_inline)) {
-      static_for<2>([&](auto C) __attribute__((always_inline)) {
-        const uint8_t* at = from + 2 * decltype(C)::value * 16 * VROW + decltype(J)::value * 32;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * VROW));
-        bf16x8 vf;
-        __builtin_memcpy(&vf, &lo, 8);
-        __builtin_memcpy(reinterpret_cast<char*>(&vf) + 8, &hi, 8);
-        fn(J, C, vf);
-      });
-    });
+  // V^T of dims 16 J .. + 15 and the tokens of score tiles 2 C, 2 C + 1; lane s of a group
+  // reads dims 4 (s % 4) .. + 3 of token s / 4 of its four
+  const uint8_t* from = own + (4 * lg + lr / 4) * VROW + lr % 4 * 8;
+  auto values = [&](auto J, auto C) __attribute__((always_inline)) {
+    const uint8_t* at = from + 2 * decltype(C)::value * 16 * VROW + decltype(J)::value * 32;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 16 * VROW));
+    bf16x8 vf;
+    __builtin_memcpy(&vf, &lo, 8);
+    __builtin_memcpy(reinterpret_cast<char*>(&vf) + 8, &hi, 8);
+    return vf;
   };
 
   const int first = t_lo + wid;
-  int pages = -1, more = -1, turn = 0;
+  int more = -1, turn = 0;
   if (first < t_hi) {
-    pages = pages_from(first);
+    place_groups(first, pages_from(first));
     more = pages_from(first + 16 * kWaves);
-    request(first, pages, 0);
+    request(0);
   }
   for (int tile = first; tile < t_hi; tile += kWaves) {
     const int k0 = tile * kKeys;
@@ -274,11 +284,12 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
 #pragma unroll
             for (int r = 0; r < 4; ++r)
               sees[i][g / 2][g % 2 * 4 + r] = (bf16)(k0 + g * 16 + 4 * lg + r < vis[i] ? 1.f : 0.f);
-        for_dims([&](auto J, auto C, const bf16x8& vf) __attribute__((always_inline)) {
-          constexpr int j = decltype(J)::value, c = decltype(C)::value;
+        static_for<2 * DT>([&](auto N) __attribute__((always_inline)) {
+          constexpr int j = decltype(N)::value / 2, c = decltype(N)::value % 2;
+          const bf16x8 odd = values(std::integral_constant<int, j>{}, std::integral_constant<int, c>{});
 #pragma unroll
           for (int i = 0; i < QT; ++i) {
-            const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, sees[i][c], zero, 0, 0, 0);
+            const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, sees[i][c], zero, 0, 0, 0);
 #pragma unroll
             for (int r = 0; r < 4; ++r)
               if (n[r] > 0.f) o[i][j][r] = NAN;
@@ -311,10 +322,11 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     }
     if (tile + kWaves < t_hi) {
       if (++turn == 16) {
-        turn = 0, pages = more;
+        turn = 0;
+        place_groups(tile + kWaves, more);
         more = pages_from(tile + 17 * kWaves);
       }
-      request(tile + kWaves, pages, turn);
+      request(turn);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -328,46 +340,66 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
           for (int r = 0; r < 4; ++r)
             if (!((has >> g & 1) && k0 + g * 16 + 4 * lg + r < vis[i])) st[i][g][r] = -INFINITY;
     }
-    bf16x8 pf[QT][2][NS];
+    float top[QT];
+    bool grown = false;
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-      float top = st[i][0][0];
+      top[i] = st[i][0][0];
 #pragma unroll
       for (int g = 0; g < 4; ++g)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) top = fmaxf(top, st[i][g][r]);
-      top *= p.log2_scale;
-      if (__any(top > m[i] + kSlack)) {
-        top = fmaxf(top, __shfl_xor(top, 16, 64));
-        top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float to = fmaxf(m[i], top), f = __builtin_amdgcn_exp2f(m[i] - to);
+        for (int r = 0; r < 4; ++r) top[i] = fmaxf(top[i], st[i][g][r]);
+      top[i] *= p.log2_scale;
+      grown |= top[i] > m[i] + kSlack;
+    }
+    if (__any(grown)) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i) {
+        top[i] = fmaxf(top[i], __shfl_xor(top[i], 16, 64));
+        top[i] = fmaxf(top[i], __shfl_xor(top[i], 32, 64));
+        const float to = top[i] > m[i] + kSlack ? top[i] : m[i], f = __builtin_amdgcn_exp2f(m[i] - to);
         m[i] = to;
         l[i] *= f;
 #pragma unroll
         for (int j = 0; j < DT; ++j) o[i][j] *= f;
       }
+    }
+    // Half of the tile's tokens at a time, so that V^T of that half stays in registers for
+    // all row tiles; the exponentials of the next row tile run between the matrix
+    // instructions of this one.
+    bf16x8 pf[2][NS], vf[DT];
+    auto exponentials = [&](auto N) __attribute__((always_inline)) {
+      constexpr int c = decltype(N)::value / QT, i = decltype(N)::value % QT;
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
+      for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           bf16 part[NS];
-          split<NS>(__builtin_amdgcn_exp2f(fmaf(st[i][g][r], p.log2_scale, -m[i])), part);
+          split<NS>(__builtin_amdgcn_exp2f(fmaf(st[i][2 * c + g][r], p.log2_scale, -m[i])), part);
 #pragma unroll
-          for (int n = 0; n < NS; ++n) pf[i][g / 2][n][g % 2 * 4 + r] = part[n];
+          for (int n = 0; n < NS; ++n) pf[decltype(N)::value & 1][n][g * 4 + r] = part[n];
         }
+    };
+    exponentials(std::integral_constant<int, 0>{});
+    static_for<2 * QT>([&](auto N) __attribute__((always_inline)) {
+      constexpr int n = decltype(N)::value, c = n / QT, i = n % QT;
+      if constexpr (i == 0)
+        static_for<DT>([&](auto J) __attribute__((always_inline)) { vf[decltype(J)::value] = values(J, std::integral_constant<int, c>{}); });
+      if constexpr (n + 1 < 2 * QT) exponentials(std::integral_constant<int, n + 1>{});
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
+      for (int k = 0; k < NS; ++k) {
+        l[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[n & 1][k], l[i], 0, 0, 0);
 #pragma unroll
-        for (int n = 0; n < NS; ++n)
-          l[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[i][c][n], l[i], 0, 0, 0);
-    }
-    for_dims([&](auto J, auto C, const bf16x8& vf) __attribute__((always_inline)) {
-      constexpr int j = decltype(J)::value, c = decltype(C)::value;
+        for (int j = 0; j < DT; ++j)
+          o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[j], pf[n & 1][k], o[i][j], 0, 0, 0);
+      }
+      if constexpr (NS == 1 && n + 1 < 2 * QT) {
 #pragma unroll
-      for (int i = 0; i < QT; ++i)
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-          o[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[i][c][n], o[i][j], 0, 0, 0);
+        for (int k = 0; k <= DT; ++k) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);              // one MFMA
+          __builtin_amdgcn_sched_group_barrier(0x2, 20 / (DT + 1), 0);  // and its share of the VALU
+        }
+      }
     });
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();

@@ -54,11 +54,31 @@ struct AttendParams {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-// The logical block of a grid of n blocks: each XCD (workgroups go to them round-robin)
-// takes a contiguous range, so that the blocks of a head share an L2.
-__device__ __forceinline__ int xcd_block(int i, int n) {
-  const int per = n / 8, rem = n % 8, x = i % 8;
-  return x * per + min(x, rem) + i / 8;
+// Which block of rows, part of the tokens, key head and sequence a workgroup takes.
+// Workgroups go to the 8 XCDs round-robin.  Where several blocks read the tokens of a
+// (sequence, key head), that pair's blocks go to one XCD, whose L2 they share, and the
+// pairs round; the pairs that 8 does not divide go to ranges of blocks.  Otherwise
+// neighbours in the grid are the parts of one pair, so that long sequences burden all
+// XCDs alike.
+struct BlockAt {
+  int rb, split, pair;
+};
+__device__ __forceinline__ BlockAt block_at(int i, int pairs, int row_blocks, int splits) {
+  const int each = row_blocks * splits;
+  int pair, k;
+  if (row_blocks == 1) {
+    pair = i / each, k = i % each;
+  } else {
+    const int x = i % 8, j = i / 8, whole = pairs / 8 * each;
+    if (j < whole) {
+      pair = j / each * 8 + x, k = j % each;
+    } else {
+      const int n = pairs % 8 * each, per = n / 8, rem = n % 8;
+      const int at = x * per + min(x, rem) + j - whole;
+      pair = pairs / 8 * 8 + at / each, k = at % each;
+    }
+  }
+  return {k / splits, k % splits, pair};
 }
 
 // bf16 parts of a float32: the first alone, or three that add up to it
@@ -116,12 +136,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
   const wam_cache& ca = a.cache;
   const int lane = threadIdx.x % kWave, wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lr = lane % 16, lg = lane / 16;
-  int id = xcd_block(blockIdx.x, gridDim.x);
-  const int split_at = id % p.splits;
-  id /= p.splits;
-  const int rb = id % p.row_blocks;
-  id /= p.row_blocks;
-  const int hk = id % ca.H, b = id / ca.H;
+  const BlockAt id = block_at(blockIdx.x, a.B * ca.H, p.row_blocks, p.splits);
+  const int rb = id.rb, split_at = id.split, hk = id.pair % ca.H, b = id.pair / ca.H;
 
   const int R = p.group * a.T, r0 = rb * QT * 16;
   const int rows = a.rows ? min(max(a.rows[b], 0), a.T) : a.T;
@@ -516,6 +532,8 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
 }
 
 // Tiles of 16 rows a block takes, and over how many blocks a sequence's tokens go.
+constexpr int64_t kSlots = 512;  // blocks that the chip holds at once
+constexpr int kPartTiles = 24;   // what a block costs beside its tiles, in tiles
 struct AttendPlan {
   int qt, row_blocks, splits;
 };
@@ -529,9 +547,18 @@ AttendPlan plan_attend(const wam_cache_attention_args& a) {
   pl.row_blocks = (int)((R + pl.qt * 16 - 1) / (pl.qt * 16));
   const int64_t blocks = (int64_t)a.B * a.cache.H * pl.row_blocks;
   const int64_t tiles = ((int64_t)a.table.width * a.cache.page + kKeys - 1) / kKeys;
-  // about four blocks a CU, each wave with two tiles at least
-  const int64_t want = (1024 + blocks - 1) / blocks;
-  pl.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want, tiles / (2 * kWaves)));
+  // Two blocks a CU at once: as many parts as make the rounds of those shortest, each wave
+  // with two tiles at least (64 rows of 24 heads over 101760 tokens in 1032 blocks, three
+  // rounds: 88 us; in 504, one: 71).
+  pl.splits = 1;
+  if (blocks < 4 * kSlots) {
+    double best = INFINITY;
+    const int64_t top = std::min<int64_t>(tiles / (2 * kWaves), 2 * kSlots / blocks);
+    for (int64_t s = 1; s <= std::max<int64_t>(top, 1); ++s) {
+      const double cost = (double)((blocks * s + kSlots - 1) / kSlots) * ((double)tiles / (double)s + kPartTiles);
+      if (cost < best) best = cost, pl.splits = (int)s;
+    }
+  }
   return pl;
 }
 

@@ -123,6 +123,27 @@ __device__ __forceinline__ void load_codes(Codes<DB>& c, const global_byte* q, c
 template <int DB>
 __device__ __forceinline__ uint32_t scale_of(const Codes<DB>& c, int i) { return DB == 3 ? c.s[i] : c.s[0]; }
 
+// A probability of zero does not keep a NaN or an infinity of a token that a row does not
+// see out of its sums.  As rows see the first tokens, it is enough to know of each dim the first
+// token with such a value, for the rows that see it, and to put zeros in their place.  Rare:
+// called where a scale may pass the bf16 range.
+template <int DB>
+__device__ __forceinline__ void drop_far(Codes<DB>& v, int token, int lg, int* first) {
+#pragma unroll
+  for (int s = 0; s < DB; ++s) {
+    const bf16x8 x = fp4_to_bf16(v.w[s], fp4_scale_operand(scale_of(v, s)));
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!(fabsf((float)x[e]) < INFINITY)) {
+        atomicMin(first + (lg * DB + s) * 8 + e, token);
+        v.w[s] &= ~(0xfu << (4 * e));
+      }
+  }
+#pragma unroll
+  for (int s = 0; s < DB; ++s)
+    if (v.s[s] == kFp4NaN) v.s[s] = 0;
+}
+
 // DB: blocks of a head; QT: tiles of 16 rows; NS: bf16 parts of q and of a probability
 template <int DB, int QT, int NS>
 __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p) {
@@ -131,6 +152,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
   constexpr int VROW = DH * 2 + 32;  // bytes of a token in LDS: the reads of 16 rows meet no bank twice
   __shared__ __attribute__((aligned(64))) uint8_t vt[kWaves][kKeys * VROW];
   __shared__ float part_m[kWaves][QT * 16], part_l[kWaves][QT * 16];
+  __shared__ int odd[DH];  // token that is the first without a finite value, by dim
 
   const wam_cache_attention_args& a = p.a;
   const wam_cache& ca = a.cache;
@@ -244,6 +266,10 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     return vf;
   };
 
+  if (a.causal) {
+    if (threadIdx.x < DH) odd[threadIdx.x] = INT32_MAX;
+    __syncthreads();
+  }
   const int first = t_lo + wid;
   int more = -1, turn = 0;
   if (first < t_hi) {
@@ -257,62 +283,23 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     const bool whole = k0 + kKeys <= least && has == 15;
     if (!whole) {
       // tokens that the sequence does not hold count as zeros, whatever lies there
-      bool far = false;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const bool live = (has >> g & 1) && k0 + g * 16 + lr < held;
 #pragma unroll
-        for (int s = 0; s < DB; ++s) {
+        for (int s = 0; s < DB; ++s)
           if (!live) vc[g].w[s] = 0, vc[g].s[s] = 0;
-          far |= scale_of(vc[g], s) >= kFar;
-        }
       }
-      if (a.causal && __any(far)) {
-        // A probability of zero does not keep a NaN of a later token out of a sum.  Rare:
-        // count such values by dim among the tokens that a row sees, then drop them.
+    }
+    if (a.causal) {
+      bool far = false;
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+      for (int g = 0; g < 4; ++g)
 #pragma unroll
-          for (int s = 0; s < DB; ++s) {
-            const bf16x8 v = fp4_to_bf16(vc[g].w[s], fp4_scale_operand(scale_of(vc[g], s)));
-            bf16x8 odd;
+        for (int s = 0; s < DB; ++s) far |= scale_of(vc[g], s) >= kFar;
+      if (__any(far)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const bool is = !(fabsf((float)v[e]) < INFINITY);
-              odd[e] = (bf16)(is ? 1.f : 0.f);
-              if (is) vc[g].w[s] &= ~(0xfu << (4 * e));
-            }
-            *reinterpret_cast<bf16x8*>(own + (g * 16 + lr) * VROW + (lg * DB + s) * 16) = odd;
-            if (scale_of(vc[g], s) == kFp4NaN) vc[g].w[s] = 0;
-          }
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-#pragma unroll
-          for (int s = 0; s < DB; ++s)
-            if (vc[g].s[s] == kFp4NaN) vc[g].s[s] = 0;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        bf16x8 sees[QT][2];
-#pragma unroll
-        for (int i = 0; i < QT; ++i)
-#pragma unroll
-          for (int g = 0; g < 4; ++g)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              sees[i][g / 2][g % 2 * 4 + r] = (bf16)(k0 + g * 16 + 4 * lg + r < vis[i] ? 1.f : 0.f);
-        static_for<2 * DT>([&](auto N) __attribute__((always_inline)) {
-          constexpr int j = decltype(N)::value / 2, c = decltype(N)::value % 2;
-          const bf16x8 odd = values(std::integral_constant<int, j>{}, std::integral_constant<int, c>{});
-#pragma unroll
-          for (int i = 0; i < QT; ++i) {
-            const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, sees[i][c], zero, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (n[r] > 0.f) o[i][j][r] = NAN;
-          }
-        });
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
+        for (int g = 0; g < 4; ++g) drop_far(vc[g], k0 + g * 16 + lr, lg, odd);
       }
     }
 #pragma unroll
@@ -459,6 +446,12 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
         top = fmaxf(top, part_m[w][i * 16 + row]);
       }
       if (r >= R) continue;
+      if (a.causal) {
+        const int sees = tokens_seen(held, length, true, rows, r / p.group);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (sees > odd[d + k]) sum[k] = NAN;
+      }
       if (p.splits > 1) {
         const int64_t at = (((int64_t)b * ca.H + hk) * p.splits + split_at) * R + r;
         float* ws = static_cast<float*>(a.workspace);

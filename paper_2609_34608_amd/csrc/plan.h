@@ -128,16 +128,21 @@ int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K, Fp8Result result = 
 }
 
 // ---------------------------------------------------------------- 4-bit products
-// Tiles of gemm_fp4.h and their cost, a stage being 256 of K.
+// Tiles of gemm_fp4.h and their cost, a stage being 256 of K (bk in values).  Least-squares
+// fits to 61 sizes (1 to 10176 rows, N 512 to 6144, K 768 to 6144) on one MI355X, standard
+// deviation 9-13%; the choice is 1.7% slower than the fastest of 15 configurations on
+// average (14% at worst).  A stage has half the bytes of the 8-bit one and a quarter of its
+// matrix cycles, so what a tile costs beside its stages weighs more and two blocks a CU
+// gain: with the 8-bit products' tiles and constants the choice was 3.7% slower on average.
 constexpr TileCfg kFp4Cfgs[] = {
-    {256, 256, 2, 4, 2, 256, 1, {1.27f}, {6.01f}},
-    {192, 256, 2, 4, 2, 256, 1, {1.08f}, {5.01f}},
-    {128, 256, 2, 4, 3, 256, 1, {0.77f}, {4.60f}},
-    {160, 128, 2, 2, 2, 256, 2, {0.63f, 1.14f}, {3.97f, 4.92f}},
-    {64, 128, 2, 2, 2, 256, 3, {0.42f, 0.59f, 0.95f}, {2.86f, 3.44f, 2.65f}},
-    {96, 64, 2, 2, 3, 256, 2, {0.30f, 0.54f}, {2.90f, 2.11f}},
-    {64, 64, 2, 2, 3, 256, 3, {0.24f, 0.38f, 0.62f}, {2.83f, 3.11f, 1.54f}},
-    {32, 32, 2, 2, 4, 256, 4, {0.15f, 0.18f, 0.26f, 0.36f}, {2.56f, 2.70f, 3.09f, 1.26f}},
+    {256, 256, 2, 4, 2, 256, 1, {1.55f}, {5.34f}},
+    {192, 256, 2, 4, 2, 256, 1, {1.32f}, {4.34f}},
+    {160, 128, 2, 2, 2, 256, 2, {0.82f, 1.29f}, {3.79f, 4.39f}},
+    {128, 128, 2, 2, 2, 256, 2, {0.73f, 1.14f}, {3.27f, 3.50f}},
+    {96, 64, 2, 2, 3, 256, 2, {0.35f, 0.66f}, {2.87f, 2.25f}},
+    {64, 64, 2, 2, 3, 256, 3, {0.24f, 0.56f, 0.78f}, {2.79f, 2.53f, 1.82f}},
+    {32, 64, 2, 2, 3, 256, 4, {0.17f, 0.36f, 0.74f, 0.82f}, {2.58f, 2.65f, 1.53f, 0.60f}},
+    {32, 32, 2, 2, 4, 256, 4, {0.12f, 0.24f, 0.40f, 0.51f}, {2.64f, 2.63f, 3.03f, 0.90f}},
 };
 // blocks: 4-bit results, only tiles whose waves hold whole blocks of 32 columns
 template <int NC>

@@ -407,6 +407,7 @@ _FP4_ARGS = struct.Struct("@3iPqPqPq")
 _CACHE_ARGS = "4i4P12qPqi0P"  # the cache and its table, inside the calls' structs
 _APPEND_ARGS = struct.Struct("@7i0P" + _CACHE_ARGS + "2P6q3PqPPd")
 _ATTENTION_ARGS = struct.Struct("@5i0P" + _CACHE_ARGS + "P3qP3qP3q2PdPN")
+_WORKSPACE = struct.Struct("@PN")  # at its end
 
 
 def _operand(t, what, dtypes, index, shape=None):
@@ -799,25 +800,34 @@ def new_kv_cache(pages, page, heads, dh, device="cuda:0") -> KvCache:
     return KvCache(make(dh // 2), make(dh // 32), make(dh // 2), make(dh // 32))
 
 
+def _cache_part(t, what, index, shape):
+    """Strides of page, token and head of one of a cache's tensors."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != index or t.dtype is not torch.uint8 or t.shape != shape:
+        raise WamError(f"{what}: the cache needs uint8 tensors on the GPU of the first operand, codes [pages, page, H, "
+                       "dh / 2] and scales [pages, page, H, dh / 32]")
+    page, token, head, step = t.stride()
+    if step != 1 and shape[3] > 1 and t.numel() > 0:
+        raise WamError(f"{what}: a head of the cache must be contiguous")
+    return page, token, head
+
+
 def _cache_values(cache, table, index, B, H, dh, what):
     """A cache and its page table as the calls' structs hold them."""
     if not isinstance(cache, tuple) or len(cache) != 4:
         raise WamError(f"{what}: cache must be a KvCache")
     k, k_scale, v, v_scale = cache
-    _operand(k, f"{what}: cache", _U8, index)
-    if k.dim() != 4 or (H is not None and k.shape[2] != H) or 2 * k.shape[3] != dh:
+    shape = k.shape if isinstance(k, torch.Tensor) else ()
+    if len(shape) != 4 or (H is not None and shape[2] != H) or 2 * shape[3] != dh:
         raise WamError(f"{what}: the cache's codes must be [pages, page, H, dh / 2]")
-    pages, page, H, half = k.shape
-    _operand(v, f"{what}: cache", _U8, index, k.shape)
+    pages, page, H, half = shape
     scales = (pages, page, H, half // 16)
-    _operand(k_scale, f"{what}: cache", _U8, index, scales)
-    _operand(v_scale, f"{what}: cache", _U8, index, scales)
     _operand(table, f"{what}: table", _I32, index)
     if table.dim() != 2 or table.shape[0] != B:
         raise WamError(f"{what}: table must be [B, pages of a sequence]")
-    return (pages, page, H, dh, k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), *k.stride()[:3],
-            *k_scale.stride()[:3], *v.stride()[:3], *v_scale.stride()[:3], table.data_ptr(), table.stride(0),
-            table.shape[1])
+    ks, kss = _cache_part(k, what, index, shape), _cache_part(k_scale, what, index, scales)
+    vs, vss = _cache_part(v, what, index, shape), _cache_part(v_scale, what, index, scales)
+    return (pages, page, H, dh, k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr(), *ks, *kss, *vs, *vss,
+            table.data_ptr(), table.stride(0), table.shape[1])
 
 
 def _per_sequence(t, what, index, B):
@@ -893,7 +903,7 @@ def cache_attention(q, cache, table, lengths, *, rows=None, causal=False, scale=
     if need:
         # freed to the call's own stream when this returns: later work there may take it
         work = _new(stream, torch.empty, need, dtype=torch.uint8, device=q.device)
-        a = _pack(_ATTENTION_ARGS, "cache_attention", *head, work.data_ptr(), need)
+        a = a[:-_WORKSPACE.size] + _WORKSPACE.pack(work.data_ptr(), need)
     _call(lib.wam_cache_attention, a, index, stream, "wam_cache_attention")
     return out
 

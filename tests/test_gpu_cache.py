@@ -533,7 +533,8 @@ def test_same_bits_twice(dev, R):
 def test_binding_refusals(dev, R):
     q, cache, table, lengths = _attend_case(R, dev, (2, 3, 4, 2, 64, 16, (40, 20)), BF16)
     for bad in (dict(q=q[0]), dict(q=q.half()), dict(q=q.cpu()), dict(q=q[:, :, :3]), dict(q=q[..., :32]), dict(cache=cache[:3]),
-                dict(cache=list(cache)), dict(cache=(cache.k[0], *cache[1:])), dict(cache=(cache.k, cache.k_scale[..., :1], *cache[2:])),
+                dict(cache=list(cache)), dict(cache=(cache.k[0], *cache[1:])), dict(cache=(None, *cache[1:])), dict(cache=(*cache[:3], None)),
+                dict(cache=(*cache[:3], cache.v_scale.cpu())), dict(cache=(cache.k, cache.k_scale, cache.v.flip(3)[:, :, :, ::2], cache.v_scale)), dict(cache=(cache.k, cache.k_scale[..., :1], *cache[2:])),
                 dict(cache=(cache.k.int(), *cache[1:])), dict(table=table.long()), dict(table=table[:1]), dict(table=table[0]),
                 dict(lengths=lengths[:1]), dict(lengths=lengths.long()), dict(rows=lengths.float()), dict(scale=0.0),
                 dict(scale=-1.0), dict(scale=math.nan), dict(out=torch.empty_like(q)[:1]), dict(out=q), dict(out=q.float()),

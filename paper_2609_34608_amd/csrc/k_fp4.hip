@@ -113,13 +113,14 @@ __device__ __forceinline__ int append_page(const AppendParams<P>& p, int b, int 
 // LDS; a thread keeps one row for all the heads it visits, with the products of its
 // cosines, sines and gains in registers.  The other values of its pairs are a load of
 // their own (a lane's eight are neighbours, so that a block of 32 lies in four lanes).
-// Heads are loaded one ahead of the arithmetic.
+// The values' heads go along with the keys'; both are loaded one ahead of the arithmetic,
+// the first before the row's page is known (10176 rows of 24 heads of 64 with the RMS norm,
+// from HBM: 36 us with keys and values in blocks of their own, 31 so; 26 without its stores).
 template <typename T, bool PAIRS, int P>
 __global__ __launch_bounds__(256) void cache_append_units_kernel(AppendParams<P> p) {
   extern __shared__ double2 turn[];
   const wam_cache_append_args& a = p.a;
   const wam_cache& ca = a.cache;
-  const bool isk = blockIdx.z == 0;
   const int rows = a.B * a.T, row0 = blockIdx.x * p.rows_block, live_rows = min(p.rows_block, rows - row0);
   const int slot = threadIdx.x / p.lanes, unit = threadIdx.x % p.lanes, col = 8 * unit;
   const int heads_par = 256 / p.lanes / p.rows_block;
@@ -130,54 +131,55 @@ __global__ __launch_bounds__(256) void cache_append_units_kernel(AppendParams<P>
   int place = 0;
   const int page = row < rows ? append_page(p, b, t, place) : -1;
 
-  const T* x = static_cast<const T*>(isk ? a.k : a.v);
-  const int64_t* si = isk ? a.k_stride : a.v_stride;
-  if (mine) x += b * si[0] + t * si[1];
-  const bool turned = isk && col < 2 * p.pairs;
-  const int other = PAIRS || !turned ? col : col < p.pairs ? col + p.pairs : col - p.pairs;
-  Pack<T, 8> own{}, far{};
+  const T *xk = static_cast<const T*>(a.k) + col, *xv = static_cast<const T*>(a.v) + col;
+  if (mine) {
+    xk += b * a.k_stride[0] + t * a.k_stride[1];
+    xv += b * a.v_stride[0] + t * a.v_stride[1];
+  }
+  const bool turned = col < 2 * p.pairs;
+  const int other = PAIRS || !turned ? 0 : col < p.pairs ? p.pairs : -p.pairs;  // from the lane's own values
+  Pack<T, 8> own{}, far{}, val{};
   auto load = [&](int hh) __attribute__((always_inline)) {
-    if (mine && page >= 0 && hh < ca.H) {
-      own = *reinterpret_cast<const Pack<T, 8>*>(x + hh * si[2] + col);
-      if (!PAIRS && turned) far = *reinterpret_cast<const Pack<T, 8>*>(x + hh * si[2] + other);
+    if (mine && hh < ca.H) {
+      own = *reinterpret_cast<const Pack<T, 8>*>(xk + hh * a.k_stride[2]);
+      if (!PAIRS && turned) far = *reinterpret_cast<const Pack<T, 8>*>(xk + hh * a.k_stride[2] + other);
+      val = *reinterpret_cast<const Pack<T, 8>*>(xv + hh * a.v_stride[2]);
     }
   };
   load(h);
   double gc[8], gs[8];  // factors of the lane's own values and of the others
-  const bool normed = isk && a.k_gain;
-  if (isk) {
-    append_turns(p, row0, live_rows, turn);
-    __syncthreads();
+  const bool normed = a.k_gain;
+  append_turns(p, row0, live_rows, turn);
+  __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int j = PAIRS ? 4 * unit + i / 2 : (col < p.pairs ? col : other) + i;
-      const bool first = PAIRS ? i % 2 == 0 : col < p.pairs;
-      const double2 cs = turned && mine ? turn[slot / heads_par * p.pairs + j] : make_double2(1.0, 0.0);
-      gc[i] = cs.x, gs[i] = first ? -cs.y : cs.y;
-      if (normed && mine) {
-        gc[i] *= (double)a.k_gain[col + i];
-        gs[i] *= (double)a.k_gain[PAIRS ? col + (i ^ 1) : other + i];
-      }
+  for (int i = 0; i < 8; ++i) {
+    const int j = PAIRS ? 4 * unit + i / 2 : (col < p.pairs ? col : col + other) + i;
+    const bool first = PAIRS ? i % 2 == 0 : col < p.pairs;
+    const double2 cs = turned && mine ? turn[slot / heads_par * p.pairs + j] : make_double2(1.0, 0.0);
+    gc[i] = cs.x, gs[i] = first ? -cs.y : cs.y;
+    if (normed && mine) {
+      gc[i] *= (double)a.k_gain[col + i];
+      gs[i] *= (double)a.k_gain[PAIRS ? col + (i ^ 1) : col + other + i];
     }
   }
-  const int64_t* so = isk ? ca.k_stride : ca.v_stride;
-  const int64_t* ss = isk ? ca.k_scale_stride : ca.v_scale_stride;
-  uint8_t* q = (isk ? ca.k : ca.v) + page * so[0] + place * so[1] + col / 2;
-  uint8_t* scale = (isk ? ca.k_scale : ca.v_scale) + page * ss[0] + place * ss[1] + col / kFp4Block;
+  uint8_t* qk = ca.k + page * ca.k_stride[0] + place * ca.k_stride[1] + col / 2;
+  uint8_t* qv = ca.v + page * ca.v_stride[0] + place * ca.v_stride[1] + col / 2;
+  uint8_t* sk = ca.k_scale + page * ca.k_scale_stride[0] + place * ca.k_scale_stride[1] + col / kFp4Block;
+  uint8_t* sv = ca.v_scale + page * ca.v_scale_stride[0] + place * ca.v_scale_stride[1] + col / kFp4Block;
   for (int h0 = blockIdx.y * heads_par; h0 < ca.H; h0 += step, h += step) {
-    float y[8];
+    float y[8], v[8];
     double z[8], w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = to_f32(own.v[i]);
-    if (isk && (p.pairs || normed)) {
+    for (int i = 0; i < 8; ++i) y[i] = to_f32(own.v[i]), v[i] = to_f32(val.v[i]);
+    if (p.pairs || normed) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         z[i] = (double)y[i];
         w[i] = (double)to_f32(PAIRS ? own.v[i ^ 1] : far.v[i]);
       }
     }
-    load(h + step);  // the next head's while this one is turned
-    if (isk && (p.pairs || normed)) {
+    load(h + step);  // while this head is turned
+    if (p.pairs || normed) {
       double rs = 1.0;
       if (normed) {
         double sum = 0.0;
@@ -189,10 +191,14 @@ __global__ __launch_bounds__(256) void cache_append_units_kernel(AppendParams<P>
       for (int i = 0; i < 8; ++i)  // past the pairs: not plus 0, which would spread a NaN or an infinity
         y[i] = (float)((turned ? z[i] * gc[i] + w[i] * gs[i] : z[i] * gc[i]) * rs);
     }
-    const uint32_t byte = fp4_scale(quad_max(mine ? most_of(y) : 0));
+    const uint32_t bk = fp4_scale(quad_max(mine ? most_of(y) : 0)), bv = fp4_scale(quad_max(mine ? most_of(v) : 0));
     if (!mine || page < 0 || h >= ca.H) continue;
-    *reinterpret_cast<uint32_t*>(q + h * so[2]) = pack_fp4(y, byte);
-    if (unit % 4 == 0) scale[h * ss[2]] = (uint8_t)byte;
+    *reinterpret_cast<uint32_t*>(qk + h * ca.k_stride[2]) = pack_fp4(y, bk);
+    *reinterpret_cast<uint32_t*>(qv + h * ca.v_stride[2]) = pack_fp4(v, bv);
+    if (unit % 4 == 0) {
+      sk[h * ca.k_scale_stride[2]] = (uint8_t)bk;
+      sv[h * ca.v_scale_stride[2]] = (uint8_t)bv;
+    }
   }
 }
 
@@ -275,13 +281,13 @@ hipError_t launch_append(const wam_cache_append_args& a, int shift, hipStream_t 
   p.lanes = 4;
   while (p.lanes * 8 < a.cache.dh) p.lanes *= 2;
   const int rows = a.B * a.T, H = a.cache.H, slots = 256 / p.lanes;
-  // eight rows a block, whose codes of a head lie side by side in its page; fewer where
+  // 16 rows a block, whose codes of a head lie side by side in its page; fewer where
   // that leaves CUs without a block
-  p.rows_block = 8;
+  p.rows_block = 16;
   while (p.rows_block > 1 && (rows + p.rows_block - 1) / p.rows_block < 512) p.rows_block /= 2;
   const int heads_par = slots / p.rows_block, head_blocks = (H + heads_par - 1) / heads_par;
   const int row_blocks = (rows + p.rows_block - 1) / p.rows_block;
-  const dim3 grid(row_blocks, row_blocks >= 512 ? 1 : std::min(head_blocks, 65535), 2);
+  const dim3 grid(row_blocks, row_blocks >= 512 ? 1 : std::min(head_blocks, 65535));
   const size_t lds = sizeof(double2) * p.rows_block * p.pairs;
   if (a.dtype == WAM_BF16) launch_append_type<bf16>(p, grid, lds, s);
   else launch_append_type<float>(p, grid, lds, s);

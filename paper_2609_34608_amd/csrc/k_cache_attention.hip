@@ -48,6 +48,7 @@ struct AttendParams {
   int group;       // query heads of a key head
   int row_blocks;  // blocks of rows of a (sequence, key head)
   int splits;      // blocks that share the tokens of a row block
+  int by_rows;     // a block's waves take rows of their own instead of tokens
   float log2_scale;
 };
 
@@ -161,7 +162,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
   const BlockAt id = block_at(blockIdx.x, a.B * ca.H, p.row_blocks, p.splits);
   const int rb = id.rb, split_at = id.split, hk = id.pair % ca.H, b = id.pair / ca.H;
 
-  const int R = p.group * a.T, r0 = rb * QT * 16;
+  const int R = p.group * a.T, r0 = (p.by_rows ? rb * kWaves + wid : rb) * QT * 16;
+  const int stride = p.by_rows ? 1 : kWaves;  // from tile to tile
   const int rows = a.rows ? min(max(a.rows[b], 0), a.T) : a.T;
   const int length = a.lengths[b], held = tokens_held(length, a.table.width, p.shift);
   // what the rows of this block see at least and at most (row r is t = r / group, in order)
@@ -206,7 +208,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
   // is read when its pages are needed costs a tile the latency of one more load, and
   // addresses that every tile works out anew cost it 200 scalar instructions.
   const int32_t* table = a.table.entry + b * a.table.stride;
-  auto token_of = [&](int tile) { return ((int64_t)tile + lane / 4 * kWaves) * kKeys + lane % 4 * 16; };
+  auto token_of = [&](int tile) { return ((int64_t)tile + lane / 4 * stride) * kKeys + lane % 4 * 16; };
   auto pages_from = [&](int tile) __attribute__((always_inline)) {
     const int64_t t = token_of(tile);
     return t < held ? page_of(table, a.table.width, p.shift, ca.pages, (int)t) : -1;
@@ -270,14 +272,14 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     if (threadIdx.x < DH) odd[threadIdx.x] = INT32_MAX;
     __syncthreads();
   }
-  const int first = t_lo + wid;
+  const int first = t_lo + (p.by_rows ? 0 : wid);
   int more = -1, turn = 0;
   if (first < t_hi) {
     place_groups(first, pages_from(first));
-    more = pages_from(first + 16 * kWaves);
+    more = pages_from(first + 16 * stride);
     request(0);
   }
-  for (int tile = first; tile < t_hi; tile += kWaves) {
+  for (int tile = first; tile < t_hi; tile += stride) {
     const int k0 = tile * kKeys;
     const uint32_t has = there;
     const bool whole = k0 + kKeys <= least && has == 15;
@@ -323,11 +325,11 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
             st[i][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][s][n], st[i][g], 0, 0, 0);
       }
     }
-    if (tile + kWaves < t_hi) {
+    if (tile + stride < t_hi) {
       if (++turn == 16) {
         turn = 0;
-        place_groups(tile + kWaves, more);
-        more = pages_from(tile + 17 * kWaves);
+        place_groups(tile + stride, more);
+        more = pages_from(tile + 17 * stride);
       }
       request(turn);
     }
@@ -408,6 +410,31 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     __builtin_amdgcn_wave_barrier();
   }
 
+  if (p.by_rows) {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      const int r = r0 + i * 16 + lr, t = r / p.group, h = hk * p.group + r % p.group;
+      if (r >= R) continue;
+      const float total = l[i][0], inv = 1.0f / total;
+      const int sees = a.causal ? tokens_seen(held, length, true, rows, t) : 0;
+      T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + t * a.out_stride[1] + h * a.out_stride[2];
+#pragma unroll
+      for (int j = 0; j < DT; ++j) {
+        const int d = j * 16 + 4 * lg;
+        Pack<T, 4> w;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float x = sees > odd[d + k] && a.causal ? NAN : o[i][j][k];
+          w.v[k] = static_cast<T>(total == 0.f ? 0.f : x * inv);
+        }
+        *reinterpret_cast<Pack<T, 4>*>(out + d) = w;
+      }
+      if (a.lse && lg == 0)
+        a.lse[b * a.lse_stride[0] + t * a.lse_stride[1] + h * a.lse_stride[2]] =
+            total == 0.f ? -INFINITY : (m[i] + __builtin_amdgcn_logf(total)) * kLn2;
+    }
+    return;
+  }
   // The waves' parts join in LDS, in the order of the waves: maximum, then the sums at
   // that maximum.
 #pragma unroll
@@ -476,15 +503,16 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
   }
 }
 
-// Joins the parts of a row, a wave a row: a lane takes four values of dh in every G-th
-// split, so that the loads of G splits go out together, and the lanes of a value add up
-// in a fixed order.
-template <typename T>
+// Joins the parts of a row, W waves a row: a lane takes four values of dh in every G-th part
+// of its wave's, so that the loads of several parts go out together, and the sums of a
+// value add up in a fixed order.
+template <typename T, int W>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
+  __shared__ float shared[W][kWave * 5];
   const wam_cache_attention_args& a = p.a;
-  const int R = p.group * a.T, DH = a.cache.dh, lane = threadIdx.x % kWave;
-  const int64_t i = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;  // (b, hk, r)
-  if (i >= (int64_t)a.B * a.cache.H * R) return;
+  const int R = p.group * a.T, DH = a.cache.dh, lane = threadIdx.x % kWave, wid = threadIdx.x / kWave % W;
+  const int64_t i = (int64_t)blockIdx.x * (4 / W) + threadIdx.x / (kWave * W);  // (b, hk, r)
+  if (i >= (int64_t)a.B * a.cache.H * R) return;                               // (W = 4: all of the block's or none)
   const int64_t bh = i / R;
   const int r = (int)(i % R), b = (int)(bh / a.cache.H), hk = (int)(bh % a.cache.H);
   const float* ws = static_cast<const float*>(a.workspace) + (bh * p.splits * R + r) * DH;
@@ -495,12 +523,12 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
 #pragma unroll
   for (int o = 1; o < kWave; o *= 2) top = fmaxf(top, __shfl_xor(top, o, 64));
   const int lanes = DH <= 64 ? DH / 4 <= 8 ? 8 : 16 : 32;  // of a row's values, a power of two
-  const int at = lane % lanes, from = lane / lanes, G = kWave / lanes;
+  const int at = lane % lanes, G = kWave / lanes;
   const bool mine = 4 * at < DH;
   f32x4 x = {0.f, 0.f, 0.f, 0.f};
   float total = 0.f;
-#pragma unroll 4
-  for (int s = from; s < p.splits; s += G) {
+#pragma unroll 8
+  for (int s = wid * G + lane / lanes; s < p.splits; s += W * G) {
     const int64_t row = (int64_t)s * R;
     const float f = __builtin_amdgcn_exp2f(ml[row * 2] - top);
     total += ml[row * 2 + 1] * f;
@@ -511,7 +539,20 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] += __shfl_xor(x[k], o, 64);
   }
-  if (from) return;
+  if constexpr (W > 1) {
+    shared[wid][lane] = total;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) shared[wid][(k + 1) * kWave + lane] = x[k];
+    __syncthreads();
+    if (wid) return;
+#pragma unroll
+    for (int w = 1; w < W; ++w) {
+      total += shared[w][lane];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] += shared[w][(k + 1) * kWave + lane];
+    }
+  }
+  if (lane >= lanes) return;
   const int t = r / p.group, h = hk * p.group + r % p.group;
   const float inv = 1.0f / total;
   T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + t * a.out_stride[1] + h * a.out_stride[2];
@@ -524,31 +565,45 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
         total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-// Tiles of 16 rows a block takes, and over how many blocks a sequence's tokens go.
-constexpr int64_t kSlots = 512;  // blocks that the chip holds at once
-constexpr int kPartTiles = 24;   // what a block costs beside its tiles, in tiles
+// Tiles of 16 rows a wave takes, whether the waves of a block share tokens or rows, and over
+// how many blocks a sequence's tokens go.
+constexpr int kShort = 32;      // tiles of a sequence
+constexpr int kPartTiles = 24;  // what a block costs beside its tiles, in tiles
 struct AttendPlan {
   int qt, row_blocks, splits;
+  bool by_rows;
 };
 AttendPlan plan_attend(const wam_cache_attention_args& a) {
   AttendPlan pl;
-  const int64_t R = (int64_t)(a.Hq / a.cache.H) * a.T;
-  const bool exact = a.dtype == WAM_FP32;
-  const int most = exact ? 1 : a.cache.dh <= 64 ? 4 : 2;
+  const int64_t R = (int64_t)(a.Hq / a.cache.H) * a.T, pairs = (int64_t)a.B * a.cache.H;
+  const int64_t tiles = ((int64_t)a.table.width * a.cache.page + kKeys - 1) / kKeys;
+  const bool narrow = a.cache.dh <= 64;
+  // As many rows as registers hold: a tile's conversions serve all of them.  In float32 that
+  // takes many blocks of long sequences (2 x 16 rows against 16: 10176 rows of 24 heads over
+  // as many tokens 2022 -> 1768 us, 4 x 864 of 12 over 864 47 -> 52).
+  int most = narrow ? 4 : 2;
+  if (a.dtype == WAM_FP32) most = narrow && tiles > kShort && pairs * ((R + 15) / 16) >= 4096 ? 2 : 1;
   pl.qt = 1;
   while (pl.qt < most && pl.qt * 16 < R) pl.qt *= 2;
   pl.row_blocks = (int)((R + pl.qt * 16 - 1) / (pl.qt * 16));
-  const int64_t blocks = (int64_t)a.B * a.cache.H * pl.row_blocks;
-  const int64_t tiles = ((int64_t)a.table.width * a.cache.page + kKeys - 1) / kKeys;
-  // Two blocks a CU at once: as many parts as make the rounds of those shortest, each wave
-  // with two tiles at least (64 rows of 24 heads over 101760 tokens in 1032 blocks, three
-  // rounds: 88 us; in 504, one: 71).
+  const int64_t blocks = pairs * pl.row_blocks;
+  // blocks that the chip holds at once, by their registers and LDS
+  const int64_t slots = pl.qt == 1 && narrow ? a.cache.dh == 32 ? 1024 : 768 : 512;
+  // Few tiles leave waves that share them without work, or with less of it than joining
+  // costs (9 x 4924 rows of 9 heads over 60 tokens 143 -> 44 us, 8 x 1000 of 16 over 700
+  // 53 -> 37); rows of their own take more blocks to fill the chip.
+  pl.by_rows = pl.row_blocks > 1 && (tiles <= kWaves || (tiles <= kShort && blocks >= 2048));
   pl.splits = 1;
-  if (blocks < 4 * kSlots) {
+  if (pl.by_rows) {
+    pl.row_blocks = (pl.row_blocks + kWaves - 1) / kWaves;
+  } else if (blocks < 4 * slots) {
+    // As many parts as make the rounds of blocks shortest, each wave with two tiles at least
+    // (64 rows of 24 heads over 101760 tokens in 1032 blocks, three rounds: 88 us; in 504,
+    // one: 71).
     double best = INFINITY;
-    const int64_t top = std::min<int64_t>(tiles / (2 * kWaves), 2 * kSlots / blocks);
+    const int64_t top = std::min<int64_t>(tiles / (2 * kWaves), 2 * slots / blocks);
     for (int64_t s = 1; s <= std::max<int64_t>(top, 1); ++s) {
-      const double cost = (double)((blocks * s + kSlots - 1) / kSlots) * ((double)tiles / (double)s + kPartTiles);
+      const double cost = (double)((blocks * s + slots - 1) / slots) * ((double)tiles / (double)s + kPartTiles);
       if (cost < best) best = cost, pl.splits = (int)s;
     }
   }
@@ -564,9 +619,9 @@ size_t workspace_of(const wam_cache_attention_args& a, const AttendPlan& pl) {
 template <int DB, int NS>
 hipError_t launch_blocks_of(const AttendParams& p, const AttendPlan& pl, dim3 grid, hipStream_t s) {
   if (pl.qt == 1) launch_k(attend_kernel<DB, 1, NS>, grid, kWaves * kWave, 0, s, p);
-  else if constexpr (NS == 1) {
+  else if constexpr (NS == 1 || DB <= 2) {
     if (pl.qt == 2) launch_k(attend_kernel<DB, 2, NS>, grid, kWaves * kWave, 0, s, p);
-    else if constexpr (DB <= 2) launch_k(attend_kernel<DB, 4, NS>, grid, kWaves * kWave, 0, s, p);
+    else if constexpr (NS == 1 && DB <= 2) launch_k(attend_kernel<DB, 4, NS>, grid, kWaves * kWave, 0, s, p);
   }
   return hipGetLastError();
 }
@@ -585,7 +640,9 @@ hipError_t launch_attend(const AttendParams& p, const AttendPlan& pl, hipStream_
   if (e != hipSuccess || pl.splits == 1) return e;
   typedef typename std::conditional<NS == 1, bf16, float>::type T;
   const int64_t rows = (int64_t)p.a.B * p.a.Hq * p.a.T;
-  launch_k(join_kernel<T>, dim3((unsigned)((rows + 3) / 4)), 256, 0, s, p);
+  // a wave a row, four where a row has many parts
+  if (pl.splits > 16) launch_k(join_kernel<T, 4>, dim3((unsigned)rows), 256, 0, s, p);
+  else launch_k(join_kernel<T, 1>, dim3((unsigned)((rows + 3) / 4)), 256, 0, s, p);
   return hipGetLastError();
 }
 
@@ -643,6 +700,7 @@ int wam_cache_attention(const wam_cache_attention_args* a, void* hip_stream) {
   p.group = a->Hq / a->cache.H;
   p.row_blocks = pl.row_blocks;
   p.splits = pl.splits;
+  p.by_rows = pl.by_rows;
   p.log2_scale = (float)(a->scale * 1.4426950408889634);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const hipError_t e = a->dtype == WAM_BF16 ? launch_attend<1>(p, pl, s) : launch_attend<3>(p, pl, s);

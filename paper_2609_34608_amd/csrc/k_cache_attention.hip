@@ -569,6 +569,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
 // how many blocks a sequence's tokens go.
 constexpr int kShort = 32;      // tiles of a sequence
 constexpr int kPartTiles = 24;  // what a block costs beside its tiles, in tiles
+constexpr int kJoinTiles = 24;  // and the launch that joins parts
 struct AttendPlan {
   int qt, row_blocks, splits;
   bool by_rows;
@@ -603,7 +604,8 @@ AttendPlan plan_attend(const wam_cache_attention_args& a) {
     double best = INFINITY;
     const int64_t top = std::min<int64_t>(tiles / (2 * kWaves), 2 * slots / blocks);
     for (int64_t s = 1; s <= std::max<int64_t>(top, 1); ++s) {
-      const double cost = (double)((blocks * s + slots - 1) / slots) * ((double)tiles / (double)s + kPartTiles);
+      const double cost = (double)((blocks * s + slots - 1) / slots) * ((double)tiles / (double)s + kPartTiles) +
+                          (s > 1 ? kJoinTiles : 0);
       if (cost < best) best = cost, pl.splits = (int)s;
     }
   }

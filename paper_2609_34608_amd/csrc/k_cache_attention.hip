@@ -18,9 +18,19 @@
 // by more than 8, so most tiles have no rescale; its denominator is one more MFMA
 // against ones, which sums exactly the rounded probabilities that multiply V.
 //
-// A block's four waves share the tokens of its rows (few rows), taking tiles in turn, and
-// join through LDS; where blocks are few, a sequence's tokens are split over blocks
-// too, whose parts go to the workspace for a second launch to join in order.
+// A block's four waves share the tokens of its rows, taking tiles in turn, and join through
+// LDS; where blocks are few, a sequence's tokens are split over blocks too, whose parts go
+// to the workspace for a second launch to join in order.  Over few tokens the waves take
+// rows of their own.
+//
+// What bounds it, on one MI355X: single rows the bytes of the cache (16 streams of 16384 to
+// 32768 tokens, 8 heads of 128: 91 us, 4.8 TB/s; a 1 GiB copy reaches 5.0); many rows the
+// instructions: 10176 rows of 24 heads of 64 over 20352 tokens take 1416 us, 899 TFLOP/s
+// (a bf16 product of 8192^3 reaches 1213), the matrix cores 40% busy, at 2.1 GHz, to which
+// the power of this mix brings the clock down.  A form for many rows that converts tokens
+// once for four waves of 64 rows, with 32x32x16 products between the exponentials and
+// without the maximum, has half the matrix instructions and 30% fewer others, and took as
+// long (1340 to 1410 us; shorter sequences longer), so this one stays.
 #include <math.h>
 
 #include <algorithm>

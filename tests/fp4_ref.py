@@ -176,3 +176,43 @@ def attention(q, cache, table, lengths, *, rows=None, causal=False, scale=None):
                 lse[b, t, h] = s.max() + torch.log(total)
                 lse_bound[b, t, h] = d + 2.0 ** -22 * (abs(float(lse[b, t, h])) + X)
     return out, lse, bound, lse_bound
+
+
+def attention_whole(q, cache, table, lengths, *, rows=None, causal=False, scale=None):
+    """attention (same results and bounds), a head's rows at once and on q's device, for sizes
+    past a row at a time."""
+    B, T, Hq, dh = q.shape
+    dev, exact = q.device, q.dtype == torch.float32
+    k, v = (values(*c).to(dev) for c in (cache[:2], cache[2:]))
+    pages, page, H = k.shape[:3]
+    scale = 1.0 / math.sqrt(dh) if scale is None else scale
+    out, bound = (torch.zeros(q.shape, dtype=F64, device=dev) for _ in range(2))
+    lse = torch.full((B, T, Hq), -math.inf, dtype=F64, device=dev)
+    lse_bound = torch.zeros(B, T, Hq, dtype=F64, device=dev)
+    room = table.shape[1] * page
+    for b in range(B):
+        length = int(lengths[b])
+        token = torch.arange(max(0, min(length, room)), device=dev)
+        entry = table[b].long()[token // page]
+        token, entry = token[(entry >= 0) & (entry < pages)], entry[(entry >= 0) & (entry < pages)]
+        if not len(token):
+            continue
+        n = T if rows is None else min(int(rows[b]), T)
+        sees = token < torch.tensor([seen(length, room, causal, n, t) for t in range(T)], device=dev)[:, None]
+        some = sees.any(-1)
+        for h in range(Hq):
+            kk, vv = (x[entry, token % page, h * H // Hq] for x in (k, v))
+            x = q[b, :, h].to(F64)
+            s = torch.where(sees, scale * (x @ kk.t()), -math.inf)
+            X = torch.where(sees, scale * (x.abs() @ kk.abs().t()), 0.0).amax(-1, keepdim=True)
+            top = s.amax(-1, keepdim=True).clamp_min(-1e300)
+            p = torch.exp(s - top)
+            total = p.sum(-1, keepdim=True).clamp_min(1e-300)
+            o, mag = p @ vv / total, p @ vv.abs() / total
+            d = 2.0 ** -22 * (2 + dh / 32 * X + 2 * X) + (0 if exact else half_step(torch.bfloat16))
+            d = d + 2.0 ** -22 * (sees.sum(-1, keepdim=True) / 32 + 16)
+            value = (top + torch.log(total))[:, 0]
+            out[b, :, h], bound[b, :, h] = torch.where(some[:, None], o, 0.0), d * (mag + o.abs())
+            lse[b, :, h] = torch.where(some, value, -math.inf)
+            lse_bound[b, :, h] = torch.where(some, d[:, 0] + 2.0 ** -22 * (value.abs() + X[:, 0]), 0.0)
+    return out, lse, bound, lse_bound

@@ -159,6 +159,15 @@ def test_attention_asks_for_its_workspace():
         assert lib.wam_cache_attention_workspace(C.byref(_attend(table__width=4096, **kw))) == 0
 
 
+def test_which_calls_take_a_workspace():
+    """Parts of long sequences do; short ones, and rows enough to fill the chip, do not."""
+    lib = L.lib()
+    for kw, parts in ((dict(T=2, table__width=188), True), (dict(T=1, Hq=2, table__width=1250), True),
+                      (dict(T=2, table__width=4), False), (dict(T=2, table__width=30), False),
+                      (dict(T=100000, table__width=188), False), (dict(T=2, table__width=188, dtype=L.WAM_FP32), True)):
+        assert (lib.wam_cache_attention_workspace(C.byref(_attend(**kw))) > 0) == parts
+
+
 def test_nothing_to_do():
     """Calls without rows or pages end before any device work."""
     lib = L.lib()

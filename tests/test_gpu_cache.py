@@ -225,6 +225,83 @@ def test_attention(dev, R, size, causal, dtype):
     _check(R, *_attend_case(R, dev, size, dtype), causal=causal)
 
 
+# Sizes that choose how rows and tokens go to waves: rows of their own over few tiles of tokens, and
+# over more where there are many blocks; parts that one wave or four join; 32 float32 rows a wave
+# B, T, Hq, H, dh, page, lengths, dtype
+FORMS = [
+    (3, 150, 4, 2, 64, 16, (200, 1, 256), BF16),
+    (2, 333, 3, 3, 128, 32, (100, 37), BF16),
+    (2, 70, 5, 5, 96, 16, (130, 64), F32),
+    (1, 65, 7, 1, 32, 16, (50,), F32),
+    (8, 1000, 16, 16, 64, 64, tuple(range(700, 300, -50)), BF16),
+    (4, 864, 12, 12, 64, 64, (864, 863, 100, 0), F32),
+    (1, 1, 2, 2, 64, 64, (20000,), BF16),
+    (1, 3, 8, 2, 128, 128, (30011,), F32),
+    (2, 2, 6, 3, 32, 16, (9000, 4001), BF16),
+    (2, 1366, 24, 24, 64, 64, (2177, 2300), F32),
+    (2, 2750, 24, 12, 32, 64, (2177, 2111), F32),
+]
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("size", FORMS)
+def test_attention_forms(dev, R, size, causal):
+    q, cache, table, lengths = _attend_case(R, dev, size[:7], size[7])
+    rows = lengths.clamp(max=size[1] - 1)  # the last row of each sequence is padding
+    lse = torch.full(q.shape[:3], 7.0, device=dev)
+    out = R.cache_attention(q, cache, table, lengths, rows=rows, causal=causal, lse=lse)
+    o, l, eo, el = F.attention_whole(q, cache, table, lengths, rows=rows, causal=causal)
+    F.check(out, o, eo, q.dtype)
+    F.check(lse, l, el, F32)
+
+
+def test_whole_and_row_references_agree(dev, R):
+    case = _attend_case(R, dev, (2, 21, 6, 2, 64, 16, (90, 30)), F32)
+    for causal in (False, True):
+        one, all_ = (f(*case, causal=causal, rows=_ints(dev, 21, 13).cpu()) for f in (F.attention, F.attention_whole))
+        for a, b in zip(one, all_):
+            assert torch.allclose(a, b.cpu(), rtol=1e-9, atol=1e-12)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [(1, 40, 2, 1, 64, 16, (300,)), (2, 90, 3, 3, 128, 16, (120, 77)), (1, 24, 2, 2, 32, 16, (9000,)),
+                                  (1, 130, 2, 2, 96, 32, (256,))])
+def test_attention_values_past_the_range(dev, R, size, dtype):
+    """Values of v past the bf16 range are NaN for the rows that see them, in their dims alone;
+    the largest that it holds are values."""
+    q, cache, table, lengths = _attend_case(R, dev, size, dtype)
+    g = torch.Generator().manual_seed(3)
+    dh, n = size[4], size[1]
+    for b in range(size[0]):
+        for t in torch.randint(max(0, int(lengths[b]) - n), int(lengths[b]), (6,), generator=g).tolist():
+            head, block = int(torch.randint(size[3], (1,), generator=g)), int(torch.randint(dh // 32, (1,), generator=g))
+            scale = [253, 254, 255][t % 3]
+            cache.v_scale[int(table[b, t // size[5]]), t % size[5], head, block] = scale
+    v = F.values(cache.v, cache.v_scale)
+    far = ~(v.abs() < 2.0 ** 128)  # NaN, or from where bf16 has no value
+    clean = R.KvCache(cache.k, cache.k_scale, cache.v.clone(), cache.v_scale.clone())
+    codes = torch.stack([cache.v & 15, cache.v >> 4], -1).flatten(-2).cpu()
+    codes[far] = 0
+    clean.v.copy_(codes[..., 0::2] | codes[..., 1::2] << 4)
+    clean.v_scale[clean.v_scale == 255] = 0
+    got = R.cache_attention(q, cache, table, lengths, causal=True).cpu()
+    o, _, eo, _ = F.attention_whole(q, clean, table, lengths, causal=True)
+    bad = torch.zeros_like(got, dtype=torch.bool)
+    for b in range(size[0]):
+        j = torch.arange(int(lengths[b]))
+        first = far[table[b].cpu().long()[j // size[5]], j % size[5]].cumsum(0) > 0  # one by then
+        for t in range(n):
+            seen = F.seen(int(lengths[b]), 1 << 30, True, n, t)
+            if seen:
+                bad[b, t] = first[seen - 1].repeat_interleave(size[2] // size[3], 0)
+    assert bad.any()
+    assert got[bad].isnan().all()
+    # sums of values next to the range's end may pass it: a probability is at most 2^8 of the row's last reference
+    whole = ~bad & (o.abs().cpu() < 2.0 ** 110)
+    if whole.any():
+        F.check(got[whole], o.cpu()[whole], eo.cpu()[whole], dtype)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("length", [0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 320])
 def test_attention_lengths(dev, R, length, dtype):

@@ -129,7 +129,7 @@ int plan_fp8(const TileCfg (&cfgs)[NC], int M, int N, int K, Fp8Result result = 
 
 // ---------------------------------------------------------------- 4-bit products
 // Tiles of gemm_fp4.h and their cost, a stage being 256 of K (bk in values).  Least-squares
-// fits to 61 sizes (1 to 10176 rows, N 512 to 6144, K 768 to 6144) on one MI355X, standard
+// fits to 57 sizes (1 to 10176 rows, N 512 to 6144, K 768 to 6144) on one MI355X, standard
 // deviation 9-13%; the choice is 1.7% slower than the fastest of 15 configurations on
 // average (14% at worst).  A stage has half the bytes of the 8-bit one and a quarter of its
 // matrix cycles, so what a tile costs beside its stages weighs more and two blocks a CU

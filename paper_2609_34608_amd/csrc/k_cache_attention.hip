@@ -608,15 +608,16 @@ AttendPlan plan_attend(const wam_cache_attention_args& a) {
   if (pl.by_rows) {
     pl.row_blocks = (pl.row_blocks + kWaves - 1) / kWaves;
   } else if (blocks < 4 * slots) {
-    // As many parts as make the rounds of blocks shortest, each wave with two tiles at least
-    // (64 rows of 24 heads over 101760 tokens in 1032 blocks, three rounds: 88 us; in 504,
-    // one: 71).
-    double best = INFINITY;
-    const int64_t top = std::min<int64_t>(tiles / (2 * kWaves), 2 * slots / blocks);
-    for (int64_t s = 1; s <= std::max<int64_t>(top, 1); ++s) {
-      const double cost = (double)((blocks * s + slots - 1) / slots) * ((double)tiles / (double)s + kPartTiles) +
-                          (s > 1 ? kJoinTiles : 0);
-      if (cost < best) best = cost, pl.splits = (int)s;
+    // As many parts as fill one round of blocks or two, whichever ends first, each wave with
+    // two tiles at least (64 rows of 24 heads over 101760 tokens in 1032 blocks, three
+    // rounds: 88 us; in 504, one: 71).
+    auto cost = [&](int64_t parts) {
+      return (double)((blocks * parts + slots - 1) / slots) * ((double)tiles / (double)parts + kPartTiles) +
+             (parts > 1 ? kJoinTiles : 0);
+    };
+    for (int rounds = 1; rounds <= 2; ++rounds) {
+      const int64_t parts = std::min(tiles / (2 * kWaves), rounds * slots / blocks);
+      if (parts > 1 && cost(parts) < cost(pl.splits)) pl.splits = (int)parts;
     }
   }
   return pl;

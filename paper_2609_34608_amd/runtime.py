@@ -688,12 +688,16 @@ _U8 = (torch.uint8,)
 _I32 = (torch.int32,)
 
 
-def _byte_rows(shape, dev, unit):
-    """A new tensor of bytes whose rows start a multiple of `unit` bytes apart."""
-    n = shape[-1]
-    if n % unit == 0:
-        return torch.empty(shape, dtype=torch.uint8, device=dev)
-    return torch.empty((*shape[:-1], -(-n // unit) * unit), dtype=torch.uint8, device=dev)[..., :n]
+def _matrix(M, n, dtype, dev):
+    """A new matrix (the fastest call for one)."""
+    return torch.empty_strided((M, n), (n, 1), dtype=dtype, device=dev)
+
+
+def _byte_rows(M, n, dev, unit):
+    """A new matrix of bytes whose rows start a multiple of `unit` bytes apart."""
+    wide = -(-n // unit) * unit
+    x = _matrix(M, wide, torch.uint8, dev)
+    return x if wide == n else x.as_strided((M, n), (wide, 1))
 
 
 def quantize_fp4(x, *, q=None, scale=None, stream: torch.cuda.Stream | None = None):
@@ -704,9 +708,9 @@ def quantize_fp4(x, *, q=None, scale=None, stream: torch.cuda.Stream | None = No
     index = _first(x, "quantize_fp4: x", _REAL, 2)
     M, K = x.shape
     codes, blocks = (M, -(-K // 2)), (M, -(-K // 32))
-    q = (_new(stream, _byte_rows, codes, x.device, 16) if q is None else
+    q = (_new(stream, _byte_rows, *codes, x.device, 16) if q is None else
          _operand(q, "quantize_fp4: q", _U8, index, codes))
-    scale = (_new(stream, _byte_rows, blocks, x.device, 4) if scale is None else
+    scale = (_new(stream, _byte_rows, *blocks, x.device, 4) if scale is None else
              _operand(scale, "quantize_fp4: scale", _U8, index, blocks))
     a = _pack(_FP4_ARGS, "quantize_fp4", M, K, _TYPES[x.dtype], x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0),
               scale.data_ptr(), scale.stride(0))
@@ -729,7 +733,7 @@ def dequantize_fp4(q, scale, *, columns=None, dtype=None, out=None, stream: torc
         dtype = torch.bfloat16 if dtype is None else dtype
         if dtype not in _REAL:
             raise WamError(f"dequantize_fp4: dtype {dtype} is not supported")
-        out = _new(stream, torch.empty, (M, K), dtype=dtype, device=q.device)
+        out = _new(stream, _matrix, M, K, dtype, q.device)
     else:
         _operand(out, "dequantize_fp4: out", _REAL if dtype is None else (dtype,), index, (M, K))
     a = _pack(_FP4_ARGS, "dequantize_fp4", M, K, _choice(_TYPES, out.dtype, "dequantize_fp4: dtype"), q.data_ptr(),
@@ -763,14 +767,14 @@ def matmul_fp4(a, a_scale, w, w_scale, *, bias=None, gelu=False, out=None, out_d
         raise WamError(f"matmul_fp4: out_dtype {kind} is not supported")
     shape = (M, -(-N // 2)) if blocks else (M, N)
     if out is None:
-        out = (_new(stream, _byte_rows, shape, a.device, 16) if blocks else
-               _new(stream, torch.empty, shape, dtype=kind, device=a.device))
+        out = (_new(stream, _byte_rows, *shape, a.device, 16) if blocks else
+               _new(stream, _matrix, *shape, kind, a.device))
     else:
         _operand(out, "matmul_fp4: out", (kind,) if out_dtype is None else (out_dtype,), index, shape)
     scale_at = scale_stride = 0
     if blocks:
         shape = (M, -(-N // 32))
-        out_scale = (_new(stream, _byte_rows, shape, a.device, 4) if out_scale is None else
+        out_scale = (_new(stream, _byte_rows, *shape, a.device, 4) if out_scale is None else
                      _operand(out_scale, "matmul_fp4: out_scale", _U8, index, shape))
         scale_at, scale_stride = out_scale.data_ptr(), out_scale.stride(0)
     args = _pack(_MATMUL_ARGS, "matmul_fp4", M, N, 2 * n, abi.WAM_FP4 if blocks else _TYPES[kind],
@@ -888,7 +892,8 @@ def cache_attention(q, cache, table, lengths, *, rows=None, causal=False, scale=
     held = _cache_values(cache, table, index, B, None, dh, "cache_attention")
     _operand(lengths, "cache_attention: lengths", _I32, index, (B,))
     count = _per_sequence(rows, "cache_attention: rows", index, B)
-    out = (_new(stream, torch.empty, q.shape, dtype=q.dtype, device=q.device) if out is None else
+    out = (_new(stream, torch.empty_strided, q.shape, (T * Hq * dh, Hq * dh, dh, 1), dtype=q.dtype, device=q.device)
+           if out is None else
            _operand(out, "cache_attention: out", (q.dtype,), index, q.shape))
     lse_stride = _NO_HEADS
     if lse is not None:
@@ -902,7 +907,7 @@ def cache_attention(q, cache, table, lengths, *, rows=None, causal=False, scale=
     need = lib.wam_cache_attention_workspace(a)
     if need:
         # freed to the call's own stream when this returns: later work there may take it
-        work = _new(stream, torch.empty, need, dtype=torch.uint8, device=q.device)
+        work = _new(stream, _matrix, 1, need, torch.uint8, q.device)
         a = a[:-_WORKSPACE.size] + _WORKSPACE.pack(work.data_ptr(), need)
     _call(lib.wam_cache_attention, a, index, stream, "wam_cache_attention")
     return out

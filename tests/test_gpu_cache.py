@@ -240,6 +240,7 @@ FORMS = [
     (2, 2, 6, 3, 32, 16, (9000, 4001), BF16),
     (2, 1366, 24, 24, 64, 64, (2177, 2300), F32),
     (2, 2750, 24, 12, 32, 64, (2177, 2111), F32),
+    (300, 1, 2, 1, 32, 16, tuple((7 * i) % 130 for i in range(300)), BF16),
 ]
 
 
@@ -253,6 +254,16 @@ def test_attention_forms(dev, R, size, causal):
     o, l, eo, el = F.attention_whole(q, cache, table, lengths, rows=rows, causal=causal)
     F.check(out, o, eo, q.dtype)
     F.check(lse, l, el, F32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_tables_wider_than_the_sequences(dev, R, dtype):
+    """Most parts of the tokens hold none, and some sequences are empty."""
+    q, cache, table, lengths = _attend_case(R, dev, (3, 2, 4, 2, 64, 16, (5, 0, 700)), dtype)
+    wide = torch.full((3, 4000), -1, dtype=I32, device=dev)
+    wide[:, :table.shape[1]] = table
+    for causal in (False, True):
+        _check(R, q, cache, wide, lengths, causal=causal)
 
 
 def test_whole_and_row_references_agree(dev, R):

@@ -602,8 +602,10 @@ AttendPlan plan_attend(const wam_cache_attention_args& a) {
   const int64_t slots = pl.qt == 1 && narrow ? a.cache.dh == 32 ? 1024 : 768 : 512;
   // Few tiles leave waves that share them without work, or with less of it than joining
   // costs (9 x 4924 rows of 9 heads over 60 tokens 143 -> 44 us, 8 x 1000 of 16 over 700
-  // 53 -> 37); rows of their own take more blocks to fill the chip.
-  pl.by_rows = pl.row_blocks > 1 && (tiles <= kWaves || (tiles <= kShort && blocks >= 2048));
+  // 53 -> 37, 8 x 4000 of 24 over 4000 940 -> 845); rows of their own take more blocks to
+  // fill the chip, and many of them where the rounds are long (10176 rows of 24 heads over
+  // as many tokens, 3816 blocks that share tokens: 742 -> 772).
+  pl.by_rows = pl.row_blocks > 1 && (tiles <= kWaves || blocks >= (tiles <= kShort ? 2048 : 8192));
   pl.splits = 1;
   if (pl.by_rows) {
     pl.row_blocks = (pl.row_blocks + kWaves - 1) / kWaves;

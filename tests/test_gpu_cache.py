@@ -241,6 +241,7 @@ FORMS = [
     (2, 1366, 24, 24, 64, 64, (2177, 2300), F32),
     (2, 2750, 24, 12, 32, 64, (2177, 2111), F32),
     (300, 1, 2, 1, 32, 16, tuple((7 * i) % 130 for i in range(300)), BF16),
+    (2, 4096, 16, 16, 96, 64, (2112, 2200), F32),
 ]
 
 

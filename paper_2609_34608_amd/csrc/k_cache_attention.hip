@@ -170,7 +170,9 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
   const int lane = threadIdx.x % kWave, wid = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lr = lane % 16, lg = lane / 16;
   const BlockAt id = block_at(blockIdx.x, a.B * ca.H, p.row_blocks, p.splits);
-  const int rb = id.rb, split_at = id.split, hk = id.pair % ca.H, b = id.pair / ca.H;
+  // causal: the rows that see most first (3000 rows of 2 x 8 heads over 4000 tokens 70 -> 55 us)
+  const int rb = a.causal ? p.row_blocks - 1 - id.rb : id.rb;
+  const int split_at = id.split, hk = id.pair % ca.H, b = id.pair / ca.H;
 
   const int R = p.group * a.T, r0 = (p.by_rows ? rb * kWaves + wid : rb) * QT * 16;
   const int stride = p.by_rows ? 1 : kWaves;  // from tile to tile

@@ -15,6 +15,11 @@
 // are neighbours and come in one 16-bit read, the second step naming the second byte.
 // The eight scale bytes of each row of a stage travel with it, by 4-byte loads
 // straight into LDS.
+//
+// What bounds it: 10176 x 6144 x 1536 takes 66 us (2.9 PFLOP/s; the instruction alone
+// reaches 9.5), 71 with the GELU.  A 256x256 tile's six stages are 9.3 us of it each, at
+// 55% of the matrix rate, and what it costs beside them 5.3: its first loads, the
+// activation, and a result whose 125 MB alone take 20 us of memory.
 #pragma once
 
 #include "fp4.h"

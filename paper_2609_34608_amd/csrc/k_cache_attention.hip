@@ -517,7 +517,8 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
 
 // Joins the parts of a row, W waves a row: a lane takes four values of dh in every G-th part
 // of its wave's, so that the loads of several parts go out together, and the sums of a
-// value add up in a fixed order.
+// value add up in a fixed order.  Bound by latency (1536 rows of 64 values in 21 parts 7.3 us
+// with a wave a row, 5.6 with four; 64 rows in 192 parts 9.5 with four, 38 -> 23 the call).
 template <typename T, int W>
 __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
   __shared__ float shared[W][kWave * 5];

@@ -14,7 +14,8 @@ namespace {
 
 // ------------------------------------------------------------- blocks of a matrix
 // A lane takes eight neighbouring columns (16 bytes of bf16), four lanes a block, whose
-// maximum they share without LDS; a wave stores its codes as 256 bytes side by side.
+// maximum they share without LDS; a wave stores its codes as 256 bytes side by side
+// (10176 x 6144 of bf16 30 us, 5.3 TB/s; back to values 23 us, 6.9 TB/s).
 template <typename T>
 __global__ __launch_bounds__(256) void quantize_fp4_kernel(wam_quantize_fp4_args a, int kb) {
   const uint32_t i = blockIdx.x * 64u + threadIdx.x / 4;  // block

@@ -31,6 +31,7 @@
 // once for four waves of 64 rows, with 32x32x16 products between the exponentials and
 // without the maximum, has half the matrix instructions and 30% fewer others, and took as
 // long (1340 to 1410 us; shorter sequences longer), so this one stays.
+#include <float.h>
 #include <math.h>
 
 #include <algorithm>
@@ -719,7 +720,8 @@ int wam_cache_attention(const wam_cache_attention_args* a, void* hip_stream) {
   p.row_blocks = pl.row_blocks;
   p.splits = pl.splits;
   p.by_rows = pl.by_rows;
-  p.log2_scale = (float)(a->scale * 1.4426950408889634);
+  // not zero: the -infinity of a token that a row does not see has to stay one
+  p.log2_scale = std::max((float)(a->scale * 1.4426950408889634), FLT_TRUE_MIN);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const hipError_t e = a->dtype == WAM_BF16 ? launch_attend<1>(p, pl, s) : launch_attend<3>(p, pl, s);
   if (e == hipErrorInvalidConfiguration) return noalloc_fail(WAM_E_SHAPE, "wam_cache_attention: too many blocks for one launch");

@@ -397,6 +397,15 @@ def test_attention_extreme_scores(dev, R, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [1e-37, 1e-42, 1e-60, 5e-324])
+def test_attention_scales_near_and_past_the_smallest_float(dev, R, scale, dtype):
+    """Every token that a row sees counts alike, also next to tokens that it does not see."""
+    for size in ((2, 5, 6, 2, 96, 32, (64, 65)), (2, 150, 4, 2, 64, 16, (200, 1)), (1, 1, 2, 2, 64, 64, (9001,))):
+        for causal in (False, True):
+            _check(R, *_attend_case(R, dev, size, dtype), causal=causal, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("order,pad,offset", [((0, 2, 1), 0, 0), ((2, 1, 0), 8, 0), ((1, 0, 2), 3, 1)])
 def test_attention_strides(dev, R, order, pad, offset, dtype):
     q, cache, table, lengths = _attend_case(R, dev, (2, 21, 6, 3, 64, 16, (77, 60)), dtype)

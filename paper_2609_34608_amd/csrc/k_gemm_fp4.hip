@@ -98,6 +98,9 @@ extern "C" int wam_matmul_fp4(const wam_matmul_fp4_args* a, void* hip_stream) {
     return noalloc_fail(WAM_E_ARG, "wam_matmul_fp4: out of WAM_FP4 needs out_scale with distinct rows");
   if (a->out == a->a || a->out == a->w || a->out == a->a_scale || a->out == a->w_scale)
     return noalloc_fail(WAM_E_ARG, "wam_matmul_fp4: out must not be an operand");
+  if (blocks && (a->out_scale == a->a || a->out_scale == a->w || a->out_scale == a->a_scale ||
+                 a->out_scale == a->w_scale || a->out_scale == a->out))
+    return noalloc_fail(WAM_E_ARG, "wam_matmul_fp4: out_scale must be a buffer of its own");
   const gemm::Fp4Operands p{a->a, a->w, a->a_scale, a->w_scale, a->M > 1 ? a->a_stride : 0, a->N > 1 ? a->w_stride : 0,
                             a->M > 1 ? a->a_scale_stride : 0, a->N > 1 ? a->w_scale_stride : 0, a->M, a->N, a->K};
   const gemm::Fp8Out o{a->bias, a->out, a->M > 1 ? a->out_stride : 0, nullptr, a->M > 1 ? a->out_scale_stride : 0};

@@ -86,6 +86,11 @@ def test_matmul_refuses(kw, code, text):
     _refused("wam_matmul_fp4", _matmul(**kw), code, text)
 
 
+@pytest.mark.parametrize("at", [P, P + 4096, P + 8192, P + 32768, P + 65536])
+def test_matmul_refuses_scales_in_another_buffer(at):
+    _refused("wam_matmul_fp4", _matmul(out_dtype=L.WAM_FP4, out_scale=at, out_scale_stride=2), L.WAM_E_ARG, "out_scale must be")
+
+
 def _cache():
     c = L.WamCache(8, 16, 2, 64, P, P + 16384, P + 32768, P + 49152)
     c.k_stride = c.v_stride = _i64(1024, 32, 512)

@@ -682,7 +682,7 @@ int wam_cache_append(const wam_cache_append_args *args, void *hip_stream);
  * token, or past rows[b] (NULL: T), is 0.  What lies in tokens that a row does not see,
  * NaN included, does not enter; a value of v past the bf16 range counts as NaN, one of k as
  * an infinity (where 2^8 times the sum of the probabilities' products with |v|, the largest
- * probability being 1, passes the float32 range, a result may be infinite or NaN).  lse
+ * probability being 1, passes the float32 range, a result may be NaN).  lse
  * (NULL: not stored) is the natural logarithm of the sum of the exponentials, -inf for
  * such a row; two results over different tokens join with it.  Scores and sums are
  * float32; with bf16 q a probability is rounded to bf16 once, with float32 q neither q nor

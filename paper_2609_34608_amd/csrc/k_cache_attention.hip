@@ -156,6 +156,13 @@ __device__ __forceinline__ void drop_far(Codes<DB>& v, int token, int lg, int* f
     if (v.s[s] == kFp4NaN) v.s[s] = 0;
 }
 
+// A value of a row from its sum and the probabilities' (inv: 1 / total): 0 where the row saw
+// nothing, and NaN where a value of v past the bf16 range, an infinity in the product, came in
+// without a mask (under one drop_far keeps it out).
+__device__ __forceinline__ float value_of(float sum, float total, float inv) {
+  return total == 0.f ? 0.f : fabsf(sum) < INFINITY ? sum * inv : NAN;
+}
+
 // DB: blocks of a head; QT: tiles of 16 rows; NS: bf16 parts of q and of a probability
 template <int DB, int QT, int NS>
 __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p) {
@@ -438,7 +445,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const float x = sees > odd[d + k] && a.causal ? NAN : o[i][j][k];
-          w.v[k] = static_cast<T>(total == 0.f ? 0.f : x * inv);
+          w.v[k] = static_cast<T>(value_of(x, total, inv));
         }
         *reinterpret_cast<Pack<T, 4>*>(out + d) = w;
       }
@@ -507,7 +514,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
       T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + t * a.out_stride[1] + h * a.out_stride[2];
       Pack<T, 4> w;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w.v[k] = static_cast<T>(total == 0.f ? 0.f : sum[k] * inv);  // 0: a row that sees nothing
+      for (int k = 0; k < 4; ++k) w.v[k] = static_cast<T>(value_of(sum[k], total, inv));
       *reinterpret_cast<Pack<T, 4>*>(out + d) = w;
       if (a.lse && d == 0)
         a.lse[b * a.lse_stride[0] + t * a.lse_stride[1] + h * a.lse_stride[2]] =
@@ -572,7 +579,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendParams p) {
   T* out = static_cast<T*>(a.out) + b * a.out_stride[0] + t * a.out_stride[1] + h * a.out_stride[2];
   Pack<T, 4> w;
 #pragma unroll
-  for (int k = 0; k < 4; ++k) w.v[k] = static_cast<T>(total == 0.f ? 0.f : x[k] * inv);
+  for (int k = 0; k < 4; ++k) w.v[k] = static_cast<T>(value_of(x[k], total, inv));
   if (mine) *reinterpret_cast<Pack<T, 4>*>(out + 4 * at) = w;
   if (a.lse && lane == 0)
     a.lse[b * a.lse_stride[0] + t * a.lse_stride[1] + h * a.lse_stride[2]] =

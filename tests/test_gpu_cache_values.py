@@ -1,0 +1,69 @@
+"""Attention over the 4-bit cache where values, keys and scores come next to the ends of
+their types' ranges or pass them, against float64 (fp4_ref)."""
+import math
+
+import pytest
+import torch
+
+import fp4_ref as F
+from gpu_common import device
+from test_gpu_cache import BF16, F32, _attend_case, _ints, _rand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dev():
+    return device()
+
+
+@pytest.fixture(scope="module")
+def R():
+    from paper_2609_34608_amd import runtime
+    return runtime
+
+
+# B, T, Hq, H, dh, page, lengths: waves that share tokens, waves with rows of their own, tokens split
+# over blocks (parts that one wave joins, and four), 32 and 64 rows a wave
+SIZES = [
+    (1, 40, 2, 1, 64, 16, (300,)),
+    (2, 90, 3, 3, 128, 16, (120, 177)),
+    (1, 24, 2, 2, 32, 16, (9000,)),
+    (1, 130, 2, 2, 96, 32, (256,)),
+    (3, 3, 4, 2, 64, 64, (3000, 200, 2500)),
+    (1, 2, 2, 2, 128, 64, (20000,)),
+]
+
+
+def _place(table, size, b, t):
+    return int(table[b, t // size[5]]), t % size[5]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", SIZES)
+def test_values_past_the_range_without_a_mask(dev, R, size, dtype):
+    """A value of v past the bf16 range is NaN, not infinite, for every row that sees it, in
+    its dim alone; the others are as if it were zero.  Rows that see nothing stay 0."""
+    q, cache, table, lengths = _attend_case(R, dev, size, dtype)
+    B, T, Hq, H, dh = size[:5]
+    g = torch.Generator().manual_seed(3)
+    bad = torch.zeros(B, T, Hq, dh, dtype=torch.bool)
+    clean = R.KvCache(cache.k, cache.k_scale, cache.v.clone(), cache.v_scale.clone())
+    for b in range(B):
+        for i, t in enumerate(torch.randperm(int(lengths[b]), generator=g)[:4].tolist()):
+            h, block, e = (int(torch.randint(n, (1,), generator=g)) for n in (H, dh // 32, 32))
+            at = *_place(table, size, b, t), h
+            half = slice(block * 16, block * 16 + 16)
+            for c in (cache, clean):
+                c.v[at][half], c.v_scale[at][block] = 0, 0
+            cache.v_scale[at][block] = (253, 254, 255, 254)[i]
+            cache.v[at][half][e // 2] = (7 if i % 2 else 15) << 4 * (e % 2)  # 6 or -6
+            dims = slice(block * 32, block * 32 + 32) if i == 2 else block * 32 + e
+            bad[b, :, h * Hq // H:(h + 1) * Hq // H, dims] = True
+    rows = torch.full((B,), T - 1)
+    bad[:, T - 1] = False
+    lse = torch.full(q.shape[:3], 7.0, device=dev)
+    got = R.cache_attention(q, cache, table, lengths, rows=rows.to(torch.int32).to(dev), lse=lse).cpu()
+    o, l, eo, el = (x.cpu() for x in F.attention_whole(q, clean, table, lengths, rows=rows))
+    F.check(got, torch.where(bad, math.nan, o), eo, dtype)
+    F.check(lse, l, el, F32)

@@ -16,7 +16,11 @@
 //    lane group holds.
 // The softmax has a running maximum m (in units of log2) that moves when a tile passes it
 // by more than 8, so most tiles have no rescale; its denominator is one more MFMA
-// against ones, which sums exactly the rounded probabilities that multiply V.
+// against ones, which sums exactly the rounded probabilities that multiply V.  A
+// probability's exponent is one multiply-add of score, scale and -m.  m is a rounded product,
+// which from 2^22 on is no longer near the exact one that the multiply-add takes (from 2^32
+// on by more than the exponent's range), so from there the scores are scaled and rounded
+// first, as m was: the largest is then m.
 //
 // A block's four waves share the tokens of its rows, taking tiles in turn, and join through
 // LDS; where blocks are few, a sequence's tokens are split over blocks too, whose parts go
@@ -50,6 +54,7 @@ constexpr int kKeys = 64;      // tokens of a tile
 constexpr int kWaves = 4;
 constexpr float kNone = -3e38f;  // running maximum of a row that has seen nothing
 constexpr float kSlack = 8.f;    // a probability reaches 2^8 before the maximum moves
+constexpr float kSteep = 0x1p22f;  // a maximum from here on takes rounded scores
 constexpr uint32_t kFar = 253;   // scales from here on may pass the bf16 range
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -292,6 +297,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
     if (threadIdx.x < DH) odd[threadIdx.x] = INT32_MAX;
     __syncthreads();
   }
+  int unit = 0;  // whether scores are scaled before their exponents
   const int first = t_lo + (p.by_rows ? 0 : wid);
   int more = -1, turn = 0;
   if (first < t_hi) {
@@ -378,6 +384,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
       grown |= top[i] > m[i] + kSlack;
     }
     if (__any(grown)) {
+      bool steep = false;
 #pragma unroll
       for (int i = 0; i < QT; ++i) {
         top[i] = fmaxf(top[i], __shfl_xor(top[i], 16, 64));
@@ -387,7 +394,16 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
         l[i] *= f;
 #pragma unroll
         for (int j = 0; j < DT; ++j) o[i][j] *= f;
+        steep |= fabsf(to) >= kSteep && to != kNone;
       }
+      unit |= __builtin_amdgcn_readfirstlane(__any(steep));
+    }
+    const float mul = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(unit ? 1.f : p.log2_scale)));
+    if (unit) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) st[i][g] *= p.log2_scale;
     }
     // Half of the tile's tokens at a time, so that V^T of that half stays in registers for
     // all row tiles; the exponentials of the next row tile run between the matrix
@@ -400,7 +416,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           bf16 part[NS];
-          split<NS>(__builtin_amdgcn_exp2f(fmaf(st[i][2 * c + g][r], p.log2_scale, -m[i])), part);
+          split<NS>(__builtin_amdgcn_exp2f(fmaf(st[i][2 * c + g][r], mul, -m[i])), part);
 #pragma unroll
           for (int n = 0; n < NS; ++n) pf[decltype(N)::value & 1][n][g * 4 + r] = part[n];
         }

@@ -67,3 +67,53 @@ def test_values_past_the_range_without_a_mask(dev, R, size, dtype):
     o, l, eo, el = (x.cpu() for x in F.attention_whole(q, clean, table, lengths, rows=rows))
     F.check(got, torch.where(bad, math.nan, o), eo, dtype)
     F.check(lse, l, el, F32)
+
+
+def _scores_of_one_dim(R, dev, size, dtype, levels, e):
+    """A cache whose keys are zero but in dim 0, where they are 2^e times a value of levels, in
+    random order, and random values."""
+    q, cache, table, lengths = _attend_case(R, dev, size, dtype)
+    B, _, _, H, dh, page = size[:6]
+    g = torch.Generator().manual_seed(4)
+    k = torch.zeros(B, table.shape[1] * page, H, dh)
+    k[..., 0] = torch.tensor(levels)[torch.randint(len(levels), k.shape[:3], generator=g)] * 2.0 ** e
+    v = _rand(dev, 8, *k.shape)
+    R.cache_append(cache, k.to(dev), v, table, _ints(dev, *[0] * B))
+    q.zero_()
+    return q, cache, table, lengths
+
+
+def _tied(size, dtype, values):
+    """Bound of attention whose rows' tokens have weights of 0 or exactly 1: the float32 sums
+    over n tokens, as in fp4_ref.attention."""
+    return 2.0 ** -22 * (max(size[6]) / 32 + 16) * 2 * float(values.nan_to_num().abs().max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [1e7, 3e9, 1e13, 1e28])
+@pytest.mark.parametrize("size", SIZES)
+def test_scores_whose_steps_pass_the_exponent(dev, R, size, scale, dtype):
+    """From scores of 2^32 on a step of float32 is more than exp's range: the tokens of the
+    largest score share a row evenly all the same, and the row's sum is theirs.  Beside such
+    rows there are ordinary ones and ones whose scores are all zero.
+
+    The products with q are exact or, for tokens of one score, round alike, and scores differ
+    by half the largest at least; the logarithm takes the rounding of the scaled score
+    (2^-22 a matrix step, four roundings of 2^-24), which leaves no doubt about the weights."""
+    q, cache, table, lengths = _scores_of_one_dim(R, dev, size, dtype, (6.0, 3.0, 1.0, -3.0, -6.0, 0.5), 0)
+    B, T, Hq, _, dh = size[:5]
+    lead = (1 + torch.rand(B, T, Hq, generator=torch.Generator().manual_seed(5))).to(dev)
+    kind = (torch.arange(T, device=dev)[:, None] + torch.arange(Hq, device=dev)) % 5
+    small, none = kind == 3, kind == 4
+    lead = torch.where(kind == 1, -lead, lead)
+    lead = torch.where(none, 0.0, torch.where(small, lead / scale, lead))
+    q[..., 0] = lead.to(dtype)
+    lse = torch.full(q.shape[:3], 7.0, device=dev)
+    for causal in (False, True):
+        got = R.cache_attention(q, cache, table, lengths, causal=causal, scale=scale, lse=lse)
+        o, l, eo, el = F.attention_whole(q, cache, table, lengths, causal=causal, scale=scale)
+        far = ~(small | none).expand(B, T, Hq)
+        eo[far] = _tied(size, dtype, F.values(cache.v, cache.v_scale))
+        el[far] = 2.0 ** -22 * (dh / 32 + 2) * l[far].nan_to_num(neginf=0).abs()
+        F.check(got, o, eo, dtype)
+        F.check(lse, l, el, F32)

@@ -679,7 +679,8 @@ int wam_cache_append(const wam_cache_append_args *args, void *hip_stream);
  * over the tokens j < seen(b, t) of key head h / (Hq / cache.H), without those that
  * have no page.  seen is lengths[b], or, causal, lengths[b] - rows[b] + t + 1 (the last
  * rows[b] tokens are the rows' own), between 0 and the table's end.  A row that sees no
- * token, or past rows[b] (NULL: T), is 0.  What lies in tokens that a row does not see,
+ * token, or only ones whose scores are -infinity in float32 (in units of log2), or past
+ * rows[b] (NULL: T), is 0.  What lies in tokens that a row does not see,
  * NaN included, does not enter; a value of v past the bf16 range counts as NaN, one of k as
  * an infinity (where 2^8 times the sum of the probabilities' products with |v|, the largest
  * probability being 1, passes the float32 range, a result may be NaN).  lse

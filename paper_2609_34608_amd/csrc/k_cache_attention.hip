@@ -52,7 +52,7 @@ namespace {
 
 constexpr int kKeys = 64;      // tokens of a tile
 constexpr int kWaves = 4;
-constexpr float kNone = -3e38f;  // running maximum of a row that has seen nothing
+constexpr float kNone = -FLT_MAX;  // running maximum of a row that has seen nothing
 constexpr float kSlack = 8.f;    // a probability reaches 2^8 before the maximum moves
 constexpr float kSteep = 0x1p22f;  // a maximum from here on takes rounded scores
 constexpr uint32_t kFar = 253;   // scales from here on may pass the bf16 range

@@ -117,3 +117,17 @@ def test_scores_whose_steps_pass_the_exponent(dev, R, size, scale, dtype):
         el[far] = 2.0 ** -22 * (dh / 32 + 2) * l[far].nan_to_num(neginf=0).abs()
         F.check(got, o, eo, dtype)
         F.check(lse, l, el, F32)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", SIZES)
+def test_scores_near_the_lowest_float(dev, R, size, dtype):
+    """A row whose scores are the lowest that float32 holds still sees its tokens: -2^127 times
+    1.3 log2(e) is -3.19e38, of -3.40e38."""
+    q, cache, table, lengths = _scores_of_one_dim(R, dev, size, dtype, (1.0,), 0)
+    q[..., 0] = -2.0 ** 127
+    lse = torch.full(q.shape[:3], 7.0, device=dev)
+    got = R.cache_attention(q, cache, table, lengths, scale=1.3, lse=lse)
+    o, l, _, _ = F.attention_whole(q, cache, table, lengths, scale=1.3)
+    F.check(got, o, torch.full_like(o, _tied(size, dtype, F.values(cache.v, cache.v_scale))), dtype)
+    F.check(lse, l, 2.0 ** -22 * (size[4] / 32 + 2) * l.abs(), F32)

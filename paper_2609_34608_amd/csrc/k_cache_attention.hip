@@ -165,7 +165,7 @@ __device__ __forceinline__ void drop_far(Codes<DB>& v, int token, int lg, int* f
 // nothing, and NaN where a value of v past the bf16 range, an infinity in the product, came in
 // without a mask (under one drop_far keeps it out).
 __device__ __forceinline__ float value_of(float sum, float total, float inv) {
-  return total == 0.f ? 0.f : fabsf(sum) < INFINITY ? sum * inv : NAN;
+  return total == 0.f ? 0.f : fmaf(sum, inv, sum * 0.f);  // infinity * 0: NaN
 }
 
 // DB: blocks of a head; QT: tiles of 16 rows; NS: bf16 parts of q and of a probability

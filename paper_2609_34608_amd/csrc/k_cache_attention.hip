@@ -108,6 +108,24 @@ __device__ __forceinline__ void split(float x, bf16 (&part)[NS]) {
   }
 }
 
+// The same of q, which may lie past the bf16 range: eight bits a part, cut off instead of
+// rounded, so that the parts have one sign and the first is finite where q is.
+template <int NS>
+__device__ __forceinline__ void split_q(float x, bf16 (&part)[NS]) {
+  if (NS == 1 || !(fabsf(x) < INFINITY)) {
+    part[0] = static_cast<bf16>(x);
+#pragma unroll
+    for (int s = 1; s < NS; ++s) part[s] = (bf16)0.f;
+    return;
+  }
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const float top = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+    part[s] = static_cast<bf16>(top);
+    x -= top;
+  }
+}
+
 typedef __attribute__((address_space(1))) const uint8_t global_byte;
 
 // Codes and scales of 16 tokens: lane (r, g) has the words g DB .. + DB - 1 of token r
@@ -222,7 +240,7 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         bf16 part[NS];
-        split<NS>(x[e], part);
+        split_q<NS>(x[e], part);
 #pragma unroll
         for (int n = 0; n < NS; ++n) qf[i][s][n][e] = part[n];
       }

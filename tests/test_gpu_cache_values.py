@@ -131,3 +131,37 @@ def test_scores_near_the_lowest_float(dev, R, size, dtype):
     o, l, _, _ = F.attention_whole(q, cache, table, lengths, scale=1.3)
     F.check(got, o, torch.full_like(o, _tied(size, dtype, F.values(cache.v, cache.v_scale))), dtype)
     F.check(lse, l, 2.0 ** -22 * (size[4] / 32 + 2) * l.abs(), F32)
+
+
+@pytest.mark.parametrize("byte", [0, 2])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("size", SIZES)
+def test_queries_past_the_bf16_range(dev, R, size, causal, byte):
+    """The largest float32 values, which bf16 rounds to an infinity, against the smallest keys,
+    subnormal ones too; and an infinite q, which makes its own row NaN."""
+    q, cache, table, lengths = _attend_case(R, dev, size, F32)
+    g = torch.Generator().manual_seed(6)
+    q.copy_(torch.where(torch.rand(q.shape, generator=g) < 0.5, -1.0, 1.0)
+            * (3.39e38 + 1e36 * torch.rand(q.shape, generator=g)))
+    cache.k_scale.fill_(byte)
+    q[:, -1, -1, 3] = math.inf
+    lse = torch.full(q.shape[:3], 7.0, device=dev)
+    got = R.cache_attention(q, cache, table, lengths, causal=causal, lse=lse)
+    q[:, -1, -1, 3] = 0.0
+    o, l, eo, el = F.attention_whole(q, cache, table, lengths, causal=causal)
+    o[:, -1, -1], l[:, -1, -1] = math.nan, math.nan
+    F.check(got, o, eo, F32)
+    F.check(lse, l, el, F32)
+
+
+@pytest.mark.parametrize("size", SIZES)
+def test_queries_next_to_the_smallest(dev, R, size):
+    """float32 q whose later bits are subnormal in bf16 lose none down to its smallest, 2^-133."""
+    q, cache, table, lengths = _attend_case(R, dev, size, F32)
+    q.copy_(torch.round(q * 2.0 ** 18) * 2.0 ** -133)
+    cache.k_scale.copy_((cache.k_scale.int() + 115).to(torch.uint8))
+    lse = torch.full(q.shape[:3], 7.0, device=dev)
+    got = R.cache_attention(q, cache, table, lengths, lse=lse)
+    o, l, eo, el = F.attention_whole(q, cache, table, lengths)
+    F.check(got, o, eo, F32)
+    F.check(lse, l, el, F32)

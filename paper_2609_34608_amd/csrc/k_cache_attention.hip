@@ -108,21 +108,19 @@ __device__ __forceinline__ void split(float x, bf16 (&part)[NS]) {
   }
 }
 
-// The same of q, which may lie past the bf16 range: eight bits a part, cut off instead of
-// rounded, so that the parts have one sign and the first is finite where q is.
+// The same of q, which may lie past the bf16 range: the first part stays finite where q is.
 template <int NS>
 __device__ __forceinline__ void split_q(float x, bf16 (&part)[NS]) {
-  if (NS == 1 || !(fabsf(x) < INFINITY)) {
-    part[0] = static_cast<bf16>(x);
+  part[0] = static_cast<bf16>(x);
+  if constexpr (NS > 1) {
+    const bool finite = fabsf(x) < INFINITY;
+    if (finite && !(fabsf((float)part[0]) < INFINITY)) part[0] = (bf16)copysignf(0x1.fep127f, x);
+    x = finite ? x - (float)part[0] : 0.f;
 #pragma unroll
-    for (int s = 1; s < NS; ++s) part[s] = (bf16)0.f;
-    return;
-  }
-#pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const float top = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-    part[s] = static_cast<bf16>(top);
-    x -= top;
+    for (int s = 1; s < NS; ++s) {
+      part[s] = static_cast<bf16>(x);
+      x -= (float)part[s];
+    }
   }
 }
 

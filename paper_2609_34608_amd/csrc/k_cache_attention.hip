@@ -353,19 +353,38 @@ __global__ __launch_bounds__(kWaves* kWave, 2) void attend_kernel(AttendParams p
         *reinterpret_cast<bf16x8*>(own + (g * 16 + lr) * VROW + (lg * DB + s) * 16) =
             fp4_to_bf16(vc[g].w[s], fp4_scale_operand(scale_of(vc[g], s)));
     f32x4 st[QT][4];
+    auto scores = [&](auto FAR) __attribute__((always_inline)) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
+      for (int g = 0; g < 4; ++g) {
 #pragma unroll
-      for (int i = 0; i < QT; ++i) st[i][g] = zero;
+        for (int i = 0; i < QT; ++i) st[i][g] = zero;
 #pragma unroll
-      for (int s = 0; s < DB; ++s) {
-        const bf16x8 kf = fp4_to_bf16(kc[g].w[s], fp4_scale_operand(scale_of(kc[g], s)));
+        for (int s = 0; s < DB; ++s) {
+          const bf16x8 kf = fp4_to_bf16(kc[g].w[s], fp4_scale_operand(scale_of(kc[g], s)));
+          bf16x8 rest = kf;  // for the later parts of q
+          if constexpr (decltype(FAR)::value) {
 #pragma unroll
-        for (int i = 0; i < QT; ++i)
+            for (int e = 0; e < 8; ++e)
+              if (!(fabsf((float)rest[e]) < INFINITY)) rest[e] = (bf16)0.f;
+          }
 #pragma unroll
-          for (int n = 0; n < NS; ++n)
-            st[i][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i][s][n], st[i][g], 0, 0, 0);
+          for (int i = 0; i < QT; ++i)
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+              st[i][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(n ? rest : kf, qf[i][s][n], st[i][g], 0, 0, 0);
+        }
       }
+    };
+    scores(std::false_type{});
+    if constexpr (NS > 1) {
+      // a key past the bf16 range, an infinity, meets the first part of q alone: the others may be
+      // zero, and add nothing to an infinite score
+      uint32_t far = 0;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int s = 0; s < DB; ++s) far = max(far, scale_of(kc[g], s));
+      if (__any(far >= kFar)) scores(std::true_type{});
     }
     if (tile + stride < t_hi) {
       if (++turn == 16) {

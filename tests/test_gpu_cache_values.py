@@ -133,6 +133,38 @@ def test_scores_near_the_lowest_float(dev, R, size, dtype):
     F.check(lse, l, 2.0 ** -22 * (size[4] / 32 + 2) * l.abs(), F32)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("size", SIZES)
+def test_keys_past_the_range(dev, R, size, causal, dtype):
+    """A value of k past the bf16 range is an infinity: where the row's q has the other sign
+    the token has no weight, and the row is what it is without the token; where it has the
+    same sign or is zero the score is infinite or NaN, and the row NaN."""
+    q, cache, table, lengths = _attend_case(R, dev, size, dtype)
+    B, T, Hq, H, dh, page = size[:6]
+    one, rest = dh - 5, slice(dh // 2 - 16, dh // 2)
+    kind = (torch.arange(T, device=dev)[:, None] + torch.arange(Hq, device=dev)) % 4
+    x = q[..., one].float().abs() + 0.25
+    x = torch.where(kind == 1, 0.5, x)  # exact in bf16
+    x = torch.where(kind == 2, -x, x)
+    q[..., one] = torch.where(kind == 3, 0.0, x).to(dtype)
+    without = table.clone()
+    for b in range(B):
+        for p in (0, (int(lengths[b]) - T) // page - 1):  # pages that every row sees
+            at = int(table[b, p])
+            without[b, p] = -1
+            cache.k[at, ..., rest] = 0
+            cache.k[at, ..., one // 2] = 0xf << 4 * (one % 2)  # -6
+            cache.k_scale[at, ..., -1] = torch.tensor([253, 254])[torch.arange(page) % 2][:, None].to(dev)
+    lse = torch.full(q.shape[:3], 7.0, device=dev)
+    got = R.cache_attention(q, cache, table, lengths, causal=causal, lse=lse)
+    o, l, eo, el = F.attention_whole(q, cache, without, lengths, causal=causal)
+    bad = (kind >= 2).expand(B, T, Hq)
+    o[bad], l[bad] = math.nan, math.nan
+    F.check(got, o, eo, dtype)
+    F.check(lse, l, el, F32)
+
+
 @pytest.mark.parametrize("byte", [0, 2])
 @pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("size", SIZES)

@@ -421,7 +421,8 @@ const char *wam_noalloc_last_error(void);
 /* ---- layer operators ---------------------------------------------------------- */
 /* Operators of a transformer layer on caller-owned device buffers, without a
  * handle: rotary positions over several axes, the norms around a block with
- * its gate and residual, 8-bit blocks and their product.  Each is enqueued on
+ * its gate and residual, 8-bit and 4-bit blocks and their products, a cache of
+ * keys and values and attention over it.  Each is enqueued on
  * hip_stream (NULL: the default stream) of the current device, allocates
  * nothing, shares no scratch between calls (calls may overlap), does not
  * synchronise and may be captured into a graph.  Struct and host pointers are

@@ -764,6 +764,9 @@ int wam_cache_attention(const wam_cache_attention_args* a, void* hip_stream) {
       (a->lse && (!strides_ok(a->lse_stride, 3) || !distinct(a->lse_stride, size, 3, 1))))
     return noalloc_fail(WAM_E_ARG, "wam_cache_attention: the elements of a result must be distinct");
   if (a->q == a->out) return noalloc_fail(WAM_E_ARG, "wam_cache_attention: out must not be q");
+  const void* lse = a->lse;
+  if (lse && (lse == a->q || lse == a->out))
+    return noalloc_fail(WAM_E_ARG, "wam_cache_attention: lse must be a buffer of its own");
   const AttendPlan pl = plan_attend(*a);
   if (const size_t need = workspace_of(*a, pl)) {
     if (!a->workspace || !aligned_to(a->workspace, 16) || a->workspace_bytes < need)

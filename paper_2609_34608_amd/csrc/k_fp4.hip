@@ -319,6 +319,9 @@ int check_cache(const wam_cache& c, const wam_page_table& t, bool written, bool 
   if (c.H > WAM_MAX_ROWS) return fail(WAM_E_SHAPE, "too many heads");
   if (empty || c.pages == 0 || t.width == 0) return WAM_OK;
   if (!c.k || !c.v || !c.k_scale || !c.v_scale || !t.entry) return fail(WAM_E_ARG, "null cache or table");
+  if (written && (c.k == c.v || c.k_scale == c.v_scale || c.k == c.k_scale || c.k == c.v_scale || c.v == c.k_scale ||
+                  c.v == c.v_scale))
+    return fail(WAM_E_ARG, "the cache's arrays must be different buffers");
   if (!aligned_to(c.k, 4) || !aligned_to(c.v, 4) || !aligned_to(t.entry, 4))
     return fail(WAM_E_ARG, "codes and table must start on 4 bytes");
   if (!strides_ok(c.k_stride, 3) || !strides_ok(c.v_stride, 3) || !strides_ok(c.k_scale_stride, 3) ||

@@ -16,8 +16,9 @@
 // The eight scale bytes of each row of a stage travel with it, by 4-byte loads
 // straight into LDS.
 //
-// What bounds it: 10176 x 6144 x 1536 takes 66 us (2.9 PFLOP/s; the instruction alone
-// reaches 9.5), 71 with the GELU.  A 256x256 tile's six stages are 9.3 us of it each, at
+// What bounds it: 10176 x 6144 x 1536 takes 64 us (3.0 PFLOP/s; the instruction alone
+// reaches 9.5), 71 with the GELU, once the card has done such work for 40 ms (the clock moves: up
+// to 95 before).  A 256x256 tile's six stages are 9.3 us of it each, at
 // 55% of the matrix rate, and what it costs beside them 5.3: its first loads, the
 // activation, and a result whose 125 MB alone take 20 us of memory.
 #pragma once

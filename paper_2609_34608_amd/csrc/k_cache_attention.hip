@@ -16,11 +16,14 @@
 //    lane group holds.
 // The softmax has a running maximum m (in units of log2) that moves when a tile passes it
 // by more than 8, so most tiles have no rescale; its denominator is one more MFMA
-// against ones, which sums exactly the rounded probabilities that multiply V.  A
-// probability's exponent is one multiply-add of score, scale and -m.  m is a rounded product,
-// which from 2^22 on is no longer near the exact one that the multiply-add takes (from 2^32
-// on by more than the exponent's range), so from there the scores are scaled and rounded
-// first, as m was: the largest is then m.
+// against ones, which sums exactly the rounded probabilities that multiply V.  Under bf16 q
+// they are rounded to bf16, the instruction's type (results are then 0.0023 off the definition,
+// 0.0017 by their own rounding alone); float32 q and its probabilities go in three bf16
+// parts, at 2.4 times the time.
+// A probability's exponent is one multiply-add of score, scale and -m.  m is a rounded
+// product, which from 2^22 on is no longer near the exact one that the multiply-add takes (from
+// 2^32 on by more than the exponent's range), so from there the scores are scaled and
+// rounded first, as m was: the largest is then m.
 //
 // A block's four waves share the tokens of its rows, taking tiles in turn, and join through
 // LDS; where blocks are few, a sequence's tokens are split over blocks too, whose parts go
@@ -29,12 +32,12 @@
 //
 // What bounds it, on one MI355X: single rows the bytes of the cache (16 streams of 16384 to
 // 32768 tokens, 8 heads of 128: 91 us, 4.8 TB/s; a 1 GiB copy reaches 5.0); many rows the
-// instructions: 10176 rows of 24 heads of 64 over 20352 tokens take 1416 us, 899 TFLOP/s
+// instructions: 10176 rows of 24 heads of 64 over 20352 tokens take 1440 us, 884 TFLOP/s
 // (a bf16 product of 8192^3 reaches 1213), the matrix cores 40% busy, at 2.1 GHz, to which
 // the power of this mix brings the clock down.  A form for many rows that converts tokens
 // once for four waves of 64 rows, with 32x32x16 products between the exponentials and
 // without the maximum, has half the matrix instructions and 30% fewer others, and took as
-// long (1340 to 1410 us; shorter sequences longer), so this one stays.
+// long (1340 to 1410 us, this one 1416 then; shorter sequences longer), so this one stays.
 #include <float.h>
 #include <math.h>
 
@@ -660,7 +663,9 @@ AttendPlan plan_attend(const wam_cache_attention_args& a) {
   while (pl.qt < most && pl.qt * 16 < R) pl.qt *= 2;
   pl.row_blocks = (int)((R + pl.qt * 16 - 1) / (pl.qt * 16));
   const int64_t blocks = pairs * pl.row_blocks;
-  // blocks that the chip holds at once, by their registers and LDS
+  // Blocks counted as a round: what 256 CUs hold at once, by registers and LDS, of most forms
+  // (two a CU, three of 16 rows of 64).  Heads of 32 hold others: five of 16 bf16 rows and three
+  // of 16 float32 rows a CU, where four are counted, and three of 32 bf16 rows, where two are.
   const int64_t slots = pl.qt == 1 && narrow ? a.cache.dh == 32 ? 1024 : 768 : 512;
   // Few tiles leave waves that share them without work, or with less of it than joining
   // costs (9 x 4924 rows of 9 heads over 60 tokens 143 -> 44 us, 8 x 1000 of 16 over 700

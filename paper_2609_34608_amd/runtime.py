@@ -886,7 +886,9 @@ def cache_attention(q, cache, table, lengths, *, rows=None, causal=False, scale=
     last tokens are the rows' own, and row t sees those up to its own.  rows int32 [B]:
     only the first rows[b] of a sequence count, the others' results are 0, as are those
     of rows that see no token.  scale: default 1 / sqrt(dh).  Returns out, of q's shape
-    and type; lse: a float32 [B, T, Hq] buffer for the logarithm of each row's sum."""
+    and type; lse: a float32 [B, T, Hq] buffer for the logarithm of each row's sum.  The
+    call is planned by the table's width: table[:, :n] with the pages that the longest
+    sequence needs is faster than one of a whole context."""
     index = _first(q, "cache_attention: q", _REAL, 4)
     B, T, Hq, dh = q.shape
     held = _cache_values(cache, table, index, B, None, dh, "cache_attention")
